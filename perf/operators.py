@@ -310,7 +310,7 @@ def _plain_rope(s):
 # ------------------------------------------------------------------------------------------------------ the own calls
 def _context(case, longest):
     from paper_2411_05787_b200 import rkv
-    key = (case["batch"], case.get("q_heads", case["kv_heads"]), case["kv_heads"], longest)
+    key = (case.get("batch", 1), case.get("q_heads", case["kv_heads"]), case["kv_heads"], longest)
     if key not in _contexts:
         _contexts[key] = rkv.Context(*key, max(1, case.get("keep", 1)))
     return _contexts[key]
@@ -318,29 +318,31 @@ def _context(case, longest):
 
 def _own(s):
     case, op = s["case"], s["op"]
-    if op == "rope":
-        from paper_2411_05787_b200 import harness
-        if "table" not in s:
-            s["table"] = harness.RopeTable(case["rot"], THETA, case["layout"], case["scaling"], case["factor"],
-                                           trained_len=TRAINED, low=LOW, high=HIGH, fast=FAST, slow=SLOW,
-                                           device=s["qkv"].device)
-        harness.rope(s["qkv"], s["pos"], s["table"], s["q"], s["k"], s["v"])
-        return
     from paper_2411_05787_b200 import rkv
+    if op == "rope":
+        if "table" not in s:
+            s["table"] = rkv.RopeTable(case["rot"], THETA, case["layout"], case["scaling"], case["factor"],
+                                       trained_len=TRAINED, low=LOW, high=HIGH, fast=FAST, slow=SLOW,
+                                       device=s["qkv"].device)
+            s["ctx"] = _context(case, 1)
+        s["ctx"].rope(s["qkv"], s["pos"], s["table"], s["q"], s["k"], s["v"])
+        return
     if "cache" not in s:
-        s["cache"] = rkv.cache_q8_struct(s["k8"], s["v8"], s["k_scale"], s["v_scale"], s["row_offset"], s["cap"], s["len"])
+        s["cache"] = rkv.quant_cache_struct(s["k8"], s["v8"], s["k_scale"], s["v_scale"], s["row_offset"], s["cap"],
+                                            s["len"])
         s["ctx"] = _context(case, int(s["cap"].max()))
         if op == "rebuild":
             s["small"] = rkv.cache_struct(s["small_k"], s["small_v"], s["small_offset"], s["small_cap"], s["small_len"])
     ctx, cache = s["ctx"], s["cache"]
     if op == "store":
-        ctx.q8_store(s["k_new"], s["v_new"], cache, start=s["start"], count=s["count"])
+        ctx.quant_store(s["k_new"], s["v_new"], cache, start=s["start"], count=s["count"])
     elif op == "attend":
-        ctx.q8_full_attention(s["q"], cache, s["out"], active=s["active"], max_len_hint=case["length"])
+        ctx.quant_full_attention(s["q"], cache, s["out"], active=s["active"], max_len_hint=case["length"],
+                                 keep_logits=case["scores"])
         if case["scores"]:
-            ctx.score_keys(s["q"], cache.rows, s["k_small"], 1, active=s["active"], scores=s["scores"])
+            ctx.score_keys(s["q"], cache, s["k_small"], 1, active=s["active"], scores=s["scores"])
     else:
-        ctx.q8_gather_small(s["topk_idx"], s["k_small"], s["topk_idx"].shape[-1], cache, s["small"])
+        ctx.quant_gather_small(s["topk_idx"], s["k_small"], s["topk_idx"].shape[-1], cache, s["small"])
 
 
 def run(s):
