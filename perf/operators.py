@@ -310,9 +310,9 @@ def _plain_rope(s):
 # ------------------------------------------------------------------------------------------------------ the own calls
 def _context(case, longest):
     from paper_2411_05787_b200 import rkv
-    key = (case.get("batch", 1), case.get("q_heads", case["kv_heads"]), case["kv_heads"], longest)
+    key = (case.get("batch", 1), case.get("q_heads", case["kv_heads"]), case["kv_heads"], longest, case.get("keep", 1))
     if key not in _contexts:
-        _contexts[key] = rkv.Context(*key, max(1, case.get("keep", 1)))
+        _contexts[key] = rkv.Context(*key)
     return _contexts[key]
 
 
