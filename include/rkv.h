@@ -67,6 +67,9 @@ typedef enum {
                                      are not valid.  Never seen in a healthy run; the waits are bounded so that
                                      a lost copy cannot hang the GPU                                          */
 
+#define RKV_DEV_BAD_LAYOUT 32     /* a sequence of an rkv_quant_cache whose row_offset or cap is no multiple of 64, or
+                                     whose rows leave the buffer: nothing is read or written for it (attention: zeros) */
+
 /* score aggregation over the query heads of a group (Sec. 2.2 footnote; App. A.3, Table 6) */
 typedef enum { RKV_AGG_MAX = 0, RKV_AGG_MEAN = 1, RKV_AGG_FIRST = 2 } rkv_agg;
 
@@ -92,6 +95,27 @@ typedef struct {
                              /*     in positions                 } may read them early    */
   int32_t* len;              /* [B] current length; append / gather_small update it    */
 } rkv_cache;
+
+/*
+ * Full cache in 8 bits (no counterpart in the paper: C_f is what its method keeps in memory, Sec. 2.2, and what the
+ * full step streams).  Rows are 128 e4m3 codes (128 bytes); the positions 64 i .. 64 i + 63 of a KV head share one
+ * scale, K and V apart:
+ *   value = code * scale.
+ * Sequence b, KV head g, position p is row r = row_offset[b] + g * cap[b] + p, its scale is scale[r / 64]; row_offset[b]
+ * and cap[b] are multiples of 64 (RKV_DEV_BAD_LAYOUT otherwise).  rkv_quant_store writes scales that are powers of two,
+ * at least 2^-126 and at most 2^120; the calls that read accept any finite scale >= 0.
+ */
+#define RKV_QUANT_BLOCK 64
+typedef struct {
+  void* k;                   /* e4m3 [n_rows][128], 16-byte aligned                    */
+  void* v;                   /* e4m3 [n_rows][128], 16-byte aligned                    */
+  float* k_scale;            /* fp32 [n_rows / 64]                                     */
+  float* v_scale;            /* fp32 [n_rows / 64]                                     */
+  int64_t n_rows;            /* host value: rows in each buffer, a multiple of 64 (< 2^31) */
+  const int64_t* row_offset; /* [B] as in rkv_cache, multiples of 64                   */
+  const int32_t* cap;        /* [B] as in rkv_cache, multiples of 64                   */
+  int32_t* len;              /* [B] current length; rkv_quant_store updates it         */
+} rkv_quant_cache;
 
 /* Host.  Creates a context on the current device and allocates its workspace
  * (cudaMalloc).  *out is NULL on failure. */
@@ -264,6 +288,59 @@ rkv_status rkv_append_small_step_evict(rkv_ctx* ctx, const void* q, const void* 
                                        const int32_t* active, void* out, const int32_t* evict_order,
                                        int32_t* evict_count, int32_t max_evict, int32_t max_len_hint,
                                        void* stream);
+
+/*
+ * Append rows to an 8-bit cache: a prompt's, a chunk's, or one token's (Sec. 2.1).  Row t < count[b] of sequence b goes
+ * to position start[b] + t of every KV head, and len[b] becomes start[b] + count[b].  start == NULL: the current
+ * lengths (append); otherwise start[b] <= len[b], and what lay from start[b] on is given up (a rejected draft, say).
+ * count == NULL: n_tok rows for every sequence; count[b] <= 0: none, and the sequence is cut to start[b].
+ * For each block of 64 positions that receives rows, with a = the largest finite |x| among the new ones:
+ *   scale' = the smallest power of two >= max(a / 448, 2^-126);  if the block holds positions below start[b], not below
+ *            their scale, and where it is above, their codes become rne(code * scale / scale');
+ *   code   = rne(x / scale'), rne = round to nearest even on the e4m3 grid.
+ * NaN and infinities are stored as NaN and set RKV_DEV_NONFINITE.  Rows beyond cap[b] are dropped and set
+ * RKV_DEV_APPEND_OVERFLOW; start[b] outside 0 .. min(len[b], cap[b]) sets RKV_DEV_LEN_CLAMPED and leaves the
+ * sequence as it is.  Rows of the buffer outside start .. start + count - 1 keep their values.
+ *   k_new, v_new   bf16; head g of row t of sequence b starts at  b * seq_stride + t * tok_stride + g * 128  (elements;
+ *                  strides are multiples of 8, so that rows can lie inside a projection's output)
+ *   n_tok          host value >= 1: rows per sequence in k_new and v_new; count[b] above it is cut to it
+ *   start, count   int32 [B] or NULL
+ */
+rkv_status rkv_quant_store(rkv_ctx* ctx, const void* k_new, int64_t k_seq_stride, int64_t k_tok_stride,
+                           const void* v_new, int64_t v_seq_stride, int64_t v_tok_stride, int32_t n_tok,
+                           const int32_t* start, const int32_t* count, const rkv_quant_cache* full /*host struct*/,
+                           void* stream);
+
+/*
+ * Attention over an 8-bit cache: rkv_full_attention on its values (code * scale), half the bytes.  keep_logits != 0
+ * leaves the logits and softmax statistics in the workspace, and rkv_quant_select_topk (or rkv_quant_score_keys, then
+ * rkv_quant_select_topk) completes the step exactly as rkv_select_topk / rkv_score_keys complete rkv_full_attention;
+ * keep_logits == 0 is attention alone, without the writes that the scores need.  rkv_quant_full_step is
+ * rkv_full_step over an 8-bit cache.  Other arguments as in those calls.  Two kernels (attention, fold), or three
+ * (attention, scores with the fold, selection).
+ */
+rkv_status rkv_quant_full_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full /*host struct*/,
+                                    const int32_t* active, void* out, int32_t keep_logits, int32_t max_len_hint,
+                                    void* stream);
+rkv_status rkv_quant_score_keys(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full /*host struct*/,
+                                const int32_t* k_small, int32_t k_max, const int32_t* active, float* scores,
+                                int64_t score_stride, void* q_last_full, void* stream);
+rkv_status rkv_quant_select_topk(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full /*host struct*/,
+                                 const int32_t* k_small, int32_t k_max, const int32_t* active, float* scores,
+                                 int64_t score_stride, int32_t* topk_idx, void* q_last_full, void* stream);
+rkv_status rkv_quant_full_step(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full /*host struct*/,
+                               const int32_t* k_small, int32_t k_max, const int32_t* active, void* out, float* scores,
+                               int64_t score_stride, int32_t* topk_idx, void* q_last_full, int32_t max_len_hint,
+                               void* stream);
+
+/*
+ * Rebuild of the bf16 small cache from an 8-bit full cache: rkv_gather_small with
+ *   small.K[b][g][r] = bf16(code * scale) of full's position topk_idx[b][g][r]    (same for V),
+ * exact for scales that are powers of two.  Bad indices, active masks and lengths as there.
+ */
+rkv_status rkv_quant_gather_small(rkv_ctx* ctx, const int32_t* topk_idx, const int32_t* k_small, int32_t k_max,
+                                  const rkv_quant_cache* full /*host struct*/, const rkv_cache* small_cache /*host struct*/,
+                                  const int32_t* active, void* stream);
 
 /*
  * Refresh trigger (Sec. 2.2 "Deciding when to decode with full cache").

@@ -12,6 +12,7 @@ namespace {
 
 using rkv::AttnParams;
 using rkv::CacheDev;
+using rkv::QuantDev;
 using rkv::ScoreParams;
 using rkv::SelectParams;
 
@@ -96,9 +97,28 @@ struct LaunchScope {
 
 CacheDev dev_of(const rkv_cache* c) { return CacheDev{c->k, c->v, c->row_offset, c->cap, c->len}; }
 
-// [n_rows][128] bf16 as {64 channels, row, half}: one box = 64 rows x both halves, 128-byte swizzle
-rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out) {
-  const std::pair<uint64_t, int64_t> key(reinterpret_cast<uint64_t>(base), n_rows);   // the map depends on nothing else
+QuantDev dev_of(const rkv_quant_cache* c) {
+  return QuantDev{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scale, c->v_scale,
+                  c->row_offset, c->cap, c->len, c->n_rows};
+}
+bool quant_ok(const rkv_quant_cache* c) {
+  return c && c->k && c->v && c->k_scale && c->v_scale && c->row_offset && c->cap && c->len && c->n_rows > 0 &&
+         c->n_rows < (int64_t(1) << 31) && c->n_rows % rkv::kQuantBlock == 0 && aligned16(c->k) && aligned16(c->v) &&
+         (reinterpret_cast<uintptr_t>(c->k_scale) & 3) == 0 && (reinterpret_cast<uintptr_t>(c->v_scale) & 3) == 0;
+}
+// What the score pass and the selection read of a cache: its sizes (the rows' pointer is its identity there).
+rkv_cache sizes_of(const rkv_quant_cache* c) { return rkv_cache{c->k, c->v, c->n_rows, c->row_offset, c->cap, c->len}; }
+// The 8-bit calls launch on the context's device only.
+bool on_device(const rkv_ctx* ctx) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device;
+}
+
+// [n_rows][128] bf16 as {64 channels, row, half}: one box = 64 rows x both halves, 128-byte swizzle.
+// quant: [n_rows][128] codes, one box = 128 rows.
+rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out, bool quant = false) {
+  // the map depends on nothing else
+  const std::pair<uint64_t, int64_t> key(reinterpret_cast<uint64_t>(base), quant ? -n_rows : n_rows);
   auto it = ctx->tmaps.find(key);
   if (it != ctx->tmaps.end()) { *out = it->second; return RKV_OK; }
   if (g_encode == nullptr) {
@@ -110,7 +130,7 @@ rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out
     g_encode = reinterpret_cast<rkv::EncodeTiledFn>(fn);
   }
   CUtensorMap tm;
-  CUresult r = rkv::encode_cache_map(g_encode, base, n_rows, &tm);
+  CUresult r = quant ? rkv::encode_quant_map(g_encode, base, n_rows, &tm) : rkv::encode_cache_map(g_encode, base, n_rows, &tm);
   if (r != CUDA_SUCCESS) {
     ctx->last_error = "cuTensorMapEncodeTiled failed with CUresult " + std::to_string((int)r);
     return RKV_ERR_CUDA;
@@ -249,6 +269,56 @@ rkv_status run_attention(rkv_ctx* ctx, const void* q, const rkv_cache* cache, co
   return RKV_OK;
 }
 
+// The pass over the 8-bit cache: the same splits and workspace as the streaming form above, tiles of 128 positions
+// dealt out in turn.
+rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cache* cache, const int32_t* active,
+                               void* out, int n_max, bool logits, cudaStream_t st, int* gx_out) {
+  if (!aligned16(q) || !aligned16(out)) return RKV_ERR_INVALID_ARG;
+  CUtensorMap tm_k, tm_v;
+  rkv_status s = tensor_map(ctx, cache->k, cache->n_rows, &tm_k, true);
+  if (s != RKV_OK) return s;
+  s = tensor_map(ctx, cache->v, cache->n_rows, &tm_v, true);
+  if (s != RKV_OK) return s;
+  int gx = 1;
+  choose_chunk(ctx, n_max, true, &gx);
+  const int tiles = (n_max + rkv::kQuantTile - 1) / rkv::kQuantTile;
+  if (gx > tiles) gx = tiles;
+  rkv::QuantAttnParams p;
+  memset(&p, 0, sizeof(p));
+  p.q = q;
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.row_offset = cache->row_offset;
+  p.cap = cache->cap;
+  p.len = cache->len;
+  p.active = active;
+  p.out = out;
+  p.partials = ctx->partials;
+  p.ml_t = ctx->ml_t;
+  p.logits = logits ? ctx->logits : nullptr;
+  p.status = ctx->status;
+  p.n_rows = cache->n_rows;
+  p.logit_stride = ctx->logit_stride;
+  p.n_q_heads = ctx->cfg.n_q_heads;
+  p.n_kv_heads = ctx->cfg.n_kv_heads;
+  p.group = ctx->group;
+  p.gp = ctx->gp;
+  p.max_splits = ctx->max_splits;
+  p.max_len = n_max;
+  p.spec = (active == nullptr && ctx->cfg.n_seq == 1) ? 1 : 0;
+  p.scale = ctx->cfg.softmax_scale;
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_ATTN_FULL);
+    e = rkv::launch_quant_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit attention launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  *gx_out = gx;
+  return RKV_OK;
+}
+
 }  // namespace
 
 namespace rkv {
@@ -340,6 +410,7 @@ rkv_status rkv_create(const rkv_config* cfg, rkv_ctx** out) {
     if (!g_prepared[ctx->device]) {
       e = rkv::prepare_attention();
       if (e == cudaSuccess) e = rkv::prepare_select();
+      if (e == cudaSuccess) e = rkv::prepare_quant_attention();
       if (e != cudaSuccess) { delete ctx; return RKV_ERR_CUDA; }
       g_prepared[ctx->device] = true;
     }
@@ -529,6 +600,110 @@ static rkv_status full_step_impl(rkv_ctx* ctx, const void* q, const rkv_cache* f
   rkv_status s = full_attention_part(ctx, q, full, active, out, max_len_hint, st, score_only, false);
   if (s != RKV_OK) return s;
   return select_part(ctx, q, full, k_small, k_max, active, out, scores, score_stride, topk_idx, q_last_full, st);
+}
+
+// The 8-bit cache's first half: as full_attention_part.  Without kept logits there is nothing for a second half.
+static rkv_status quant_attention_part(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full, const int32_t* active,
+                                       void* out, int32_t max_len_hint, bool logits, bool fold_out, cudaStream_t st) {
+  if (!ctx || !q || !quant_ok(full) || !out || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+  const int n_max = max_len_hint == 0 ? ctx->cfg.max_len : max_len_hint;
+  if (n_max < 1 || n_max > ctx->cfg.max_len) return RKV_ERR_INVALID_ARG;
+  int gx = 1;
+  ctx->pending_full.valid = false;
+  ctx->pending_keys.valid = false;
+  rkv_status s = run_quant_attention(ctx, q, full, active, out, n_max, logits, st, &gx);
+  if (s != RKV_OK) return s;
+  if (fold_out) {
+    cudaError_t e;
+    {
+      LaunchScope scope(ctx, st, RKV_KERNEL_FOLD);
+      e = rkv::launch_fold(ctx->partials, ctx->ml_t, full->len, full->cap, active, out, ctx->cfg.n_seq,
+                           ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads, rkv::kQuantTile, ctx->max_splits, n_max, gx, st);
+    }
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "fold launch");
+    ctx->launches += 1;
+    rkv::note_launch(st, nullptr, nullptr, true);
+  }
+  if (logits) ctx->pending_full = {true, rkv::kQuantTile, gx, n_max, full->k, active};
+  return RKV_OK;
+}
+
+rkv_status rkv_quant_full_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full, const int32_t* active,
+                                    void* out, int32_t keep_logits, int32_t max_len_hint, void* stream) {
+  return quant_attention_part(ctx, q, full, active, out, max_len_hint, keep_logits != 0, true,
+                              static_cast<cudaStream_t>(stream));
+}
+
+rkv_status rkv_quant_full_step(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full, const int32_t* k_small,
+                               int32_t k_max, const int32_t* active, void* out, float* scores, int64_t score_stride,
+                               int32_t* topk_idx, void* q_last_full, int32_t max_len_hint, void* stream) {
+  // everything the second half would reject is rejected before the first half launches
+  if (!ctx || !q || !quant_ok(full) || !k_small || !out || !topk_idx) return RKV_ERR_INVALID_ARG;
+  if (k_max < 1 || k_max > ctx->cfg.max_small) return RKV_ERR_INVALID_ARG;
+  const int n_max = max_len_hint == 0 ? ctx->cfg.max_len : max_len_hint;
+  if (n_max < 1 || n_max > ctx->cfg.max_len) return RKV_ERR_INVALID_ARG;
+  if (scores != nullptr && score_stride < n_max) return RKV_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  rkv_status s = quant_attention_part(ctx, q, full, active, out, max_len_hint, true, false, st);
+  if (s != RKV_OK) return s;
+  const rkv_cache sizes = sizes_of(full);
+  return select_part(ctx, q, &sizes, k_small, k_max, active, out, scores, score_stride, topk_idx, q_last_full, st);
+}
+
+rkv_status rkv_quant_score_keys(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full, const int32_t* k_small,
+                                int32_t k_max, const int32_t* active, float* scores, int64_t score_stride,
+                                void* q_last_full, void* stream) {
+  if (!ctx || !quant_ok(full) || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+  const rkv_cache sizes = sizes_of(full);
+  return rkv_score_keys(ctx, q, &sizes, k_small, k_max, active, scores, score_stride, q_last_full, stream);
+}
+
+rkv_status rkv_quant_select_topk(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full, const int32_t* k_small,
+                                 int32_t k_max, const int32_t* active, float* scores, int64_t score_stride,
+                                 int32_t* topk_idx, void* q_last_full, void* stream) {
+  if (!ctx || !quant_ok(full) || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+  const rkv_cache sizes = sizes_of(full);
+  return rkv_select_topk(ctx, q, &sizes, k_small, k_max, active, scores, score_stride, topk_idx, q_last_full, stream);
+}
+
+rkv_status rkv_quant_store(rkv_ctx* ctx, const void* k_new, int64_t k_seq_stride, int64_t k_tok_stride,
+                           const void* v_new, int64_t v_seq_stride, int64_t v_tok_stride, int32_t n_tok,
+                           const int32_t* start, const int32_t* count, const rkv_quant_cache* full, void* stream) {
+  if (!ctx || !k_new || !v_new || !quant_ok(full) || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || ((k_seq_stride | k_tok_stride | v_seq_stride | v_tok_stride) & 7) != 0)
+    return RKV_ERR_INVALID_ARG;   // the kernel reads 16 bytes at a time
+  if (n_tok < 1 || n_tok > full->n_rows) return RKV_ERR_INVALID_ARG;
+  const rkv::QuantNew rows = {k_new, v_new, k_seq_stride, k_tok_stride, v_seq_stride, v_tok_stride, n_tok};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_APPEND);
+    e = rkv::launch_quant_store(rows, start, count, dev_of(full), ctx->cfg.n_seq, ctx->cfg.n_kv_heads,
+                                ctx->len_tickets, ctx->status, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit store launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  return RKV_OK;
+}
+
+rkv_status rkv_quant_gather_small(rkv_ctx* ctx, const int32_t* topk_idx, const int32_t* k_small, int32_t k_max,
+                                  const rkv_quant_cache* full, const rkv_cache* small_cache, const int32_t* active,
+                                  void* stream) {
+  if (!ctx || !topk_idx || !k_small || !quant_ok(full) || !cache_ok(small_cache) || !on_device(ctx))
+    return RKV_ERR_INVALID_ARG;
+  if (k_max < 1 || k_max > ctx->cfg.max_small) return RKV_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_GATHER);
+    e = rkv::launch_quant_gather(topk_idx, k_small, k_max, dev_of(full), dev_of(small_cache), active, ctx->cfg.n_seq,
+                                 ctx->cfg.n_kv_heads, ctx->status, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit gather launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, small_cache, nullptr);
+  return RKV_OK;
 }
 
 rkv_status rkv_full_step(rkv_ctx* ctx, const void* q, const rkv_cache* full, const int32_t* k_small, int32_t k_max,

@@ -26,6 +26,8 @@ constexpr int kScoreThreads = 256;
 constexpr int kSelectMaxKeysPerCta = 40960;   // max_len <= kSelectCluster * this
 constexpr int kSelectBins = 4096;      // bins of the per-(sequence, KV head) score histogram in the workspace
 constexpr int kSelectMaxSlice = 8192;  // most positions one CTA of the score pass takes
+constexpr int kQuantBlock = 64;        // positions that share a scale in the 8-bit cache
+constexpr int kQuantTile = 128;        // positions per pipeline stage of the pass over the 8-bit cache
 
 struct PartialLayout {                 // split-K partial of one (b, g, split)
   // o: [8 heads][128] fp32 unnormalised, then m[8], l[8]
@@ -119,6 +121,40 @@ struct CacheDev {
   void* k; void* v;
   const int64_t* row_offset; const int32_t* cap; int32_t* len;
 };
+
+// The 8-bit cache as the kernels see it, and new rows for it (strides in elements).
+struct QuantDev {
+  uint8_t* k; uint8_t* v; float* k_scale; float* v_scale;
+  const int64_t* row_offset; const int32_t* cap; int32_t* len;
+  int64_t n_rows;
+};
+struct QuantNew {
+  const void* k; const void* v;
+  int64_t k_seq, k_tok, v_seq, v_tok;
+  int32_t n_tok;
+};
+
+struct QuantAttnParams {
+  const void* q;              // bf16 [B][Hq][128]
+  const float* k_scale; const float* v_scale;   // [n_rows / 64]
+  const int64_t* row_offset; const int32_t* cap; const int32_t* len; const int32_t* active;
+  void* out;                  // bf16 [B][Hq][128]: written here for empty sequences only
+  float* partials; float* ml_t; float* logits;  // as in AttnParams
+  int32_t* status;
+  int64_t n_rows, logit_stride;
+  int32_t n_q_heads, n_kv_heads, group, gp, max_splits, max_len;
+  int32_t spec;               // 1: first tiles may be requested before the length is read (one sequence, no mask)
+  float scale;
+};
+
+cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                                   int n_seq, int grid_x, cudaStream_t st);
+cudaError_t launch_quant_store(const QuantNew& rows, const int32_t* start, const int32_t* count, const QuantDev& c,
+                               int n_seq, int n_kv_heads, int32_t* tickets, int32_t* status, cudaStream_t st);
+cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small, int k_max, const QuantDev& full,
+                                const CacheDev& small_cache, const int32_t* active, int n_seq, int n_kv_heads,
+                                int32_t* status, cudaStream_t st);
+cudaError_t prepare_quant_attention();
 
 cudaError_t launch_attention(const AttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                              int n_seq, int grid_x, bool write_logits, cudaStream_t st, bool append = false);
@@ -217,6 +253,16 @@ inline CUresult encode_cache_map(EncodeTiledFn encode, void* base, int64_t n_row
   return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+// One 8-bit cache buffer ([n_rows][128] codes): a box is 128 rows, landing with the 128-byte swizzle.
+inline CUresult encode_quant_map(EncodeTiledFn encode, void* base, int64_t n_rows, CUtensorMap* out) {
+  const cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)n_rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)kHeadDim};
+  const cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)kQuantTile};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 }  // namespace rkv

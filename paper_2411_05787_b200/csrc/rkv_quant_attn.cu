@@ -1,0 +1,462 @@
+// Split-K grouped-query decode attention over the 8-bit cache (sm_100a).
+//
+//   s[h][j] = scale ks(j) <q[h], K8[j]>,  p = softmax_j s,  out[h] = sum_j p[h][j] vs(j) V8[j],
+// K8, V8 e4m3 codes, ks, vs the scales of position j's block of 64.  The split partials, the softmax statistics and
+// the raw logits go to the same workspace, in the same layout, as those of the bf16 pass: the fold kernel, the score
+// pass and the selection behind it are the same kernels.
+//
+// What bounds it: 256 bytes per position and KV head from HBM, half of the bf16 pass.  The shape is that pass's: one
+// CTA per (sequence, KV head, split), two to an SM, a copy warp that keeps a ring of three 32 KB stages full (one
+// tensor-map copy of 128 positions for K and one for V per stage: a copy instruction costs its warp about 100 cycles,
+// so tiles are as many bytes as there), four MMA warps with 32 positions of a tile each, i.e. half a block, so that a
+// scale is one number per warp and tile.
+//
+// Arithmetic.  Codes become halves exactly (cvt.e4m3x2) and the products run as m16n8k16 f16 MMAs with fp32
+// accumulators; the heads of the group are the N = 8 dimension.  fp8 MMAs would want q and p as e4m3, which is not
+// enough for either.  The queries are scaled by a power of two per head so that the largest element is near 2^15 and
+// every bf16 query element down to 2^-28 of it is exact as a half.  The probabilities meet V as halves
+//   p' = p vs / vref 2^13,   vref = the smallest power of two >= every vs this warp has seen,
+// so that they are normal halves (relative rounding 2^-11) down to p vs / vref = 2^-27 and never above 2^13; the
+// accumulators are rescaled when vref rises and carry vref 2^-13 until they are published.
+// K codes are read with ldmatrix as they lie: a lane holds four consecutive channels of a row, and the order of the
+// channels in the k dimension is free as long as the query fragments use the same.  For V^T the transposed ldmatrix
+// moves pairs of channels; one byte permutation turns (two positions x two channels) into the two halves the A
+// fragment wants, channel 2r in row r and channel 2r + 1 in row r + 8 of the fragment.
+#include <float.h>
+
+#include "rkv_ptx.cuh"
+#include "rkv_quant.cuh"
+
+namespace rkv {
+namespace {
+
+constexpr int kQStages = 3;
+constexpr int kQHalfBytes = kQuantTile * kHeadDim;   // codes of K (or V) of one tile
+constexpr int kQStageBytes = 2 * kQHalfBytes;
+constexpr int kQWarps = 4;                           // MMA warps; warp kQWarps is the copy warp
+constexpr int kQThreads = 32 * (kQWarps + 1);
+constexpr int kQBand = kQuantTile / kQWarps;         // positions of a tile per warp
+constexpr int kQBlocks = kQBand / 16;                // 16-row MMA blocks per band
+constexpr int kQRow = 144;                           // halves per query row in shared memory (fragment reads spread over the banks)
+constexpr int kQOPad = 132;                          // floats per head row in the merge buffer
+constexpr float kPBase = 8192.f;                     // 2^13: the largest p'
+static_assert(kQuantBlock % kQBand == 0, "a warp's band must not straddle two blocks");
+
+constexpr int kBarsAt = kQStages * kQStageBytes;
+constexpr int kQAt = kBarsAt + 64;
+constexpr int kQsAt = kQAt + kMaxGroup * kQRow * 2;
+constexpr int kWmAt = kQsAt + kMaxGroup * 4;
+constexpr int kQSmem = kWmAt + kQWarps * kMaxGroup * 4 + 1024;   // + alignment of the stages
+
+__device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* tm, int row, uint32_t bar,
+                                               uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
+      "l"(tm), "r"(0), "r"(row), "r"(bar), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <bool kLogits>
+__global__ void __launch_bounds__(kQThreads, 2)
+quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                  const QuantAttnParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const int b = blockIdx.z, g = blockIdx.y, split = blockIdx.x, n_cta = gridDim.x;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+  const uint32_t bar_full = smem_base + kBarsAt, bar_empty = bar_full + 8 * kQStages;
+  if (tid == 0) {
+    for (int s = 0; s < kQStages; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, kQWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid == 32 * kQWarps) {
+    prefetch_tensormap(&tm_k);
+    prefetch_tensormap(&tm_v);
+  }
+  const int G = p.group;
+  const int64_t head0 = ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim;
+  const int qd = lane >> 2, qc = (lane & 3) * 2;   // row of an 8-row group; first of the two heads this lane holds
+  // geometry: never written by a kernel, read above the dependency wait
+  const int cap = __ldg(p.cap + b);
+  const int64_t roff = __ldg(p.row_offset + b);
+  const bool layout_ok = quant_layout_ok(roff, cap, p.n_kv_heads, p.n_rows);
+  const int64_t row0 = roff + (int64_t)g * cap;
+  __syncthreads();
+
+  // The tiles of a (sequence, KV head) are dealt out to its CTAs in turn.
+  auto tile_pos = [&](int t) { return (split + t * n_cta) * kQuantTile; };
+  auto issue_tile = [&](int t, uint64_t policy) {
+    const int s = t % kQStages;
+    const uint32_t dst = smem_base + s * kQStageBytes, bar = bar_full + 8 * s;
+    const int row = (int)(row0 + tile_pos(t));
+    mbar_expect_tx(bar, kQStageBytes);
+    tma_load_codes(dst, &tm_k, row, bar, policy);
+    tma_load_codes(dst + kQHalfBytes, &tm_v, row, bar, policy);
+  };
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  pdl_wait();
+  pdl_launch();   // after the wait: at most one predecessor is ever in flight behind a kernel of this library
+  // One sequence and no mask: the first tiles are requested before the length has been read, as far as the host's
+  // bound says that there are any (rows past the buffer's end arrive as zeros; tiles past the length are ignored).
+  int n_spec = 0;
+  if (p.spec != 0 && layout_ok) {
+    const int room = cap < p.max_len ? cap : p.max_len;
+    const int bound = (room + kQuantTile - 1) / kQuantTile;
+    n_spec = bound > split ? (bound - split + n_cta - 1) / n_cta : 0;
+    if (n_spec > kQStages) n_spec = kQStages;
+    if (tid == 32 * kQWarps)
+      for (int t = 0; t < n_spec; ++t) issue_tile(t, policy);
+  }
+
+  // sizes, queries and the first scales: independent loads, one round trip
+  const int act = (p.active != nullptr) ? __ldcg(p.active + b) : 1;
+  int n = __ldcg(p.len + b);
+  // Lane i holds the two scales of the warp's half block in the CTA's tile  t0 + i  for 32 tiles at a time.
+  const int band0 = kQBand * warp;
+  float ks_all = 0.f, vs_all = 0.f;
+  auto load_scales = [&](int t0) {
+    const int64_t pos = (int64_t)(split + (int64_t)(t0 + lane) * n_cta) * kQuantTile + band0;
+    ks_all = vs_all = 0.f;
+    if (layout_ok && pos < cap) {
+      ks_all = __ldcg(p.k_scale + (row0 + pos) / kQuantBlock);
+      vs_all = __ldcg(p.v_scale + (row0 + pos) / kQuantBlock);
+    }
+  };
+  __half* sm_q = reinterpret_cast<__half*>(smem + kQAt);
+  float* sm_qs = reinterpret_cast<float*>(smem + kQsAt);
+  float* sm_wm = reinterpret_cast<float*>(smem + kWmAt);
+  uint32_t qb[8][2];              // B fragments of Q^T: [16-channel segment][k half]
+  float qs0 = 0.f, qs1 = 0.f;     // softmax scale over the queries' powers of two, for heads qc and qc + 1
+  if (warp < kQWarps) {
+    uint4 qv = make_uint4(0u, 0u, 0u, 0u);
+    const int h = tid >> 4;       // 16 lanes to a head's row
+    if (h < G) qv = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + head0) + tid);
+    load_scales(0);
+    uint32_t m = __vmaxu2(__vmaxu2(qv.x & 0x7fff7fffu, qv.y & 0x7fff7fffu), __vmaxu2(qv.z & 0x7fff7fffu, qv.w & 0x7fff7fffu));
+    m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    // 2^e brings the largest magnitude into [2^14, 2^15); nothing is done for a row that is not finite or zero
+    int e = 14 - ((int)(m >> 7) - 127);
+    if (m >= 0x7f80u || m == 0u) e = 0;
+    if (e > 126) e = 126;
+    const float up = pow2f(e);
+    const uint32_t x[4] = {qv.x, qv.y, qv.z, qv.w};
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = pack_f16(__uint_as_float(x[i] << 16) * up, __uint_as_float(x[i] & 0xffff0000u) * up);
+    *reinterpret_cast<uint4*>(sm_q + h * kQRow + (tid & 15) * 8) = make_uint4(y[0], y[1], y[2], y[3]);
+    if ((tid & 15) == 0) sm_qs[h] = p.scale * pow2f(-e);
+    consumer_bar_n<32 * kQWarps>();
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {   // channels 16 s + 4 t .. + 3 of head qd, t = lane & 3
+      const uint2 f = *reinterpret_cast<const uint2*>(sm_q + qd * kQRow + 16 * s + 4 * (lane & 3));
+      qb[s][0] = f.x;
+      qb[s][1] = f.y;
+    }
+    qs0 = sm_qs[qc];
+    qs1 = sm_qs[qc + 1];
+  }
+
+  auto drain_spec = [&] {   // tiles requested ahead of the length must land before the CTA may go
+    if (n_spec > 0) {
+      if (tid == 0)
+        for (int t = 0; t < n_spec; ++t)
+          if (!mbar_wait(bar_full + 8 * t, 0)) atomicOr(p.status, RKV_DEV_TIMEOUT);
+      __syncthreads();
+    }
+  };
+  if (act == 0) return;   // (with a mask nothing is requested ahead)
+  const int64_t bg = (int64_t)b * p.n_kv_heads + g;
+  float* part = p.partials + (bg * p.max_splits + split) * PartialLayout::kFloats;
+  float* ml = p.ml_t + bg * 16 * p.max_splits + split;   // split-contiguous copy of (m, l), for the kernels that read across the splits
+  if (!layout_ok) {   // nothing is read; the kernels behind fold this to zero (they know the length, not the layout)
+    if (tid == 0 && split == 0) atomicOr(p.status, RKV_DEV_BAD_LAYOUT);
+    for (int i = tid; i < G * kHeadDim; i += kQThreads) part[i] = 0.f;
+    if (tid < kMaxGroup) {
+      part[kMaxGroup * kHeadDim + tid] = ml[(int64_t)tid * p.max_splits] = 0.f;
+      part[kMaxGroup * kHeadDim + kMaxGroup + tid] = ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = 1.f;
+    }
+    n = 0;
+  }
+  {
+    const int lim = cap < p.max_len ? cap : p.max_len;
+    if (n > lim) {
+      n = lim;
+      if (tid == 0 && split == 0) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
+    }
+  }
+  if (n <= 0) {   // nothing cached: the output is defined as zero
+    drain_spec();
+    if (split == 0 && tid < kHeadDim)
+      for (int h = 0; h < G; ++h) static_cast<__nv_bfloat16*>(p.out)[head0 + h * kHeadDim + tid] = __float2bfloat16(0.f);
+    return;
+  }
+  const int total_tiles = (n + kQuantTile - 1) / kQuantTile;
+  const int n_tiles = total_tiles > split ? (total_tiles - split + n_cta - 1) / n_cta : 0;
+  if (n_tiles == 0) {
+    drain_spec();
+    return;
+  }
+
+  if (warp == kQWarps) {
+    // ------------------------------------------------------------ copy warp
+    if (lane == 0) {
+      for (int t = n_spec; t < n_tiles; ++t) {
+        const int s = t % kQStages, use = t / kQStages;
+        if (use > 0 && !mbar_wait(bar_empty + 8 * s, (use - 1) & 1)) {
+          atomicOr(p.status, RKV_DEV_TIMEOUT);
+          break;
+        }
+        issue_tile(t, policy);
+      }
+    }
+    return;
+  }
+
+  // ---------------------------------------------------------------- MMA warps
+  const float ninf = -INFINITY;
+  float m0 = ninf, m1 = ninf, l0 = 0.f, l1 = 0.f;
+  float vref = 1.17549435e-38f, vrcp = 8.50705917e37f;   // 2^-126 and its reciprocal
+  float o[8][4];   // [16-channel segment]: (channel 16 s + 2 qd, heads qc, qc + 1), (the next channel, the same heads)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  float* lg0 = nullptr;   // logit scratch, position-major: [position][gp] floats
+  uint64_t keep_policy = 0;
+  if (kLogits) {
+    lg0 = p.logits + bg * p.logit_stride * p.gp + qc;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep_policy));
+  }
+  const bool lg_on = kLogits && qc < p.gp;
+
+  const int n_wait = n_tiles > n_spec ? n_tiles : n_spec;   // tiles requested ahead of the length are always consumed
+  for (int t = 0; t < n_wait; ++t) {
+    const int s = t % kQStages;
+    if (t > 0 && (t & 31) == 0) load_scales(t);
+    const float ks = __shfl_sync(0xffffffffu, ks_all, t & 31), vs = __shfl_sync(0xffffffffu, vs_all, t & 31);
+    if (!mbar_wait(bar_full + 8 * s, (t / kQStages) & 1)) {
+      if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+      break;
+    }
+    const int pos_base = tile_pos(t) + band0;
+    if (t < n_tiles && pos_base < n) {
+      const uint32_t kbase = smem_base + s * kQStageBytes;
+      float c[kQBlocks][4], c2[kQBlocks][4];   // two accumulator chains per block
+#pragma unroll
+      for (int i = 0; i < kQBlocks; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[i][j] = c2[i][j] = 0.f;
+#pragma unroll
+      for (int cs = 0; cs < 4; ++cs) {   // 32 channels
+#pragma unroll
+        for (int i = 0; i < kQBlocks; ++i) {
+          const int krow = band0 + 16 * i + (lane & 15), piece = 2 * cs + (lane >> 4);
+          uint32_t a[4];
+          ldsm_x4(a, kbase + krow * kHeadDim + ((piece ^ (krow & 7)) << 4));
+          mma_f16(c[i], codes_lo_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[0]), codes_hi_f16x2(a[1]),
+                  qb[2 * cs][0], qb[2 * cs][1]);
+          mma_f16(c2[i], codes_lo_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[2]), codes_hi_f16x2(a[3]),
+                  qb[2 * cs + 1][0], qb[2 * cs + 1][1]);
+        }
+      }
+      // one factor per head and tile; kept finite, so that a zero product stays zero (NaN scales pass)
+      float f0 = ks * qs0, f1 = ks * qs1;
+      f0 = f0 > FLT_MAX ? FLT_MAX : f0;
+      f1 = f1 > FLT_MAX ? FLT_MAX : f1;
+      float sc[kQBlocks][4];
+      float t0 = ninf, t1 = ninf;
+#pragma unroll
+      for (int i = 0; i < kQBlocks; ++i) {
+        const int r0 = pos_base + 16 * i + qd, r1 = r0 + 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sc[i][j] = (c[i][j] + c2[i][j]) * ((j & 1) ? f1 : f0);
+        if (kLogits) {
+          if (lg_on) {
+            if (r0 < n) st_keep_f2(lg0 + (int64_t)r0 * p.gp, sc[i][0], sc[i][1], keep_policy);
+            if (r1 < n) st_keep_f2(lg0 + (int64_t)r1 * p.gp, sc[i][2], sc[i][3], keep_policy);
+          }
+        }
+        if (r0 >= n) sc[i][0] = sc[i][1] = ninf;
+        if (r1 >= n) sc[i][2] = sc[i][3] = ninf;
+        t0 = fmaxf(t0, fmaxf(sc[i][0], sc[i][2]));
+        t1 = fmaxf(t1, fmaxf(sc[i][1], sc[i][3]));
+      }
+#pragma unroll
+      for (int sh = 4; sh <= 16; sh <<= 1) {
+        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, sh));
+        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, sh));
+      }
+      const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+      if (__any_sync(0xffffffffu, (n0 > m0) || (n1 > m1))) {
+        const float a0 = (n0 == m0) ? 1.f : ex2((m0 - n0) * kLog2e);
+        const float a1 = (n1 == m1) ? 1.f : ex2((m1 - n1) * kLog2e);
+        l0 *= a0;
+        l1 *= a1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          o[i][0] *= a0;
+          o[i][1] *= a1;
+          o[i][2] *= a0;
+          o[i][3] *= a1;
+        }
+        m0 = n0;
+        m1 = n1;
+      }
+      if (vs > vref) {   // the same for the whole warp
+        uint32_t up = (__float_as_uint(vs) + 0x7fffffu) & 0x7f800000u;   // the next power of two, 2^126 at most
+        if (up > 0x7e800000u) up = 0x7e800000u;
+        const float a = vref * __uint_as_float(0x7f000000u - up);
+        vref = __uint_as_float(up);
+        vrcp = __uint_as_float(0x7f000000u - up);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][j] *= a;
+      }
+      const float vf = vs * vrcp * kPBase;
+      const float nm0 = (m0 == ninf) ? 0.f : -m0 * kLog2e;
+      const float nm1 = (m1 == ninf) ? 0.f : -m1 * kLog2e;
+      const uint32_t vbase = kbase + kQHalfBytes;
+#pragma unroll
+      for (int i = 0; i < kQBlocks; ++i) {
+        const int pos_i = pos_base + 16 * i;
+        if (pos_i >= n) continue;   // the whole block lies past the end
+        const float p0 = ex2(fmaf(sc[i][0], kLog2e, nm0)), p1 = ex2(fmaf(sc[i][1], kLog2e, nm1));
+        const float p2 = ex2(fmaf(sc[i][2], kLog2e, nm0)), p3 = ex2(fmaf(sc[i][3], kLog2e, nm1));
+        l0 += p0 + p2;
+        l1 += p1 + p3;
+        // P^T as the B operand: the two 8x8 [position][head] blocks transposed inside the warp
+        const uint32_t b0 = movmatrix_t(pack_f16(p0 * vf, p1 * vf)), b1 = movmatrix_t(pack_f16(p2 * vf, p3 * vf));
+        const bool tail = pos_i + 16 > n;
+        // rows past the end may hold anything (even NaN): their codes are cleared so that 0 * x stays 0.  A register
+        // holds positions 2 t, 2 t + 1 (t = lane & 3) of the first or of the second eight.
+        uint32_t mk0 = 0xffffffffu, mk1 = 0xffffffffu;
+        if (tail) {
+          const int pa = pos_i + qc;
+          mk0 = (pa < n ? 0x0000ffffu : 0u) | (pa + 1 < n ? 0xffff0000u : 0u);
+          mk1 = (pa + 8 < n ? 0x0000ffffu : 0u) | (pa + 9 < n ? 0xffff0000u : 0u);
+        }
+        const int vrow = band0 + 16 * i + (lane & 15);
+#pragma unroll
+        for (int sp = 0; sp < 4; ++sp) {   // two 16-channel segments
+          const int piece = 2 * sp + (lane >> 4);
+          uint32_t a[4];
+          ldsm_x4_t(a, vbase + vrow * kHeadDim + ((piece ^ (vrow & 7)) << 4));
+          if (tail) {
+            a[0] &= mk0;
+            a[1] &= mk1;
+            a[2] &= mk0;
+            a[3] &= mk1;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[j] = __byte_perm(a[j], 0u, 0x3120);   // (channel, two positions) in each half
+          mma_f16(o[2 * sp], codes_lo_f16x2(a[0]), codes_hi_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[1]), b0, b1);
+          mma_f16(o[2 * sp + 1], codes_lo_f16x2(a[2]), codes_hi_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[3]), b0, b1);
+        }
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_empty + 8 * s);
+  }
+
+#pragma unroll
+  for (int sh = 4; sh <= 16; sh <<= 1) {
+    l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
+  }
+
+  // ------------------------------------------------ merge the MMA warps: accumulators scaled to the CTA-wide maximum
+  if (lane < 4) *reinterpret_cast<float2*>(sm_wm + warp * kMaxGroup + qc) = make_float2(m0, m1);
+  consumer_bar_n<32 * kQWarps>();   // every warp's maxima are visible, and the stage memory is free
+  float* sm_o = reinterpret_cast<float*>(smem);              // [warps][8][kQOPad]
+  float* sm_l = sm_o + kQWarps * kMaxGroup * kQOPad;         // [warps][8]
+  float* sm_M = sm_l + kQWarps * kMaxGroup;                  // [8]
+  {
+    float M0 = ninf, M1 = ninf;
+#pragma unroll
+    for (int w = 0; w < kQWarps; ++w) {
+      const float2 mw = *reinterpret_cast<const float2*>(sm_wm + w * kMaxGroup + qc);
+      M0 = fmaxf(M0, mw.x);
+      M1 = fmaxf(M1, mw.y);
+    }
+    const float e0 = (m0 == ninf) ? 0.f : ex2((m0 - M0) * kLog2e);
+    const float e1 = (m1 == ninf) ? 0.f : ex2((m1 - M1) * kLog2e);
+    const float unit = vref * (1.f / kPBase);
+    float* base = sm_o + (warp * kMaxGroup + qc) * kQOPad + 2 * qd;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      *reinterpret_cast<float2*>(base + 16 * s) = make_float2(o[s][0] * e0 * unit, o[s][2] * e0 * unit);
+      *reinterpret_cast<float2*>(base + kQOPad + 16 * s) = make_float2(o[s][1] * e1 * unit, o[s][3] * e1 * unit);
+    }
+    if (lane < 4) {
+      sm_l[warp * kMaxGroup + qc] = l0 * e0;
+      sm_l[warp * kMaxGroup + qc + 1] = l1 * e1;
+      if (warp == 0) {
+        sm_M[qc] = M0;
+        sm_M[qc + 1] = M1;
+      }
+    }
+  }
+  consumer_bar_n<32 * kQWarps>();
+  for (int item = tid; item < G * 32; item += 32 * kQWarps) {   // (head, four channels)
+    const float* src = sm_o + (item >> 5) * kQOPad + (item & 31) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kQWarps; ++w) {
+      const float4 v = *reinterpret_cast<const float4*>(src + w * kMaxGroup * kQOPad);
+      acc.x += v.x;
+      acc.y += v.y;
+      acc.z += v.z;
+      acc.w += v.w;
+    }
+    *reinterpret_cast<float4*>(part + (item >> 5) * kHeadDim + (item & 31) * 4) = acc;
+  }
+  if (tid < kMaxGroup) {
+    float M = ninf, L = 0.f;
+    if (tid < G) {
+      M = sm_M[tid];
+#pragma unroll
+      for (int w = 0; w < kQWarps; ++w) L += sm_l[w * kMaxGroup + tid];
+    }
+    part[kMaxGroup * kHeadDim + tid] = M;
+    part[kMaxGroup * kHeadDim + kMaxGroup + tid] = L;
+    ml[(int64_t)tid * p.max_splits] = M;
+    ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = L;
+  }
+}
+
+}  // namespace
+
+cudaError_t prepare_quant_attention() {
+  cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmem);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(quant_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmem);
+  return e;
+}
+
+cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                                   int n_seq, int grid_x, cudaStream_t st) {
+  dim3 grid(grid_x, p.n_kv_heads, n_seq);
+  if (p.logits != nullptr)
+    return launch_ex(quant_attn_kernel<true>, grid, dim3(kQThreads), (size_t)kQSmem, st, 1, tm_k, tm_v, p);
+  return launch_ex(quant_attn_kernel<false>, grid, dim3(kQThreads), (size_t)kQSmem, st, 1, tm_k, tm_v, p);
+}
+
+}  // namespace rkv

@@ -17,13 +17,17 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librkv.so"
 RKV_OK = 0
 AGG_MAX, AGG_MEAN, AGG_FIRST = 0, 1, 2
 DEV_APPEND_OVERFLOW, DEV_LEN_CLAMPED, DEV_NONFINITE, DEV_BAD_INDEX, DEV_TIMEOUT = 1, 2, 4, 8, 16
+DEV_BAD_LAYOUT = 32
 
 EXPORTS = ["rkv_create", "rkv_destroy", "rkv_workspace_bytes", "rkv_full_step", "rkv_gather_small",
            "rkv_small_step", "rkv_append", "rkv_should_refresh", "rkv_get_device_status",
            "rkv_status_string", "rkv_last_cuda_error", "rkv_launch_count", "rkv_set_profiling", "rkv_get_profile",
            "rkv_set_option", "rkv_small_step_noalloc", "rkv_append_small_step", "rkv_score_step",
            "rkv_gather_small_evict", "rkv_append_small_step_evict", "rkv_full_attention", "rkv_select_topk",
-           "rkv_append_full_attention", "rkv_get_option", "rkv_score_keys"]
+           "rkv_append_full_attention", "rkv_get_option", "rkv_score_keys", "rkv_quant_store",
+           "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk", "rkv_quant_full_step",
+           "rkv_quant_gather_small"]
+QUANT_BLOCK = 64
 NOALLOC_MAX_PROBLEMS, NOALLOC_MAX_LEN = 32, 65536
 OPT_SMALL_MIN_CHUNK, OPT_DEPENDENT_LAUNCH, OPT_SMALL_CLUSTER, OPT_EARLY_CACHE_READ, OPT_INTERLEAVE_TILES = 1, 2, 3, 4, 5
 OPT_SELECT_KEYS_PER_CTA = 6
@@ -40,6 +44,12 @@ class RkvConfig(ctypes.Structure):
 class RkvCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_rows", ctypes.c_int64),
                 ("row_offset", ctypes.c_void_p), ("cap", ctypes.c_void_p), ("len", ctypes.c_void_p)]
+
+
+class RkvQuantCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_rows", ctypes.c_int64), ("row_offset", ctypes.c_void_p), ("cap", ctypes.c_void_p),
+                ("len", ctypes.c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -91,6 +101,16 @@ def _load() -> ctypes.CDLL:
     lib.rkv_get_profile.restype = i32
     lib.rkv_small_step_noalloc.argtypes = [cfgp, vp, cachep, vp, vp, i32, vp, vp, ctypes.c_char_p, ctypes.c_size_t]
     lib.rkv_small_step_noalloc.restype = i32
+    quantp = ctypes.POINTER(RkvQuantCache)
+    lib.rkv_quant_store.argtypes = [vp, vp, i64, i64, vp, i64, i64, i32, vp, vp, quantp, vp]
+    lib.rkv_quant_full_attention.argtypes = [vp, vp, quantp, vp, vp, i32, i32, vp]
+    lib.rkv_quant_score_keys.argtypes = [vp, vp, quantp, vp, i32, vp, vp, i64, vp, vp]
+    lib.rkv_quant_select_topk.argtypes = [vp, vp, quantp, vp, i32, vp, vp, i64, vp, vp, vp]
+    lib.rkv_quant_full_step.argtypes = [vp, vp, quantp, vp, i32, vp, vp, vp, i64, vp, vp, i32, vp]
+    lib.rkv_quant_gather_small.argtypes = [vp, vp, vp, i32, quantp, cachep, vp, vp]
+    for name in ("rkv_quant_store", "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk",
+                 "rkv_quant_full_step", "rkv_quant_gather_small"):
+        getattr(lib, name).restype = i32
     for name in ("rkv_create", "rkv_destroy", "rkv_full_step", "rkv_gather_small", "rkv_small_step",
                  "rkv_append", "rkv_should_refresh", "rkv_get_device_status"):
         getattr(lib, name).restype = i32
@@ -130,6 +150,32 @@ def cache_struct(k, v, row_offset, cap, length) -> RkvCache:
     return RkvCache(_ptr(k), _ptr(v), k.numel() // 128, _ptr(row_offset), _ptr(cap), _ptr(length))
 
 
+def quant_cache_struct(k8, v8, k_scale, v_scale, row_offset, cap, length) -> RkvQuantCache:
+    """Describe a packed 8-bit K/V cache (see include/rkv.h).  The caller keeps the tensors alive.
+
+    k8, v8: float8_e4m3fn (or uint8 codes) [n_rows, 128], n_rows a multiple of 64; scales: float32 [n_rows / 64];
+    row_offset and cap hold multiples of 64 (checked on the device: DEV_BAD_LAYOUT)."""
+    for t in (k8, v8):
+        if t.dtype not in (torch.float8_e4m3fn, torch.uint8) or t.dim() != 2 or t.shape[1] != 128:
+            raise ValueError("k8 and v8 are float8_e4m3fn or uint8 tensors [n_rows, 128]")
+    n_rows = k8.shape[0]
+    if v8.shape[0] != n_rows or n_rows == 0 or n_rows % QUANT_BLOCK != 0:
+        raise ValueError("k8 and v8 have the same number of rows, a multiple of 64")
+    for t in (k_scale, v_scale):
+        if t.dtype != torch.float32 or t.numel() != n_rows // QUANT_BLOCK:
+            raise ValueError("scales are float32 tensors with one element per 64 rows")
+    if row_offset.dtype != torch.int64 or cap.dtype != torch.int32 or length.dtype != torch.int32:
+        raise ValueError("row_offset is int64, cap and length are int32")
+    c = RkvQuantCache(_ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), n_rows, _ptr(row_offset), _ptr(cap), _ptr(length))
+    c.device = k8.device.index
+    if any(t.device != k8.device for t in (v8, k_scale, v_scale, row_offset, cap, length)):
+        raise ValueError("the tensors of a cache are on one device")
+    if not row_offset.numel() == cap.numel() == length.numel():
+        raise ValueError("row_offset, cap and length have one element per sequence")
+    c.n_seq = cap.numel()
+    return c
+
+
 def small_step_noalloc(cfg: RkvConfig, q, small: RkvCache, out, active=None, max_len_hint=0, device_status=None,
                        stream=None):
     """Partial step for callers that may not allocate device memory (no context; see include/rkv.h).
@@ -154,6 +200,7 @@ class Context:
         if rc != RKV_OK:
             raise RkvError(rc)
         self._h = handle
+        self.device = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "_h", None):
@@ -200,15 +247,26 @@ class Context:
         self._check(lib.rkv_append_full_attention(self._h, _ptr(q), _ptr(k_new), _ptr(v_new), ctypes.byref(full),
                                                   _ptr(active), _ptr(out), max_len_hint, _stream(stream)))
 
-    def select_topk(self, q, full: RkvCache, k_small, k_max, topk_idx, active=None, scores=None, q_last_full=None,
-                    stream=None):
+    def select_topk(self, q, full: RkvCache | RkvQuantCache, k_small, k_max, topk_idx, active=None, scores=None,
+                    q_last_full=None, stream=None):
         stride = scores.shape[-1] if scores is not None else 0
+        if isinstance(full, RkvQuantCache):
+            self._on_device(full, q, k_small, topk_idx, active, scores, q_last_full)
+            self._quant(lib.rkv_quant_select_topk, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max,
+                        _ptr(active), _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full))
+            return
         self._check(lib.rkv_select_topk(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                                         _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full), _stream(stream)))
 
-    def score_keys(self, q, full: RkvCache, k_small, k_max, active=None, scores=None, q_last_full=None, stream=None):
+    def score_keys(self, q, full: RkvCache | RkvQuantCache, k_small, k_max, active=None, scores=None, q_last_full=None,
+                   stream=None):
         """The score pass alone; the next select_topk (scores=None, q_last_full=None) launches the selection alone."""
         stride = scores.shape[-1] if scores is not None else 0
+        if isinstance(full, RkvQuantCache):
+            self._on_device(full, q, k_small, active, scores, q_last_full)
+            self._quant(lib.rkv_quant_score_keys, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
+                        _ptr(scores), stride, _ptr(q_last_full))
+            return
         self._check(lib.rkv_score_keys(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                                        _ptr(scores), stride, _ptr(q_last_full), _stream(stream)))
 
@@ -244,6 +302,85 @@ class Context:
                                                     ctypes.byref(small), _ptr(k_small), _ptr(active), _ptr(out),
                                                     _ptr(evict_order), _ptr(evict_count), evict_order.shape[-1],
                                                     max_len_hint, _stream(stream)))
+
+    # ------------------------------------------------------------------ the full cache in 8 bits
+    def _on_device(self, cache, *tensors):
+        if cache.device != self.device:
+            raise ValueError("the cache is on another device than the context")
+        if cache.n_seq != self.cfg.n_seq:
+            raise ValueError("the cache holds another number of sequences than the context")
+        for t in tensors:
+            if t is not None and t.device.index != self.device:
+                raise ValueError("a tensor is on another device than the context")
+
+    def _quant(self, fn, stream, *args):
+        """One call on the context's device, whichever is current, and on its current stream unless one is given."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        if torch.cuda.current_device() == self.device:
+            return self._check(fn(self._h, *args, _stream(stream)))
+        with torch.cuda.device(self.device):
+            return self._check(fn(self._h, *args, _stream(stream)))
+
+    def _q_shape(self, *tensors):
+        shape = (self.cfg.n_seq, self.cfg.n_q_heads, 128)
+        for t in tensors:
+            if t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != shape):
+                raise ValueError(f"queries and outputs are bfloat16 tensors {list(shape)}")
+
+    def _per_seq(self, *tensors):
+        for t in tensors:
+            if t is not None and (t.dtype != torch.int32 or t.numel() != self.cfg.n_seq):
+                raise ValueError("per-sequence arguments are int32 tensors with one element per sequence")
+
+    def quant_store(self, k_new, v_new, full: RkvQuantCache, start=None, count=None, stream=None):
+        """Append rows to an 8-bit cache.  k_new, v_new: bfloat16 [B, T, Hkv, 128]; sequences and tokens may be strided
+        (a slice of a projection's output), the heads of a token lie side by side.  start, count: int32 [B] or None."""
+        args = []
+        for x in (k_new, v_new):
+            if (x.dtype != torch.bfloat16 or x.dim() != 4 or x.shape[0] != self.cfg.n_seq or
+                    x.shape[2:] != (self.cfg.n_kv_heads, 128) or x.shape[1] < 1):
+                raise ValueError("k_new and v_new are bfloat16 tensors [B, T, Hkv, 128]")
+            if not x.is_cuda:
+                raise ValueError("librkv takes device tensors")
+            if x.stride(3) != 1 or (x.stride(2) != 128 and self.cfg.n_kv_heads > 1):
+                raise ValueError("the heads of a new row lie side by side")
+            seq = x.stride(0) if x.shape[0] > 1 else 0     # (a stride that is never taken may have any value)
+            tok = x.stride(1) if x.shape[1] > 1 else 0
+            if seq % 8 or tok % 8 or x.data_ptr() % 16:
+                raise ValueError("new rows start on 16-byte boundaries")
+            args += [x.data_ptr(), seq, tok]
+        if k_new.shape[1] != v_new.shape[1]:
+            raise ValueError("k_new and v_new hold the same number of rows")
+        self._per_seq(start, count)
+        self._on_device(full, k_new, v_new, start, count)
+        self._quant(lib.rkv_quant_store, stream, *args, k_new.shape[1], _ptr(start), _ptr(count), ctypes.byref(full))
+
+    def quant_full_attention(self, q, full: RkvQuantCache, out, active=None, max_len_hint=0, keep_logits=True, stream=None):
+        """Attention over an 8-bit cache.  keep_logits: leave what score_keys / select_topk need in the workspace."""
+        self._q_shape(q, out)
+        self._per_seq(active)
+        self._on_device(full, q, out, active)
+        self._quant(lib.rkv_quant_full_attention, stream, _ptr(q), ctypes.byref(full), _ptr(active), _ptr(out),
+                    1 if keep_logits else 0, max_len_hint)
+
+    def quant_full_step(self, q, full: RkvQuantCache, k_small, k_max, out, topk_idx, active=None, scores=None,
+                        q_last_full=None, max_len_hint=0, stream=None):
+        stride = scores.shape[-1] if scores is not None else 0
+        self._q_shape(q, out, q_last_full)
+        self._per_seq(k_small, active)
+        self._on_device(full, q, out, k_small, topk_idx, active, scores, q_last_full)
+        self._quant(lib.rkv_quant_full_step, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
+                    _ptr(out), _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full), max_len_hint)
+
+    def quant_gather_small(self, topk_idx, k_small, k_max, full: RkvQuantCache, small: RkvCache, active=None, stream=None):
+        """Rebuild of the bf16 small cache from the selected positions of an 8-bit full cache."""
+        if topk_idx.dtype != torch.int32 or topk_idx.numel() != self.cfg.n_seq * self.cfg.n_kv_heads * k_max:
+            raise ValueError("topk_idx is an int32 tensor [B, Hkv, k_max]")
+        self._per_seq(k_small, active)
+        self._on_device(full, topk_idx, k_small, active)
+        self._quant(lib.rkv_quant_gather_small, stream, _ptr(topk_idx), _ptr(k_small), k_max, ctypes.byref(full),
+                    ctypes.byref(small), _ptr(active))
 
     def should_refresh(self, q_now, q_last_full, threshold, flag, sim=None, keep=None, stream=None):
         self._check(lib.rkv_should_refresh(self._h, _ptr(q_now), _ptr(q_last_full), float(threshold), _ptr(flag),

@@ -23,7 +23,7 @@ class LayerState:
         self.k_max = max(max(k_small), 1)
         self.k_small = torch.tensor(k_small, dtype=torch.int32, device=dev)
         self.small = alloc_cache([k + small_extra for k in k_small], [0] * self.n_seq, n_kv_heads, dev, fill=0.0)
-        self.full_c = rkv.cache_struct(full.k, full.v, full.row_offset, full.cap, full.len)
+        self.full_c = self._describe_full(full)
         self.small_c = rkv.cache_struct(self.small.k, self.small.v, self.small.row_offset, self.small.cap,
                                         self.small.len)
         self.out = torch.zeros((self.n_seq, n_q_heads, HEAD_DIM), dtype=torch.bfloat16, device=dev)
@@ -36,6 +36,10 @@ class LayerState:
         if want_scores:
             stride = int(full.cap.max().item())
             self.scores = torch.zeros((self.n_seq, n_kv_heads, stride), dtype=torch.float32, device=dev)
+
+    @staticmethod
+    def _describe_full(full):
+        return rkv.cache_struct(full.k, full.v, full.row_offset, full.cap, full.len)
 
     def enable_eviction(self, max_evict: int):
         """Fixed-size small cache: allocate the eviction order and counter that the *_evict calls keep."""
@@ -116,6 +120,68 @@ class LayerState:
     def check_trigger(self, q, threshold):
         self.ctx.should_refresh(q, self.q_last_full, threshold, self.flag, self.sim, keep=self.not_flag)
         return self.flag
+
+
+class QuantLayerState(LayerState):
+    """A layer whose full cache C_f is held in 8 bits (synth.QuantLayerCache): half the memory and half the bytes of a
+    full step.  C_p stays bf16, rebuilt from C_f's values.  Takes the place of a LayerState in the schedules below;
+    the eviction and score-only forms are those of a bf16 C_f."""
+
+    @staticmethod
+    def _describe_full(full):
+        return rkv.quant_cache_struct(full.k, full.v, full.k_scale, full.v_scale, full.row_offset, full.cap, full.len)
+
+    def _refused(self, *args, **kwargs):
+        raise NotImplementedError("not built for a full cache in 8 bits")
+
+    enable_eviction = refresh_evict = append_partial_evict = refresh_scores_only = _refused
+
+    def store_prompt(self, k_new, v_new, start=None, count=None):
+        """Rows [B, T, Hkv, 128] join the full cache (a prompt, or a chunk of one)."""
+        self.ctx.quant_store(k_new, v_new, self.full_c, start=start, count=count)
+
+    def _rows(self, x):
+        return x.view(self.n_seq, 1, self.n_kv, HEAD_DIM)
+
+    def _store(self, k_new, v_new, stream=None):
+        self.ctx.quant_store(self._rows(k_new), self._rows(v_new), self.full_c, stream=stream)
+
+    def refresh(self, q, active=None, max_len_hint=0):
+        self.ctx.quant_full_step(q, self.full_c, self.k_small, self.k_max, self.out, self.topk_idx, active=active,
+                                 scores=self.scores, q_last_full=self.q_last_full, max_len_hint=max_len_hint)
+        self._rebuild(active)
+        return self.out
+
+    def _rebuild(self, active=None, stream=None):
+        self.ctx.quant_gather_small(self.topk_idx, self.k_small, self.k_max, self.full_c, self.small_c, active=active,
+                                    stream=stream)
+
+    def refresh_attention(self, q, active=None, max_len_hint=0, stream=None):
+        self.ctx.quant_full_attention(q, self.full_c, self.out, active=active, max_len_hint=max_len_hint, stream=stream)
+        return self.out
+
+    def append_refresh_attention(self, q, k_new, v_new, active=None, max_len_hint=0, stream=None):
+        self._store(k_new, v_new, stream)
+        return self.refresh_attention(q, active, max_len_hint, stream)
+
+    def refresh_select(self, q, active=None, stream=None):
+        self.ctx.select_topk(q, self.full_c, self.k_small, self.k_max, self.topk_idx, active=active, scores=self.scores,
+                             q_last_full=self.q_last_full, stream=stream)
+        self._rebuild(active, stream)
+
+    def refresh_select_only(self, active=None, stream=None):
+        self.ctx.select_topk(None, self.full_c, self.k_small, self.k_max, self.topk_idx, active=active, stream=stream)
+        self._rebuild(active, stream)
+
+    def append_partial(self, q, k_new, v_new, active=None, max_len_hint=0):
+        """The row joins C_f (encoded) and C_p; attention over C_p."""
+        self._store(k_new, v_new)
+        self.ctx.append_small_step(q, k_new, v_new, None, self.small_c, self.out, active=active, max_len_hint=max_len_hint)
+        return self.out
+
+    def append(self, k_new, v_new):
+        self._store(k_new, v_new)
+        self.ctx.append(k_new, v_new, None, self.small_c)
 
 
 class OverlappedRefresh:

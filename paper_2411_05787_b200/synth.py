@@ -166,6 +166,36 @@ def alloc_cache(caps: list, lens: list, n_kv_heads: int, device, fill=None) -> L
                       torch.tensor(lens, dtype=torch.int32, device=device))
 
 
+@dataclass
+class QuantLayerCache:
+    """Packed 8-bit K/V buffers of one layer, their scales per block of 64 rows, and the index tensors."""
+    k: torch.Tensor           # [n_rows, 128] float8_e4m3fn
+    v: torch.Tensor
+    k_scale: torch.Tensor     # [n_rows / 64] fp32
+    v_scale: torch.Tensor
+    row_offset: torch.Tensor  # [B] int64, multiples of 64
+    cap: torch.Tensor         # [B] int32, multiples of 64
+    len: torch.Tensor         # [B] int32
+
+    @property
+    def n_rows(self) -> int:
+        return self.k.shape[0]
+
+
+def alloc_quant_cache(caps: list, n_kv_heads: int, device) -> QuantLayerCache:
+    """Allocate one layer's packed 8-bit K/V, empty; capacities are rounded up to whole blocks of 64."""
+    caps = [max(64, (c + 63) // 64 * 64) for c in caps]
+    offs, total = [], 0
+    for c in caps:
+        offs.append(total)
+        total += n_kv_heads * c
+    k, v = (torch.zeros((total, HEAD_DIM), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+    return QuantLayerCache(k, v, *(torch.ones((total // 64,), dtype=torch.float32, device=device) for _ in range(2)),
+                           torch.tensor(offs, dtype=torch.int64, device=device),
+                           torch.tensor(caps, dtype=torch.int32, device=device),
+                           torch.zeros((len(caps),), dtype=torch.int32, device=device))
+
+
 def unit_group_mean(q: torch.Tensor, n_kv_heads: int) -> torch.Tensor:
     """Unit vector of the mean of the G query heads of every KV group: [Hkv, 128] fp32."""
     qf = q.float().reshape(n_kv_heads, -1, HEAD_DIM).mean(dim=1)
