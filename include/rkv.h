@@ -343,6 +343,51 @@ rkv_status rkv_quant_gather_small(rkv_ctx* ctx, const int32_t* topk_idx, const i
                                   const int32_t* active, void* stream);
 
 /*
+ * Rotary positions in front of the cache (the paper's models, Sec. 3, rotate queries and keys; contexts beyond the
+ * trained length scale the frequencies): the rows of the fused projection are split into queries, keys and values, and
+ * in every query and key head the first rot_dim channels are turned,
+ *   (x, y) -> (x cos a - y sin a, x sin a + y cos a) * amplitude,   a = pos[t] * f_i,
+ * i = 0 .. rot_dim/2 - 1, in fp32, rounded once to bf16; the other channels and the values are copied.
+ *   RKV_ROPE_HALF         pairs (i, i + rot_dim/2)
+ *   RKV_ROPE_INTERLEAVED  pairs (2i, 2i + 1)
+ * Frequencies, with w_i = theta^(-2i / rot_dim):
+ *   RKV_ROPE_NONE     f_i = w_i
+ *   RKV_ROPE_LINEAR   f_i = w_i / factor
+ *   RKV_ROPE_BANDS    with n_i = trained_len w_i / 2 pi (turns over the trained length):  w_i where n_i >= high, w_i / factor
+ *                     where n_i <= low, and between them the mean of the two weighted by (n_i - low) / (high - low)
+ *   RKV_ROPE_RAMP     r_i = clamp((i - first) / max(last - first, 0.001), 0, 1),  f_i = w_i (1 - r_i) + w_i / factor r_i,
+ *                     first, last = rot_dim ln(trained_len / (2 pi n)) / (2 ln theta) for n = fast (floor, at least 0) and
+ *                     slow (ceil, at most rot_dim - 1); amplitude = 0.1 ln(factor) + 1 (1 in the other forms)
+ */
+#define RKV_ROPE_HALF 0
+#define RKV_ROPE_INTERLEAVED 1
+#define RKV_ROPE_NONE 0
+#define RKV_ROPE_LINEAR 1
+#define RKV_ROPE_BANDS 2
+#define RKV_ROPE_RAMP 3
+typedef struct {
+  int32_t rot_dim;      /* a multiple of 16, 16..128                           */
+  int32_t scaling;      /* RKV_ROPE_NONE .. RKV_ROPE_RAMP                      */
+  double theta;         /* > 1                                                 */
+  double factor;        /* >= 1 (ignored by RKV_ROPE_NONE)                     */
+  int32_t trained_len;  /* >= 1              } RKV_ROPE_BANDS and RKV_ROPE_RAMP */
+  double low, high;     /* 0 < low < high    } RKV_ROPE_BANDS                  */
+  double fast, slow;    /* 0 < slow < fast   } RKV_ROPE_RAMP                   */
+} rkv_rope_config;
+/* Host.  freqs[i] = f_i / 2 pi in turns per position, as a fraction of 2^64 (rot_dim / 2 of them); *amplitude. */
+rkv_status rkv_rope_frequencies(const rkv_rope_config* cfg /*host*/, uint64_t* freqs /*host*/, float* amplitude /*host*/);
+/* One launch for n_tok tokens (a prompt's, a chunk's, or one).
+ *   qkv        [n_tok][Hq + 2 Hkv][128], bf16 (is_bf16 != 0) or fp32: queries, keys, values; 16-byte aligned, token t at
+ *              t * tok_stride elements (a multiple of 16 bytes)
+ *   pos        int32 [n_tok], any value (the angle is exact for all of them)
+ *   freqs      DEVICE copy of rkv_rope_frequencies' output, with its rot_dim and amplitude
+ *   q          bf16 [n_tok][Hq][128];  k, v  bf16 [n_tok][Hkv][128];  v NULL: the values are not copied
+ * The outputs must not overlap qkv.  Only Hq and Hkv of the context's configuration are read. */
+rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_stride, const int32_t* pos,
+                    int32_t n_tok, const uint64_t* freqs, int32_t rot_dim, int32_t layout, float amplitude, void* q,
+                    void* k, void* v, void* stream);
+
+/*
  * Refresh trigger (Sec. 2.2 "Deciding when to decode with full cache").
  *   qbar  = mean over the Hq heads of q_now[b];  qbar' likewise from q_last_full[b]
  *   sim   = <qbar, qbar'> / (|qbar| |qbar'|)          (fp32)
@@ -461,15 +506,16 @@ rkv_status rkv_get_option(const rkv_ctx* ctx, int32_t option, int32_t* value);
  * the sums and the launch counts and forgets the samples.  Do not enable it during stream capture.
  *   total_us, launches   host arrays of RKV_KERNEL_KINDS entries
  */
-#define RKV_KERNEL_ATTN_FULL 0  /* full-cache attention + logit emission (rkv_full_step, 1st kernel) */
+#define RKV_KERNEL_ATTN_FULL 0  /* full-cache attention + logit emission (rkv_[quant_]full_step, 1st kernel) */
 #define RKV_KERNEL_SELECT 1     /* top-K from the keys' histogram        (rkv_full_step, 3rd kernel) */
 #define RKV_KERNEL_ATTN_SMALL 2 /* small-cache attention                 (rkv_small_step)            */
-#define RKV_KERNEL_GATHER 3     /* rkv_gather_small                                                  */
-#define RKV_KERNEL_APPEND 4     /* rkv_append                                                        */
+#define RKV_KERNEL_GATHER 3     /* rkv_gather_small, rkv_quant_gather_small                          */
+#define RKV_KERNEL_APPEND 4     /* rkv_append, rkv_quant_store                                       */
 #define RKV_KERNEL_TRIGGER 5    /* rkv_should_refresh                                                */
 #define RKV_KERNEL_FOLD 6       /* output from the split partials        (rkv_[append_]full_attention, 2nd kernel) */
 #define RKV_KERNEL_SCORE 7      /* logits -> scores, keys, histogram     (rkv_full_step, 2nd kernel) */
-#define RKV_KERNEL_KINDS 8
+#define RKV_KERNEL_ROPE 8       /* rkv_rope                                                          */
+#define RKV_KERNEL_KINDS 9
 rkv_status rkv_set_profiling(rkv_ctx* ctx, int32_t on);
 rkv_status rkv_get_profile(rkv_ctx* ctx, double* total_us /*host*/, int64_t* launches /*host*/);
 

@@ -706,6 +706,68 @@ rkv_status rkv_quant_gather_small(rkv_ctx* ctx, const int32_t* topk_idx, const i
   return RKV_OK;
 }
 
+rkv_status rkv_rope_frequencies(const rkv_rope_config* c, uint64_t* freqs, float* amplitude) {
+  if (!c || !freqs || !amplitude) return RKV_ERR_INVALID_ARG;
+  if (c->rot_dim < 16 || c->rot_dim > rkv::kHeadDim || c->rot_dim % 16 != 0 || c->scaling < RKV_ROPE_NONE ||
+      c->scaling > RKV_ROPE_RAMP)
+    return RKV_ERR_UNSUPPORTED;
+  const bool scaled = c->scaling != RKV_ROPE_NONE;
+  if (!(c->theta > 1.0) || isinf(c->theta) || (scaled && (!(c->factor >= 1.0) || isinf(c->factor))))
+    return RKV_ERR_INVALID_ARG;
+  if (c->scaling >= RKV_ROPE_BANDS && c->trained_len < 1) return RKV_ERR_INVALID_ARG;
+  if (c->scaling == RKV_ROPE_BANDS && !(c->low > 0.0 && c->low < c->high)) return RKV_ERR_INVALID_ARG;
+  if (c->scaling == RKV_ROPE_RAMP && !(c->slow > 0.0 && c->slow < c->fast)) return RKV_ERR_INVALID_ARG;
+  constexpr long double kTwoPi = 6.283185307179586476925286766559L;
+  const long double factor = scaled ? c->factor : 1.0L, ln_theta = logl((long double)c->theta);
+  double first = 0.0, last = 0.0;
+  if (c->scaling == RKV_ROPE_RAMP) {   // the pairs that turn `fast` and `slow` times over the trained length
+    auto at = [&](double turns) {
+      return (double)(c->rot_dim * logl(c->trained_len / (turns * kTwoPi)) / (2.0L * ln_theta));
+    };
+    first = fmax(floor(at(c->fast)), 0.0);
+    last = fmin(ceil(at(c->slow)), (double)(c->rot_dim - 1));
+  }
+  for (int i = 0; i < c->rot_dim / 2; ++i) {
+    const long double w = expl(-2.0L * i / c->rot_dim * ln_theta);
+    long double stretched = 1.0L;      // share of w / factor
+    if (!scaled) {
+      stretched = 0.0L;
+    } else if (c->scaling == RKV_ROPE_BANDS) {
+      const long double turns = c->trained_len * w / kTwoPi;
+      const long double kept = turns >= c->high ? 1.0L : turns <= c->low ? 0.0L : (turns - c->low) / ((long double)c->high - c->low);
+      stretched = 1.0L - kept;
+    } else if (c->scaling == RKV_ROPE_RAMP) {
+      stretched = fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);
+    }
+    const long double f = (w * (1.0L - stretched) + w / factor * stretched) / kTwoPi;   // < 0.16 turns per position
+    freqs[i] = (uint64_t)roundl(ldexpl(f, 64));
+  }
+  *amplitude = c->scaling == RKV_ROPE_RAMP ? (float)(0.1L * logl(factor) + 1.0L) : 1.0f;
+  return RKV_OK;
+}
+
+rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_stride, const int32_t* pos,
+                    int32_t n_tok, const uint64_t* freqs, int32_t rot_dim, int32_t layout, float amplitude, void* q,
+                    void* k, void* v, void* stream) {
+  if (!ctx || !qkv || !pos || !freqs || !q || !k || n_tok < 1 || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+  if (rot_dim < 16 || rot_dim > rkv::kHeadDim || rot_dim % 16 != 0 || (layout != RKV_ROPE_HALF && layout != RKV_ROPE_INTERLEAVED))
+    return RKV_ERR_UNSUPPORTED;
+  if (!aligned16(qkv) || !aligned16(q) || !aligned16(k) || !aligned16(v) || (tok_stride * (is_bf16 ? 2 : 4)) % 16 != 0 ||
+      (reinterpret_cast<uintptr_t>(freqs) & 7) != 0)
+    return RKV_ERR_INVALID_ARG;   // the kernel reads and writes 16 bytes at a time
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_ROPE);
+    e = rkv::launch_rope(qkv, is_bf16 != 0, tok_stride, pos, n_tok, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads, freqs,
+                         rot_dim, layout == RKV_ROPE_INTERLEAVED, amplitude, q, k, v, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "rotary launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  return RKV_OK;
+}
+
 rkv_status rkv_full_step(rkv_ctx* ctx, const void* q, const rkv_cache* full, const int32_t* k_small, int32_t k_max,
                          const int32_t* active, void* out, float* scores, int64_t score_stride, int32_t* topk_idx,
                          void* q_last_full, int32_t max_len_hint, void* stream) {

@@ -155,6 +155,9 @@ cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small,
                                 const CacheDev& small_cache, const int32_t* active, int n_seq, int n_kv_heads,
                                 int32_t* status, cudaStream_t st);
 cudaError_t prepare_quant_attention();
+cudaError_t launch_rope(const void* qkv, bool is_bf16, int64_t tok_stride, const int32_t* pos, int n_tok, int n_q,
+                        int n_kv, const uint64_t* freqs, int rot, bool interleaved, float amp, void* q, void* k, void* v,
+                        cudaStream_t st);
 
 cudaError_t launch_attention(const AttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                              int n_seq, int grid_x, bool write_logits, cudaStream_t st, bool append = false);

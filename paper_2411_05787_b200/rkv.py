@@ -26,13 +26,13 @@ EXPORTS = ["rkv_create", "rkv_destroy", "rkv_workspace_bytes", "rkv_full_step", 
            "rkv_gather_small_evict", "rkv_append_small_step_evict", "rkv_full_attention", "rkv_select_topk",
            "rkv_append_full_attention", "rkv_get_option", "rkv_score_keys", "rkv_quant_store",
            "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk", "rkv_quant_full_step",
-           "rkv_quant_gather_small"]
+           "rkv_quant_gather_small", "rkv_rope_frequencies", "rkv_rope"]
 QUANT_BLOCK = 64
 NOALLOC_MAX_PROBLEMS, NOALLOC_MAX_LEN = 32, 65536
 OPT_SMALL_MIN_CHUNK, OPT_DEPENDENT_LAUNCH, OPT_SMALL_CLUSTER, OPT_EARLY_CACHE_READ, OPT_INTERLEAVE_TILES = 1, 2, 3, 4, 5
 OPT_SELECT_KEYS_PER_CTA = 6
 OPT_SCORE_SLICE = 7
-KERNEL_NAMES = ["attn_full", "select", "attn_small", "gather", "append", "trigger", "fold", "score"]
+KERNEL_NAMES = ["attn_full", "select", "attn_small", "gather", "append", "trigger", "fold", "score", "rope"]
 
 
 class RkvConfig(ctypes.Structure):
@@ -50,6 +50,16 @@ class RkvQuantCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_rows", ctypes.c_int64), ("row_offset", ctypes.c_void_p), ("cap", ctypes.c_void_p),
                 ("len", ctypes.c_void_p)]
+
+
+class RkvRopeConfig(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("theta", ctypes.c_double),
+                ("factor", ctypes.c_double), ("trained_len", ctypes.c_int32), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("fast", ctypes.c_double), ("slow", ctypes.c_double)]
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2, "ramp": 3}
 
 
 def _load() -> ctypes.CDLL:
@@ -108,7 +118,10 @@ def _load() -> ctypes.CDLL:
     lib.rkv_quant_select_topk.argtypes = [vp, vp, quantp, vp, i32, vp, vp, i64, vp, vp, vp]
     lib.rkv_quant_full_step.argtypes = [vp, vp, quantp, vp, i32, vp, vp, vp, i64, vp, vp, i32, vp]
     lib.rkv_quant_gather_small.argtypes = [vp, vp, vp, i32, quantp, cachep, vp, vp]
-    for name in ("rkv_quant_store", "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk",
+    lib.rkv_rope_frequencies.argtypes = [ctypes.POINTER(RkvRopeConfig), ctypes.POINTER(ctypes.c_uint64),
+                                         ctypes.POINTER(f32)]
+    lib.rkv_rope.argtypes = [vp, vp, i32, i64, vp, i32, vp, i32, i32, f32, vp, vp, vp, vp]
+    for name in ("rkv_rope_frequencies", "rkv_rope", "rkv_quant_store", "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk",
                  "rkv_quant_full_step", "rkv_quant_gather_small"):
         getattr(lib, name).restype = i32
     for name in ("rkv_create", "rkv_destroy", "rkv_full_step", "rkv_gather_small", "rkv_small_step",
@@ -174,6 +187,29 @@ def quant_cache_struct(k8, v8, k_scale, v_scale, row_offset, cap, length) -> Rkv
         raise ValueError("row_offset, cap and length have one element per sequence")
     c.n_seq = cap.numel()
     return c
+
+
+class RopeTable:
+    """What rkv_rope needs of a model's rotary positions, laid out once: the frequencies as fixed-point turns on the
+    device, the rotated part, the pairs' layout and the amplitude (formulas: include/rkv.h).
+
+    layout: "half" or "interleaved"; scaling: "none", "linear", "bands" (trained_len, low, high) or "ramp" (trained_len,
+    fast, slow)."""
+
+    def __init__(self, rot_dim=128, theta=10000.0, layout="half", scaling="none", factor=1.0, trained_len=8192, low=1.0,
+                 high=4.0, fast=32.0, slow=1.0, device="cuda"):
+        if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+            raise ValueError(f"layout is one of {list(ROPE_LAYOUTS)}, scaling one of {list(ROPE_SCALINGS)}")
+        cfg = RkvRopeConfig(rot_dim, ROPE_SCALINGS[scaling], theta, factor, trained_len, low, high, fast, slow)
+        turns = (ctypes.c_uint64 * 64)()
+        amp = ctypes.c_float(0.0)
+        rc = lib.rkv_rope_frequencies(ctypes.byref(cfg), turns, ctypes.byref(amp))
+        if rc != RKV_OK:
+            raise RkvError(rc, "rotary positions")
+        self.rot_dim, self.layout, self.amplitude = rot_dim, ROPE_LAYOUTS[layout], amp.value
+        self.turns = [turns[i] for i in range(rot_dim // 2)]          # f_i / 2 pi as a fraction of 2^64
+        signed = [t - (1 << 64) if t >> 63 else t for t in self.turns]
+        self.freqs = torch.tensor(signed, dtype=torch.int64).to(device)
 
 
 def small_step_noalloc(cfg: RkvConfig, q, small: RkvCache, out, active=None, max_len_hint=0, device_status=None,
@@ -252,7 +288,7 @@ class Context:
         stride = scores.shape[-1] if scores is not None else 0
         if isinstance(full, RkvQuantCache):
             self._on_device(full, q, k_small, topk_idx, active, scores, q_last_full)
-            self._quant(lib.rkv_quant_select_topk, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max,
+            self._call(lib.rkv_quant_select_topk, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max,
                         _ptr(active), _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full))
             return
         self._check(lib.rkv_select_topk(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
@@ -264,7 +300,7 @@ class Context:
         stride = scores.shape[-1] if scores is not None else 0
         if isinstance(full, RkvQuantCache):
             self._on_device(full, q, k_small, active, scores, q_last_full)
-            self._quant(lib.rkv_quant_score_keys, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
+            self._call(lib.rkv_quant_score_keys, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                         _ptr(scores), stride, _ptr(q_last_full))
             return
         self._check(lib.rkv_score_keys(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
@@ -303,7 +339,7 @@ class Context:
                                                     _ptr(evict_order), _ptr(evict_count), evict_order.shape[-1],
                                                     max_len_hint, _stream(stream)))
 
-    # ------------------------------------------------------------------ the full cache in 8 bits
+    # ------------------------------------------------------------------ the full cache in 8 bits, rotary positions
     def _on_device(self, cache, *tensors):
         if cache.device != self.device:
             raise ValueError("the cache is on another device than the context")
@@ -313,7 +349,7 @@ class Context:
             if t is not None and t.device.index != self.device:
                 raise ValueError("a tensor is on another device than the context")
 
-    def _quant(self, fn, stream, *args):
+    def _call(self, fn, stream, *args):
         """One call on the context's device, whichever is current, and on its current stream unless one is given."""
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
@@ -354,14 +390,14 @@ class Context:
             raise ValueError("k_new and v_new hold the same number of rows")
         self._per_seq(start, count)
         self._on_device(full, k_new, v_new, start, count)
-        self._quant(lib.rkv_quant_store, stream, *args, k_new.shape[1], _ptr(start), _ptr(count), ctypes.byref(full))
+        self._call(lib.rkv_quant_store, stream, *args, k_new.shape[1], _ptr(start), _ptr(count), ctypes.byref(full))
 
     def quant_full_attention(self, q, full: RkvQuantCache, out, active=None, max_len_hint=0, keep_logits=True, stream=None):
         """Attention over an 8-bit cache.  keep_logits: leave what score_keys / select_topk need in the workspace."""
         self._q_shape(q, out)
         self._per_seq(active)
         self._on_device(full, q, out, active)
-        self._quant(lib.rkv_quant_full_attention, stream, _ptr(q), ctypes.byref(full), _ptr(active), _ptr(out),
+        self._call(lib.rkv_quant_full_attention, stream, _ptr(q), ctypes.byref(full), _ptr(active), _ptr(out),
                     1 if keep_logits else 0, max_len_hint)
 
     def quant_full_step(self, q, full: RkvQuantCache, k_small, k_max, out, topk_idx, active=None, scores=None,
@@ -370,7 +406,7 @@ class Context:
         self._q_shape(q, out, q_last_full)
         self._per_seq(k_small, active)
         self._on_device(full, q, out, k_small, topk_idx, active, scores, q_last_full)
-        self._quant(lib.rkv_quant_full_step, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
+        self._call(lib.rkv_quant_full_step, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                     _ptr(out), _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full), max_len_hint)
 
     def quant_gather_small(self, topk_idx, k_small, k_max, full: RkvQuantCache, small: RkvCache, active=None, stream=None):
@@ -379,8 +415,28 @@ class Context:
             raise ValueError("topk_idx is an int32 tensor [B, Hkv, k_max]")
         self._per_seq(k_small, active)
         self._on_device(full, topk_idx, k_small, active)
-        self._quant(lib.rkv_quant_gather_small, stream, _ptr(topk_idx), _ptr(k_small), k_max, ctypes.byref(full),
+        self._call(lib.rkv_quant_gather_small, stream, _ptr(topk_idx), _ptr(k_small), k_max, ctypes.byref(full),
                     ctypes.byref(small), _ptr(active))
+
+    def rope(self, qkv, pos, table: RopeTable, q, k, v=None, stream=None):
+        """Split the fused projection's rows [T, (Hq + 2 Hkv) * 128] (bfloat16 or float32; tokens may be strided) into
+        q [T, Hq, 128] and k, v [T, Hkv, 128] (bfloat16), queries and keys turned by their positions.  pos: int32 [T].
+        v=None: the values are not copied."""
+        nq, nkv, n = self.cfg.n_q_heads, self.cfg.n_kv_heads, qkv.shape[0]
+        if qkv.dtype not in (torch.bfloat16, torch.float32) or qkv.dim() != 2 or qkv.shape[1] != (nq + 2 * nkv) * 128 or n < 1:
+            raise ValueError("qkv is a bfloat16 or float32 tensor [T, (Hq + 2 Hkv) * 128]")
+        if pos.dtype != torch.int32 or pos.numel() != n:
+            raise ValueError("pos is an int32 tensor [T]")
+        for t, heads in ((q, nq), (k, nkv), (v, nkv)):
+            if t is not None and (t.dtype != torch.bfloat16 or t.numel() != n * heads * 128):
+                raise ValueError("q, k and v are bfloat16 tensors [T, heads, 128]")
+        if any(t is not None and t.device.index != self.device for t in (qkv, pos, table.freqs, q, k, v)):
+            raise ValueError("a tensor is on another device than the context")
+        stride = qkv.stride(0) if n > 1 else 0
+        if qkv.stride(1) != 1 or stride * qkv.element_size() % 16 or qkv.data_ptr() % 16:
+            raise ValueError("the projection's rows are contiguous and start on 16-byte boundaries")
+        self._call(lib.rkv_rope, stream, qkv.data_ptr(), 1 if qkv.dtype == torch.bfloat16 else 0, stride, _ptr(pos), n,
+                    _ptr(table.freqs), table.rot_dim, table.layout, table.amplitude, _ptr(q), _ptr(k), _ptr(v))
 
     def should_refresh(self, q_now, q_last_full, threshold, flag, sim=None, keep=None, stream=None):
         self._check(lib.rkv_should_refresh(self._h, _ptr(q_now), _ptr(q_last_full), float(threshold), _ptr(flag),
