@@ -140,15 +140,17 @@ struct QuantAttnParams {
   const int64_t* row_offset; const int32_t* cap; const int32_t* len; const int32_t* active;
   void* out;                  // bf16 [B][Hq][128]: written here for empty sequences only
   float* partials; float* ml_t; float* logits;  // as in AttnParams
+  uint32_t* hist;             // [B*Hkv][kSelectBins]: cleared when logits are kept
   int32_t* status;
   int64_t n_rows, logit_stride;
   int32_t n_q_heads, n_kv_heads, group, gp, max_splits, max_len;
   int32_t spec;               // 1: first tiles may be requested before the length is read (one sequence, no mask)
+  int32_t early;              // how many of them before the dependency wait (AttnParams::early)
   float scale;
 };
 
 cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                                   int n_seq, int grid_x, cudaStream_t st);
+                                   int n_seq, int grid_x, bool cluster, cudaStream_t st);
 cudaError_t launch_quant_store(const QuantNew& rows, const int32_t* start, const int32_t* count, const QuantDev& c,
                                int n_seq, int n_kv_heads, int32_t* tickets, int32_t* status, cudaStream_t st);
 cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small, int k_max, const QuantDev& full,
@@ -233,6 +235,8 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 // library starts).
 void note_launch(cudaStream_t st, const rkv_cache* a, const rkv_cache* b, bool fold = false);
 bool early_read_safe(cudaStream_t st, const rkv_cache* c);
+void note_quant_store(cudaStream_t st, const rkv_quant_cache* c);   // the last launch writes rows of an 8-bit cache
+bool early_read_safe(cudaStream_t st, const rkv_quant_cache* c);
 bool last_launch_was_fold(cudaStream_t st);   // the library's last launch on the stream was the full step's merge kernel
 
 cudaError_t prepare_attention();  // one-time function attributes (dynamic shared memory sizes)

@@ -39,6 +39,7 @@ constexpr int kQBand = kQuantTile / kQWarps;         // positions of a tile per 
 constexpr int kQBlocks = kQBand / 16;                // 16-row MMA blocks per band
 constexpr int kQRow = 144;                           // halves per query row in shared memory (fragment reads spread over the banks)
 constexpr int kQOPad = 132;                          // floats per head row in the merge buffer
+constexpr int kQCluster = 8;                         // most CTAs that finish an output together
 constexpr float kPBase = 8192.f;                     // 2^13: the largest p'
 static_assert(kQuantBlock % kQBand == 0, "a warp's band must not straddle two blocks");
 
@@ -68,7 +69,19 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <bool kLogits>
+__device__ __forceinline__ float4 ld_peer4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ float2 ld_peer2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+  return v;
+}
+
+// kCluster: the CTAs of a (sequence, KV head) are one thread-block cluster and finish the output themselves.
+template <bool kLogits, bool kCluster>
 __global__ void __launch_bounds__(kQThreads, 2)
 quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const QuantAttnParams p) {
@@ -111,18 +124,27 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   };
   uint64_t policy;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-  pdl_wait();
-  pdl_launch();   // after the wait: at most one predecessor is ever in flight behind a kernel of this library
   // One sequence and no mask: the first tiles are requested before the length has been read, as far as the host's
-  // bound says that there are any (rows past the buffer's end arrive as zeros; tiles past the length are ignored).
-  int n_spec = 0;
+  // bound says that there are any (rows past the buffer's end arrive as zeros; tiles past the length are ignored),
+  // and p.early of them before the dependency wait, when the launch before this one leaves the cache alone.
+  int n_spec = 0, n_early = 0;
   if (p.spec != 0 && layout_ok) {
     const int room = cap < p.max_len ? cap : p.max_len;
     const int bound = (room + kQuantTile - 1) / kQuantTile;
     n_spec = bound > split ? (bound - split + n_cta - 1) / n_cta : 0;
     if (n_spec > kQStages) n_spec = kQStages;
-    if (tid == 32 * kQWarps)
-      for (int t = 0; t < n_spec; ++t) issue_tile(t, policy);
+    n_early = p.early < n_spec ? p.early : n_spec;
+  }
+  if (tid == 32 * kQWarps)
+    for (int t = 0; t < n_early; ++t) issue_tile(t, policy);
+  pdl_wait();
+  pdl_launch();   // after the wait: at most one predecessor is ever in flight behind a kernel of this library
+  if (tid == 32 * kQWarps)
+    for (int t = n_early; t < n_spec; ++t) issue_tile(t, policy);
+
+  if (kLogits) {   // the score pass that may follow adds to the keys' histogram: it starts from zero, whatever ran before
+    uint32_t* hist = p.hist + ((int64_t)b * p.n_kv_heads + g) * kSelectBins;
+    for (int i = split * kQThreads + tid; i < kSelectBins; i += n_cta * kQThreads) hist[i] = 0u;
   }
 
   // sizes, queries and the first scales: independent loads, one round trip
@@ -187,7 +209,7 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   const int64_t bg = (int64_t)b * p.n_kv_heads + g;
   float* part = p.partials + (bg * p.max_splits + split) * PartialLayout::kFloats;
   float* ml = p.ml_t + bg * 16 * p.max_splits + split;   // split-contiguous copy of (m, l), for the kernels that read across the splits
-  if (!layout_ok) {   // nothing is read; the kernels behind fold this to zero (they know the length, not the layout)
+  if (!layout_ok) {   // nothing is read; a fold behind this one must come to zero (it knows the length, not the layout)
     if (tid == 0 && split == 0) atomicOr(p.status, RKV_DEV_BAD_LAYOUT);
     for (int i = tid; i < G * kHeadDim; i += kQThreads) part[i] = 0.f;
     if (tid < kMaxGroup) {
@@ -211,7 +233,7 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
   const int total_tiles = (n + kQuantTile - 1) / kQuantTile;
   const int n_tiles = total_tiles > split ? (total_tiles - split + n_cta - 1) / n_cta : 0;
-  if (n_tiles == 0) {
+  if (!kCluster && n_tiles == 0) {   // (in a cluster an idle CTA still owns channels of the output)
     drain_spec();
     return;
   }
@@ -415,6 +437,8 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     }
   }
   consumer_bar_n<32 * kQWarps>();
+  float* sm_sum = reinterpret_cast<float*>(smem + kQStageBytes);   // cluster: this CTA's share, [8][128] and [8][2]
+  float* sm_ml = sm_sum + kMaxGroup * kHeadDim;
   for (int item = tid; item < G * 32; item += 32 * kQWarps) {   // (head, four channels)
     const float* src = sm_o + (item >> 5) * kQOPad + (item & 31) * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -426,7 +450,7 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       acc.z += v.z;
       acc.w += v.w;
     }
-    *reinterpret_cast<float4*>(part + (item >> 5) * kHeadDim + (item & 31) * 4) = acc;
+    *reinterpret_cast<float4*>((kCluster ? sm_sum : part) + (item >> 5) * kHeadDim + (item & 31) * 4) = acc;
   }
   if (tid < kMaxGroup) {
     float M = ninf, L = 0.f;
@@ -435,28 +459,75 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 #pragma unroll
       for (int w = 0; w < kQWarps; ++w) L += sm_l[w * kMaxGroup + tid];
     }
-    part[kMaxGroup * kHeadDim + tid] = M;
-    part[kMaxGroup * kHeadDim + kMaxGroup + tid] = L;
-    ml[(int64_t)tid * p.max_splits] = M;
-    ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = L;
+    if (kCluster) {
+      *reinterpret_cast<float2*>(sm_ml + 2 * tid) = make_float2(M, L);
+    } else {
+      part[kMaxGroup * kHeadDim + tid] = M;
+      part[kMaxGroup * kHeadDim + kMaxGroup + tid] = L;
+    }
+    if (kLogits || !kCluster) {
+      ml[(int64_t)tid * p.max_splits] = M;
+      ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = L;
+    }
+  }
+  if (kCluster) {
+    // Every CTA finishes 128 / C channels of every head from its peers' shared memory; the second barrier keeps that
+    // memory until the last reader is done.  (Threads that have left count as arrived.)
+    cluster_sync_alive();
+    const int c_sh = __ffs(n_cta) - 1, per_sh = 5 - c_sh;      // C = 1, 2, 4 or 8; log2 of the items per head
+    const int h = tid >> per_sh, ch = (split << (7 - c_sh)) + (tid & ((1 << per_sh) - 1)) * 4;
+    for (int hh = h; hh < G; hh += (32 * kQWarps) >> per_sh) {
+      const uint32_t at = smem_u32(sm_sum + hh * kHeadDim + ch), ml_at = smem_u32(sm_ml + 2 * hh);
+      float4 v[kQCluster];
+      float2 e[kQCluster];
+      float M = ninf, L = 0.f;
+#pragma unroll
+      for (int r = 0; r < kQCluster; ++r) {
+        if (r < n_cta) {
+          v[r] = ld_peer4(map_rank(at, r));
+          e[r] = ld_peer2(map_rank(ml_at, r));
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < kQCluster; ++r)
+        if (r < n_cta) M = fmaxf(M, e[r].x);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int r = 0; r < kQCluster; ++r) {
+        if (r < n_cta) {
+          const float w = (e[r].x == ninf) ? 0.f : ex2((e[r].x - M) * kLog2e);
+          L = fmaf(e[r].y, w, L);
+          acc.x = fmaf(v[r].x, w, acc.x);
+          acc.y = fmaf(v[r].y, w, acc.y);
+          acc.z = fmaf(v[r].z, w, acc.z);
+          acc.w = fmaf(v[r].w, w, acc.w);
+        }
+      }
+      const float inv = 1.f / L;
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + head0 + hh * kHeadDim + ch) =
+          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    }
+    cluster_sync_alive();
   }
 }
 
 }  // namespace
 
 cudaError_t prepare_quant_attention() {
-  cudaError_t e = cudaFuncSetAttribute(quant_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmem);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(quant_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmem);
+  cudaError_t e = cudaSuccess;
+  for (auto kernel : {quant_attn_kernel<true, false>, quant_attn_kernel<false, false>, quant_attn_kernel<true, true>,
+                      quant_attn_kernel<false, true>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmem);
   return e;
 }
 
 cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                                   int n_seq, int grid_x, cudaStream_t st) {
-  dim3 grid(grid_x, p.n_kv_heads, n_seq);
-  if (p.logits != nullptr)
-    return launch_ex(quant_attn_kernel<true>, grid, dim3(kQThreads), (size_t)kQSmem, st, 1, tm_k, tm_v, p);
-  return launch_ex(quant_attn_kernel<false>, grid, dim3(kQThreads), (size_t)kQSmem, st, 1, tm_k, tm_v, p);
+                                   int n_seq, int grid_x, bool cluster, cudaStream_t st) {
+  const bool logits = p.logits != nullptr;
+  auto kernel = cluster ? (logits ? quant_attn_kernel<true, true> : quant_attn_kernel<false, true>)
+                        : (logits ? quant_attn_kernel<true, false> : quant_attn_kernel<false, false>);
+  return launch_ex(kernel, dim3(grid_x, p.n_kv_heads, n_seq), dim3(kQThreads), (size_t)kQSmem, st, cluster ? grid_x : 1,
+                   tm_k, tm_v, p);
 }
 
 }  // namespace rkv

@@ -150,6 +150,10 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream    # cudaStream_t of a device's current stream
+_current_device = torch._C._cuda_getDevice
+
+
 def _stream(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
@@ -237,6 +241,7 @@ class Context:
             raise RkvError(rc)
         self._h = handle
         self.device = torch.cuda.current_device()
+        self.cfg_n_seq, self.q_numel = n_seq, n_seq * n_q_heads * 128
 
     def close(self):
         if getattr(self, "_h", None):
@@ -287,10 +292,9 @@ class Context:
                     q_last_full=None, stream=None):
         stride = scores.shape[-1] if scores is not None else 0
         if isinstance(full, RkvQuantCache):
-            self._on_device(full, q, k_small, topk_idx, active, scores, q_last_full)
-            self._call(lib.rkv_quant_select_topk, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max,
-                        _ptr(active), _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full))
-            return
+            at, stride = self._scores(scores)
+            return self._call(lib.rkv_quant_select_topk, stream, self._q(q), self._cache(full), self._seq(k_small), k_max,
+                              self._seq(active), at, stride, self._idx(topk_idx, k_max), self._q(q_last_full))
         self._check(lib.rkv_select_topk(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                                         _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full), _stream(stream)))
 
@@ -299,10 +303,9 @@ class Context:
         """The score pass alone; the next select_topk (scores=None, q_last_full=None) launches the selection alone."""
         stride = scores.shape[-1] if scores is not None else 0
         if isinstance(full, RkvQuantCache):
-            self._on_device(full, q, k_small, active, scores, q_last_full)
-            self._call(lib.rkv_quant_score_keys, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
-                        _ptr(scores), stride, _ptr(q_last_full))
-            return
+            at, stride = self._scores(scores)
+            return self._call(lib.rkv_quant_score_keys, stream, self._q(q), self._cache(full), self._seq(k_small), k_max,
+                              self._seq(active), at, stride, self._q(q_last_full))
         self._check(lib.rkv_score_keys(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                                        _ptr(scores), stride, _ptr(q_last_full), _stream(stream)))
 
@@ -340,103 +343,115 @@ class Context:
                                                     max_len_hint, _stream(stream)))
 
     # ------------------------------------------------------------------ the full cache in 8 bits, rotary positions
-    def _on_device(self, cache, *tensors):
-        if cache.device != self.device:
-            raise ValueError("the cache is on another device than the context")
-        if cache.n_seq != self.cfg.n_seq:
-            raise ValueError("the cache holds another number of sequences than the context")
-        for t in tensors:
-            if t is not None and t.device.index != self.device:
-                raise ValueError("a tensor is on another device than the context")
-
+    # These calls run in decode loops, where the host's time per launch counts: the checks use the tensors' cheapest
+    # accessors, each once.
     def _call(self, fn, stream, *args):
         """One call on the context's device, whichever is current, and on its current stream unless one is given."""
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        if torch.cuda.current_device() == self.device:
-            return self._check(fn(self._h, *args, _stream(stream)))
-        with torch.cuda.device(self.device):
-            return self._check(fn(self._h, *args, _stream(stream)))
+        stream = _raw_stream(self.device) if stream is None else _stream(stream)
+        if _current_device() == self.device:
+            rc = fn(self._h, *args, stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(self._h, *args, stream)
+        if rc != RKV_OK:
+            self._check(rc)
 
-    def _q_shape(self, *tensors):
-        shape = (self.cfg.n_seq, self.cfg.n_q_heads, 128)
-        for t in tensors:
-            if t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != shape):
-                raise ValueError(f"queries and outputs are bfloat16 tensors {list(shape)}")
+    def _cache(self, full):
+        if full.device != self.device:
+            raise ValueError("the cache is on another device than the context")
+        if full.n_seq != self.cfg_n_seq:
+            raise ValueError("the cache holds another number of sequences than the context")
+        return ctypes.byref(full)
 
-    def _per_seq(self, *tensors):
-        for t in tensors:
-            if t is not None and (t.dtype != torch.int32 or t.numel() != self.cfg.n_seq):
-                raise ValueError("per-sequence arguments are int32 tensors with one element per sequence")
+    def _arg(self, t, dtype, numel, what):
+        """Device pointer of a contiguous tensor of this context's device (None: NULL)."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.numel() != numel:
+            raise ValueError(f"{what}: {dtype} with {numel} elements expected, {t.dtype} with {t.numel()} given")
+        if t.get_device() != self.device:
+            raise ValueError(f"{what} is on another device than the context")
+        if not t.is_contiguous():
+            raise ValueError("librkv takes contiguous tensors")
+        return t.data_ptr()
+
+    def _q(self, t):
+        return self._arg(t, torch.bfloat16, self.q_numel, "queries and outputs [B, Hq, 128]")
+
+    def _seq(self, t):
+        return self._arg(t, torch.int32, self.cfg_n_seq, "a per-sequence argument")
+
+    def _idx(self, t, k_max):
+        return self._arg(t, torch.int32, self.cfg_n_seq * self.cfg.n_kv_heads * k_max, "topk_idx [B, Hkv, k_max]")
+
+    def _scores(self, t):
+        if t is None:
+            return None, 0
+        stride = t.shape[-1]
+        return self._arg(t, torch.float32, self.cfg_n_seq * self.cfg.n_kv_heads * stride, "scores [B, Hkv, stride]"), stride
+
+    def _new_rows(self, x, what):
+        n_seq, n_tok, n_kv, dim = x.shape if x.dim() == 4 else (0, 0, 0, 0)
+        if x.dtype is not torch.bfloat16 or n_seq != self.cfg_n_seq or n_kv != self.cfg.n_kv_heads or dim != 128 or n_tok < 1:
+            raise ValueError(f"{what} is a bfloat16 tensor [B, T, Hkv, 128]")
+        if x.get_device() != self.device:
+            raise ValueError(f"{what} is on another device than the context")
+        seq, tok, head, one = x.stride()
+        if one != 1 or (head != 128 and n_kv > 1):
+            raise ValueError("the heads of a new row lie side by side")
+        seq = seq if n_seq > 1 else 0       # (a stride that is never taken may have any value)
+        tok = tok if n_tok > 1 else 0
+        at = x.data_ptr()
+        if seq % 8 or tok % 8 or at % 16:
+            raise ValueError("new rows start on 16-byte boundaries")
+        return at, seq, tok, n_tok
 
     def quant_store(self, k_new, v_new, full: RkvQuantCache, start=None, count=None, stream=None):
         """Append rows to an 8-bit cache.  k_new, v_new: bfloat16 [B, T, Hkv, 128]; sequences and tokens may be strided
         (a slice of a projection's output), the heads of a token lie side by side.  start, count: int32 [B] or None."""
-        args = []
-        for x in (k_new, v_new):
-            if (x.dtype != torch.bfloat16 or x.dim() != 4 or x.shape[0] != self.cfg.n_seq or
-                    x.shape[2:] != (self.cfg.n_kv_heads, 128) or x.shape[1] < 1):
-                raise ValueError("k_new and v_new are bfloat16 tensors [B, T, Hkv, 128]")
-            if not x.is_cuda:
-                raise ValueError("librkv takes device tensors")
-            if x.stride(3) != 1 or (x.stride(2) != 128 and self.cfg.n_kv_heads > 1):
-                raise ValueError("the heads of a new row lie side by side")
-            seq = x.stride(0) if x.shape[0] > 1 else 0     # (a stride that is never taken may have any value)
-            tok = x.stride(1) if x.shape[1] > 1 else 0
-            if seq % 8 or tok % 8 or x.data_ptr() % 16:
-                raise ValueError("new rows start on 16-byte boundaries")
-            args += [x.data_ptr(), seq, tok]
-        if k_new.shape[1] != v_new.shape[1]:
+        k, k_seq, k_tok, n_tok = self._new_rows(k_new, "k_new")
+        v, v_seq, v_tok, n_tok_v = self._new_rows(v_new, "v_new")
+        if n_tok != n_tok_v:
             raise ValueError("k_new and v_new hold the same number of rows")
-        self._per_seq(start, count)
-        self._on_device(full, k_new, v_new, start, count)
-        self._call(lib.rkv_quant_store, stream, *args, k_new.shape[1], _ptr(start), _ptr(count), ctypes.byref(full))
+        self._call(lib.rkv_quant_store, stream, k, k_seq, k_tok, v, v_seq, v_tok, n_tok, self._seq(start),
+                   self._seq(count), self._cache(full))
 
     def quant_full_attention(self, q, full: RkvQuantCache, out, active=None, max_len_hint=0, keep_logits=True, stream=None):
         """Attention over an 8-bit cache.  keep_logits: leave what score_keys / select_topk need in the workspace."""
-        self._q_shape(q, out)
-        self._per_seq(active)
-        self._on_device(full, q, out, active)
-        self._call(lib.rkv_quant_full_attention, stream, _ptr(q), ctypes.byref(full), _ptr(active), _ptr(out),
-                    1 if keep_logits else 0, max_len_hint)
+        self._call(lib.rkv_quant_full_attention, stream, self._q(q), self._cache(full), self._seq(active), self._q(out),
+                   1 if keep_logits else 0, max_len_hint)
 
     def quant_full_step(self, q, full: RkvQuantCache, k_small, k_max, out, topk_idx, active=None, scores=None,
                         q_last_full=None, max_len_hint=0, stream=None):
-        stride = scores.shape[-1] if scores is not None else 0
-        self._q_shape(q, out, q_last_full)
-        self._per_seq(k_small, active)
-        self._on_device(full, q, out, k_small, topk_idx, active, scores, q_last_full)
-        self._call(lib.rkv_quant_full_step, stream, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
-                    _ptr(out), _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full), max_len_hint)
+        at, stride = self._scores(scores)
+        self._call(lib.rkv_quant_full_step, stream, self._q(q), self._cache(full), self._seq(k_small), k_max,
+                   self._seq(active), self._q(out), at, stride, self._idx(topk_idx, k_max), self._q(q_last_full), max_len_hint)
 
     def quant_gather_small(self, topk_idx, k_small, k_max, full: RkvQuantCache, small: RkvCache, active=None, stream=None):
         """Rebuild of the bf16 small cache from the selected positions of an 8-bit full cache."""
-        if topk_idx.dtype != torch.int32 or topk_idx.numel() != self.cfg.n_seq * self.cfg.n_kv_heads * k_max:
-            raise ValueError("topk_idx is an int32 tensor [B, Hkv, k_max]")
-        self._per_seq(k_small, active)
-        self._on_device(full, topk_idx, k_small, active)
-        self._call(lib.rkv_quant_gather_small, stream, _ptr(topk_idx), _ptr(k_small), k_max, ctypes.byref(full),
-                    ctypes.byref(small), _ptr(active))
+        self._call(lib.rkv_quant_gather_small, stream, self._idx(topk_idx, k_max), self._seq(k_small), k_max,
+                   self._cache(full), ctypes.byref(small), self._seq(active))
 
     def rope(self, qkv, pos, table: RopeTable, q, k, v=None, stream=None):
         """Split the fused projection's rows [T, (Hq + 2 Hkv) * 128] (bfloat16 or float32; tokens may be strided) into
         q [T, Hq, 128] and k, v [T, Hkv, 128] (bfloat16), queries and keys turned by their positions.  pos: int32 [T].
         v=None: the values are not copied."""
-        nq, nkv, n = self.cfg.n_q_heads, self.cfg.n_kv_heads, qkv.shape[0]
-        if qkv.dtype not in (torch.bfloat16, torch.float32) or qkv.dim() != 2 or qkv.shape[1] != (nq + 2 * nkv) * 128 or n < 1:
+        n, width = qkv.shape if qkv.dim() == 2 else (0, 0)
+        n_q, n_kv, dtype = self.cfg.n_q_heads, self.cfg.n_kv_heads, qkv.dtype
+        if dtype not in (torch.bfloat16, torch.float32) or width != (n_q + 2 * n_kv) * 128 or n < 1:
             raise ValueError("qkv is a bfloat16 or float32 tensor [T, (Hq + 2 Hkv) * 128]")
-        if pos.dtype != torch.int32 or pos.numel() != n:
-            raise ValueError("pos is an int32 tensor [T]")
-        for t, heads in ((q, nq), (k, nkv), (v, nkv)):
-            if t is not None and (t.dtype != torch.bfloat16 or t.numel() != n * heads * 128):
-                raise ValueError("q, k and v are bfloat16 tensors [T, heads, 128]")
-        if any(t is not None and t.device.index != self.device for t in (qkv, pos, table.freqs, q, k, v)):
-            raise ValueError("a tensor is on another device than the context")
-        stride = qkv.stride(0) if n > 1 else 0
-        if qkv.stride(1) != 1 or stride * qkv.element_size() % 16 or qkv.data_ptr() % 16:
+        if qkv.get_device() != self.device or table.freqs.get_device() != self.device:
+            raise ValueError("qkv or the table is on another device than the context")
+        tok, one = qkv.stride()
+        tok = tok if n > 1 else 0
+        at = qkv.data_ptr()
+        if one != 1 or tok % (8 if dtype is torch.bfloat16 else 4) or at % 16:
             raise ValueError("the projection's rows are contiguous and start on 16-byte boundaries")
-        self._call(lib.rkv_rope, stream, qkv.data_ptr(), 1 if qkv.dtype == torch.bfloat16 else 0, stride, _ptr(pos), n,
-                    _ptr(table.freqs), table.rot_dim, table.layout, table.amplitude, _ptr(q), _ptr(k), _ptr(v))
+        self._call(lib.rkv_rope, stream, at, 1 if dtype is torch.bfloat16 else 0, tok, self._arg(pos, torch.int32, n, "pos [T]"),
+                   n, table.freqs.data_ptr(), table.rot_dim, table.layout, table.amplitude,
+                   self._arg(q, torch.bfloat16, n * n_q * 128, "q [T, Hq, 128]"),
+                   self._arg(k, torch.bfloat16, n * n_kv * 128, "k [T, Hkv, 128]"),
+                   self._arg(v, torch.bfloat16, n * n_kv * 128, "v [T, Hkv, 128]"))
 
     def should_refresh(self, q_now, q_last_full, threshold, flag, sim=None, keep=None, stream=None):
         self._check(lib.rkv_should_refresh(self._h, _ptr(q_now), _ptr(q_last_full), float(threshold), _ptr(flag),

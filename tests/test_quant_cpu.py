@@ -53,6 +53,7 @@ def _fake(n_seq=2, n_q=8, n_kv=2):
     c = object.__new__(rkv.Context)
     c.cfg = rkv.RkvConfig(n_seq, n_q, n_kv, 128, 256, 64, 0, 1, 0.0)
     c.device, c._h = 0, None
+    c.cfg_n_seq, c.q_numel = n_seq, n_seq * n_q * 128
     return rkv, c
 
 

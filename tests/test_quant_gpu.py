@@ -584,7 +584,7 @@ def test_select_completes_the_pass_it_belongs_to(mods):
     with pytest.raises(rkv.RkvError):
         ctx.quant_full_attention(q, cs, out, max_len_hint=513)
     with pytest.raises(rkv.RkvError):
-        ctx.quant_full_step(q, cs, k_small, 65, out, idx)
+        ctx.quant_full_step(q, cs, k_small, 65, out, torch.empty((1, 2, 65), dtype=torch.int32, device="cuda"))
     odd = torch.empty(q.numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(q.shape)
     with pytest.raises(rkv.RkvError):                   # not on a 16-byte boundary
         ctx.quant_full_attention(odd, cs, out)
