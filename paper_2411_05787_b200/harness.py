@@ -104,10 +104,18 @@ class LlamaShape:
 
 
 class LlamaDecoder:
-    """Weights, caches and the per-token call sequence.  Batch 1."""
+    """Weights, caches and the per-token call sequence.  Batch 1.
+
+    cache_bits: 16 (bf16 full caches) or 8 (rkv_quant_cache: e4m3 with a scale per 64 positions and KV head).
+    rope_scaling: None (the loop's own unscaled rotation) or the arguments of rkv.RopeTable beside the shape's theta,
+    e.g. dict(scaling="bands", factor=8.0) - prompt and tokens are then rotated by rkv_rope."""
 
     def __init__(self, shape: LlamaShape, prompt_len: int, max_new: int, k_small: int, qc_stride: int,
-                 threshold: float, seed: int = 5, device="cuda"):
+                 threshold: float, seed: int = 5, device="cuda", cache_bits: int = 16, rope_scaling: dict | None = None):
+        if cache_bits not in (8, 16):
+            raise ValueError("cache_bits is 8 or 16")
+        self.cache_bits = cache_bits
+        self.table = None if rope_scaling is None else rkv.RopeTable(128, shape.theta, device=device, **rope_scaling)
         self.s, self.dev = shape, torch.device(device)
         self.prompt_len, self.max_new, self.k_small = prompt_len, max_new, k_small
         self.qc, self.threshold = qc_stride, threshold
@@ -136,8 +144,11 @@ class LlamaDecoder:
         self.ctx = rkv.Context(1, s.n_q, s.n_kv, cap, self.small_hint)
         self.states = []
         for _ in range(s.n_layers):
-            cache = synth.alloc_cache([cap], [0], s.n_kv, dev, fill=0.0)
-            self.states.append(runner.LayerState(self.ctx, cache, [k_small], small_extra, s.n_q, s.n_kv))
+            if cache_bits == 8:
+                cache, state = synth.alloc_quant_cache([cap], s.n_kv, dev), runner.QuantLayerState
+            else:
+                cache, state = synth.alloc_cache([cap], [0], s.n_kv, dev, fill=0.0), runner.LayerState
+            self.states.append(state(self.ctx, cache, [k_small], small_extra, s.n_q, s.n_kv))
         f32 = dict(dtype=torch.float32, device=dev)
         self.x, self.h = torch.zeros(s.hidden, **f32), torch.zeros(s.hidden, **f32)
         self.qkv = torch.zeros((s.n_q + 2 * s.n_kv) * 128, **f32)
@@ -171,14 +182,22 @@ class LlamaDecoder:
         for l, wl in enumerate(self.layers_w):
             h = F.rms_norm(x.float(), (s.hidden,), wl["norm1"].float(), eps=s.eps).to(torch.bfloat16)
             qkv = h @ wl["wqkv"].t()
-            q = rot(qkv[:, : s.n_q * 128].float().view(L, s.n_q, 128)).to(torch.bfloat16)
-            k = rot(qkv[:, s.n_q * 128: (s.n_q + s.n_kv) * 128].float().view(L, s.n_kv, 128)).to(torch.bfloat16)
             v = qkv[:, (s.n_q + s.n_kv) * 128:].view(L, s.n_kv, 128)
+            if self.table is not None:
+                q, k = torch.empty((L, s.n_q, 128), dtype=torch.bfloat16, device=self.dev), torch.empty_like(v)
+                self.ctx.rope(qkv, torch.arange(L, dtype=torch.int32, device=self.dev), self.table, q, k)
+            else:
+                q = rot(qkv[:, : s.n_q * 128].float().view(L, s.n_q, 128)).to(torch.bfloat16)
+                k = rot(qkv[:, s.n_q * 128: (s.n_q + s.n_kv) * 128].float().view(L, s.n_kv, 128)).to(torch.bfloat16)
             cache = self.states[l].full
-            cap = int(cache.cap[0])
-            cache.k.view(s.n_kv, cap, 128)[:, :L] = k.transpose(0, 1)
-            cache.v.view(s.n_kv, cap, 128)[:, :L] = v.transpose(0, 1)
-            cache.len.fill_(L)
+            if self.cache_bits == 8:
+                cache.len.zero_()
+                self.states[l].store_prompt(k[None], v[None])
+            else:
+                cap = int(cache.cap[0])
+                cache.k.view(s.n_kv, cap, 128)[:, :L] = k.transpose(0, 1)
+                cache.v.view(s.n_kv, cap, 128)[:, :L] = v.transpose(0, 1)
+                cache.len.fill_(L)
             att = F.scaled_dot_product_attention(q.transpose(0, 1)[None], k.transpose(0, 1)[None], v.transpose(0, 1)[None],
                                                  is_causal=True, enable_gqa=True)[0]            # [Hq, L, 128]
             x = x + att.transpose(0, 1).reshape(L, s.n_q * 128) @ wl["wo"].t()
@@ -224,7 +243,11 @@ class LlamaDecoder:
         for l, wl in enumerate(self.layers_w):
             if with_harness:
                 gemv(wl["wqkv"], self.x, self.qkv, norm_w=wl["norm1"], eps=s.eps)        # RMSNorm fused into the read of x
-                rope_split(self.qkv, self.states[l].full.len, s.theta, self.q[l], self.k[l], self.v[l], s.n_q, s.n_kv)
+                pos = self.states[l].full.len
+                if self.table is not None:
+                    self.ctx.rope(self.qkv[None], pos, self.table, self.q[l], self.k[l], self.v[l])
+                else:
+                    rope_split(self.qkv, pos, s.theta, self.q[l], self.k[l], self.v[l], s.n_q, s.n_kv)
             out = self.attention(l, kind) if with_attention else self.states[l].out
             if with_harness:
                 gemv(wl["wo"], out.view(-1), self.x, residual=self.x)
