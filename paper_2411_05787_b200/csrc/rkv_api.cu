@@ -314,12 +314,13 @@ rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cach
   p.max_len = n_max;
   p.spec = (active == nullptr && ctx->cfg.n_seq == 1) ? 1 : 0;
   // as in the bf16 pass: one tile ahead of the wait behind the short merge kernel, the whole ring behind others
-  if (p.spec != 0 && ctx->early_read && rkv::early_read_safe(st, cache)) p.early = rkv::last_launch_was_fold(st) ? 1 : rkv::kStages;
+  if (p.spec != 0 && ctx->early_read && rkv::early_read_safe(st, cache)) p.early = rkv::last_launch_was_fold(st) ? 1 : 2;
   p.scale = ctx->cfg.softmax_scale;
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_ATTN_FULL);
-    e = rkv::launch_quant_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, st);
+    const bool one_wave = (int64_t)gx * ctx->cfg.n_kv_heads * ctx->cfg.n_seq <= 2 * ctx->sm_count;
+    e = rkv::launch_quant_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, one_wave, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit attention launch");
   ctx->launches += 1;

@@ -150,7 +150,7 @@ struct QuantAttnParams {
 };
 
 cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                                   int n_seq, int grid_x, bool cluster, cudaStream_t st);
+                                   int n_seq, int grid_x, bool cluster, bool one_wave, cudaStream_t st);
 cudaError_t launch_quant_store(const QuantNew& rows, const int32_t* start, const int32_t* count, const QuantDev& c,
                                int n_seq, int n_kv_heads, int32_t* tickets, int32_t* status, cudaStream_t st);
 cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small, int k_max, const QuantDev& full,

@@ -6,10 +6,13 @@
 // pass and the selection behind it are the same kernels.
 //
 // What bounds it: 256 bytes per position and KV head from HBM, half of the bf16 pass.  The shape is that pass's: one
-// CTA per (sequence, KV head, split), two to an SM, a copy warp that keeps a ring of three 32 KB stages full (one
+// CTA per (sequence, KV head, split), two to an SM, a copy warp that keeps a ring of two 32 KB stages full (one
 // tensor-map copy of 128 positions for K and one for V per stage: a copy instruction costs its warp about 100 cycles,
-// so tiles are as many bytes as there), four MMA warps with 32 positions of a tile each, i.e. half a block, so that a
-// scale is one number per warp and tile.
+// so tiles are as many bytes as there; two stages put 19 MB in flight over the GPU, three 28 MB, which HBM serves more
+// slowly: 46.2 against 42.9 us at 131072 positions of eight heads), four MMA warps with 32 positions of a tile each,
+// i.e. half a block, so that a scale is one number per warp and tile.
+// Measured (attention alone, fold included): 131072 positions of eight heads 42.9 us, 6.26 TB/s; 32768: 14.7 us; 16
+// ragged sequences of up to 65535 positions, four heads of seven queries: 71.3 us, 5.76 TB/s; 1000: 4.1 us.
 //
 // Arithmetic.  Codes become halves exactly (cvt.e4m3x2) and the products run as m16n8k16 f16 MMAs with fp32
 // accumulators; the heads of the group are the N = 8 dimension.  fp8 MMAs would want q and p as e4m3, which is not
@@ -30,7 +33,7 @@
 namespace rkv {
 namespace {
 
-constexpr int kQStages = 3;
+constexpr int kQStages = 2;
 constexpr int kQHalfBytes = kQuantTile * kHeadDim;   // codes of K (or V) of one tile
 constexpr int kQStageBytes = 2 * kQHalfBytes;
 constexpr int kQWarps = 4;                           // MMA warps; warp kQWarps is the copy warp
@@ -48,6 +51,8 @@ constexpr int kQAt = kBarsAt + 64;
 constexpr int kQsAt = kQAt + kMaxGroup * kQRow * 2;
 constexpr int kWmAt = kQsAt + kMaxGroup * 4;
 constexpr int kQSmem = kWmAt + kQWarps * kMaxGroup * 4 + 1024;   // + alignment of the stages
+constexpr int kQSmemPair = kQSmem + 20 * 1024;       // as much as lets only two CTAs onto an SM
+static_assert(2 * (kQSmemPair + 1024) <= 228 * 1024 && 3 * (kQSmemPair + 1024) > 228 * 1024, "two CTAs per SM, no third");
 
 __device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* tm, int row, uint32_t bar,
                                                uint64_t policy) {
@@ -473,6 +478,7 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   if (kCluster) {
     // Every CTA finishes 128 / C channels of every head from its peers' shared memory; the second barrier keeps that
     // memory until the last reader is done.  (Threads that have left count as arrived.)
+    __syncwarp();
     cluster_sync_alive();
     const int c_sh = __ffs(n_cta) - 1, per_sh = 5 - c_sh;      // C = 1, 2, 4 or 8; log2 of the items per head
     const int h = tid >> per_sh, ch = (split << (7 - c_sh)) + (tid & ((1 << per_sh) - 1)) * 4;
@@ -507,6 +513,7 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + head0 + hh * kHeadDim + ch) =
           make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
     }
+    __syncwarp();
     cluster_sync_alive();
   }
 }
@@ -517,17 +524,19 @@ cudaError_t prepare_quant_attention() {
   cudaError_t e = cudaSuccess;
   for (auto kernel : {quant_attn_kernel<true, false>, quant_attn_kernel<false, false>, quant_attn_kernel<true, true>,
                       quant_attn_kernel<false, true>})
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmemPair);
   return e;
 }
 
 cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
-                                   int n_seq, int grid_x, bool cluster, cudaStream_t st) {
+                                   int n_seq, int grid_x, bool cluster, bool one_wave, cudaStream_t st) {
   const bool logits = p.logits != nullptr;
   auto kernel = cluster ? (logits ? quant_attn_kernel<true, true> : quant_attn_kernel<false, true>)
                         : (logits ? quant_attn_kernel<true, false> : quant_attn_kernel<false, false>);
-  return launch_ex(kernel, dim3(grid_x, p.n_kv_heads, n_seq), dim3(kQThreads), (size_t)kQSmem, st, cluster ? grid_x : 1,
-                   tm_k, tm_v, p);
+  // A grid that fits two to an SM must not be packed three to an SM beside idle ones (16384 positions of eight
+  // sequences: 49.3 us packed, 43.2 spread); one of several waves gains from the third (ragged batch: 74.3, 71.3 us).
+  const size_t smem = one_wave ? kQSmemPair : kQSmem;
+  return launch_ex(kernel, dim3(grid_x, p.n_kv_heads, n_seq), dim3(kQThreads), smem, st, cluster ? grid_x : 1, tm_k, tm_v, p);
 }
 
 }  // namespace rkv
