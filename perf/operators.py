@@ -324,7 +324,7 @@ def _own(s):
             s["table"] = rkv.RopeTable(case["rot"], THETA, case["layout"], case["scaling"], case["factor"],
                                        trained_len=TRAINED, low=LOW, high=HIGH, fast=FAST, slow=SLOW,
                                        device=s["qkv"].device)
-            s["ctx"] = _context(case, 1)
+            s["ctx"] = _context(dict(kv_heads=1), 1)      # (the rotation takes its heads from its tensors)
         s["ctx"].rope(s["qkv"], s["pos"], s["table"], s["q"], s["k"], s["v"])
         return
     if "cache" not in s:
