@@ -377,14 +377,15 @@ typedef struct {
 /* Host.  freqs[i] = f_i / 2 pi in turns per position, as a fraction of 2^64 (rot_dim / 2 of them); *amplitude. */
 rkv_status rkv_rope_frequencies(const rkv_rope_config* cfg /*host*/, uint64_t* freqs /*host*/, float* amplitude /*host*/);
 /* One launch for n_tok tokens (a prompt's, a chunk's, or one).
- *   qkv        [n_tok][Hq + 2 Hkv][128], bf16 (is_bf16 != 0) or fp32: queries, keys, values; 16-byte aligned, token t at
+ *   n_q, n_kv  heads of queries, and of keys and of values (any numbers >= 1; the context's configuration does not matter)
+ *   qkv        [n_tok][n_q + 2 n_kv][128], bf16 (is_bf16 != 0) or fp32: queries, keys, values; 16-byte aligned, token t at
  *              t * tok_stride elements (a multiple of 16 bytes)
  *   pos        int32 [n_tok], any value (the angle is exact for all of them)
  *   freqs      DEVICE copy of rkv_rope_frequencies' output, with its rot_dim and amplitude
- *   q          bf16 [n_tok][Hq][128];  k, v  bf16 [n_tok][Hkv][128];  v NULL: the values are not copied
- * The outputs must not overlap qkv.  Only Hq and Hkv of the context's configuration are read. */
+ *   q          bf16 [n_tok][n_q][128];  k, v  bf16 [n_tok][n_kv][128];  v NULL: the values are not copied
+ * The outputs must not overlap qkv. */
 rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_stride, const int32_t* pos,
-                    int32_t n_tok, const uint64_t* freqs, int32_t rot_dim, int32_t layout, float amplitude, void* q,
+                    int32_t n_tok, int32_t n_q, int32_t n_kv, const uint64_t* freqs, int32_t rot_dim, int32_t layout, float amplitude, void* q,
                     void* k, void* v, void* stream);
 
 /*

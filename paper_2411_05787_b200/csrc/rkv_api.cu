@@ -779,9 +779,11 @@ rkv_status rkv_rope_frequencies(const rkv_rope_config* c, uint64_t* freqs, float
 }
 
 rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_stride, const int32_t* pos,
-                    int32_t n_tok, const uint64_t* freqs, int32_t rot_dim, int32_t layout, float amplitude, void* q,
-                    void* k, void* v, void* stream) {
-  if (!ctx || !qkv || !pos || !freqs || !q || !k || n_tok < 1 || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+                    int32_t n_tok, int32_t n_q, int32_t n_kv, const uint64_t* freqs, int32_t rot_dim, int32_t layout,
+                    float amplitude, void* q, void* k, void* v, void* stream) {
+  if (!ctx || !qkv || !pos || !freqs || !q || !k || n_tok < 1 || n_q < 1 || n_kv < 1 || n_q > (1 << 16) ||
+      n_kv > (1 << 16) || !on_device(ctx))
+    return RKV_ERR_INVALID_ARG;
   if (rot_dim < 16 || rot_dim > rkv::kHeadDim || rot_dim % 16 != 0 || (layout != RKV_ROPE_HALF && layout != RKV_ROPE_INTERLEAVED))
     return RKV_ERR_UNSUPPORTED;
   if (!aligned16(qkv) || !aligned16(q) || !aligned16(k) || !aligned16(v) || (tok_stride * (is_bf16 ? 2 : 4)) % 16 != 0 ||
@@ -791,7 +793,7 @@ rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_ROPE);
-    e = rkv::launch_rope(qkv, is_bf16 != 0, tok_stride, pos, n_tok, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads, freqs,
+    e = rkv::launch_rope(qkv, is_bf16 != 0, tok_stride, pos, n_tok, n_q, n_kv, freqs,
                          rot_dim, layout == RKV_ROPE_INTERLEAVED, amplitude, q, k, v, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "rotary launch");

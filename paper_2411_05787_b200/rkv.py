@@ -120,7 +120,7 @@ def _load() -> ctypes.CDLL:
     lib.rkv_quant_gather_small.argtypes = [vp, vp, vp, i32, quantp, cachep, vp, vp]
     lib.rkv_rope_frequencies.argtypes = [ctypes.POINTER(RkvRopeConfig), ctypes.POINTER(ctypes.c_uint64),
                                          ctypes.POINTER(f32)]
-    lib.rkv_rope.argtypes = [vp, vp, i32, i64, vp, i32, vp, i32, i32, f32, vp, vp, vp, vp]
+    lib.rkv_rope.argtypes = [vp, vp, i32, i64, vp, i32, i32, i32, vp, i32, i32, f32, vp, vp, vp, vp]
     for name in ("rkv_rope_frequencies", "rkv_rope", "rkv_quant_store", "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk",
                  "rkv_quant_full_step", "rkv_quant_gather_small"):
         getattr(lib, name).restype = i32
@@ -435,9 +435,11 @@ class Context:
     def rope(self, qkv, pos, table: RopeTable, q, k, v=None, stream=None):
         """Split the fused projection's rows [T, (Hq + 2 Hkv) * 128] (bfloat16 or float32; tokens may be strided) into
         q [T, Hq, 128] and k, v [T, Hkv, 128] (bfloat16), queries and keys turned by their positions.  pos: int32 [T].
-        v=None: the values are not copied."""
+        Hq and Hkv are those of q and k, whatever the context's.  v=None: the values are not copied."""
         n, width = qkv.shape if qkv.dim() == 2 else (0, 0)
-        n_q, n_kv, dtype = self.cfg.n_q_heads, self.cfg.n_kv_heads, qkv.dtype
+        if q.dim() != 3 or k.dim() != 3:
+            raise ValueError("q is a tensor [T, Hq, 128], k and v are tensors [T, Hkv, 128]")
+        n_q, n_kv, dtype = q.shape[1], k.shape[1], qkv.dtype
         if dtype not in (torch.bfloat16, torch.float32) or width != (n_q + 2 * n_kv) * 128 or n < 1:
             raise ValueError("qkv is a bfloat16 or float32 tensor [T, (Hq + 2 Hkv) * 128]")
         if qkv.get_device() != self.device or table.freqs.get_device() != self.device:
@@ -448,7 +450,7 @@ class Context:
         if one != 1 or tok % (8 if dtype is torch.bfloat16 else 4) or at % 16:
             raise ValueError("the projection's rows are contiguous and start on 16-byte boundaries")
         self._call(lib.rkv_rope, stream, at, 1 if dtype is torch.bfloat16 else 0, tok, self._arg(pos, torch.int32, n, "pos [T]"),
-                   n, table.freqs.data_ptr(), table.rot_dim, table.layout, table.amplitude,
+                   n, n_q, n_kv, table.freqs.data_ptr(), table.rot_dim, table.layout, table.amplitude,
                    self._arg(q, torch.bfloat16, n * n_q * 128, "q [T, Hq, 128]"),
                    self._arg(k, torch.bfloat16, n * n_kv * 128, "k [T, Hkv, 128]"),
                    self._arg(v, torch.bfloat16, n * n_kv * 128, "v [T, Hkv, 128]"))

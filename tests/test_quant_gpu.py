@@ -375,6 +375,78 @@ def test_attention_flags(mods):
     assert ctx.device_status() & rkv.DEV_NONFINITE
 
 
+def test_smallest_cache(mods):
+    """One block in all: 64 rows, fewer than a tile of the pass."""
+    rkv, runner, synth = mods
+    for n in (1, 64):
+        c = filled(synth, [n], 1, n, caps=[64])
+        q = normal(gen(n), 1, 1, 128).to(torch.bfloat16)
+        ctx = context(rkv, 1, 1, 1, 64)
+        out = torch.empty_like(q)
+        ctx.quant_full_attention(q, struct(rkv, c), out)
+        check_out(out[0], reference(Host(c, 1), q, 1, [n])[0])
+        assert ctx.device_status() == 0
+
+
+def test_attention_right_behind_a_store(mods):
+    """Store and attention back to back many times: the pass must not read its first tiles before the store is done
+    (and may behind other launches)."""
+    rkv, runner, synth = mods
+    n_kv, n = 2, 300
+    c = synth.alloc_quant_cache([n + 40], n_kv, torch.device("cuda"))
+    ctx = context(rkv, 1, 8, n_kv, n + 64)
+    cs = struct(rkv, c)
+    g = gen(9)
+    host = Host(c, n_kv)
+    x = normal(g, 1, n, n_kv, 128).to(torch.bfloat16)
+    ctx.quant_store(x, x, cs)
+    host.store(x, x)
+    qs, outs, news = [], [], []
+    for i in range(20):
+        q, k = normal(g, 1, 8, 128).to(torch.bfloat16), (normal(g, 1, 1, n_kv, 128) * 3).to(torch.bfloat16)
+        qs.append(q); news.append(k); outs.append((torch.empty_like(q), torch.empty_like(q)))
+    torch.cuda.synchronize()
+    for q, k, (a, b) in zip(qs, news, outs):
+        ctx.quant_store(k, k, cs)
+        ctx.quant_full_attention(q, cs, a)
+        ctx.quant_full_attention(q, cs, b)
+    for q, k, (a, b) in zip(qs, news, outs):
+        host.store(k, k)
+        ref = reference(host, q, n_kv, host.len)
+        check_out(a[0], ref[0])
+        assert torch.equal(a, b)
+    host.check()
+    assert ctx.device_status() == 0
+
+
+def test_selection_after_scores_without_one(mods):
+    """A captured graph of attention and scores alone, replayed between full steps, leaves the full steps' selections
+    as they are (the keys' histogram starts from zero in every pass)."""
+    rkv, runner, synth = mods
+    c = filled(synth, [5000], 2, 3)
+    q = normal(gen(3), 1, 8, 128).to(torch.bfloat16)
+    ctx = context(rkv, 1, 8, 2, 5120, 300)
+    cs = struct(rkv, c)
+    out, idx = torch.empty_like(q), torch.empty((1, 2, 300), dtype=torch.int32, device="cuda")
+    scores = torch.zeros((1, 2, 5120), device="cuda")
+    k_small = i32([300])
+    ctx.quant_full_step(q, cs, k_small, 300, out, idx)
+    want = idx.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            ctx.quant_full_attention(q, cs, out)
+            ctx.score_keys(q, cs, k_small, 300, scores=scores)
+        for _ in range(3):
+            graph.replay()
+            idx.fill_(-7)
+            ctx.quant_full_step(q, cs, k_small, 300, out, idx)
+            assert torch.equal(idx, want)
+    assert ctx.device_status(side) == 0
+
+
 # -------------------------------------------------------------------------------------------------------------- rebuild
 @pytest.mark.parametrize("keep", [1, 63, 64, 65, 200, 1000])
 def test_rebuild_bit_exact(mods, keep):

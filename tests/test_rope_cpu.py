@@ -62,7 +62,7 @@ def test_unknown_names_are_refused(rkv):
     with pytest.raises(ValueError):
         rkv.RopeTable(scaling="other", device="cpu")
     assert rkv.lib.rkv_rope_frequencies(None, None, None) == 1
-    assert rkv.lib.rkv_rope(None, None, 1, 0, None, 1, None, 128, 0, 1.0, None, None, None, None) == 1
+    assert rkv.lib.rkv_rope(None, None, 1, 0, None, 1, 1, 1, None, 128, 0, 1.0, None, None, None, None) == 1
 
 
 def test_call_refusals(rkv):

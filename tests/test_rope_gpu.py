@@ -30,7 +30,7 @@ def make(rkv, n, nq, nkv, dtype, seed, pad=0):
     g.manual_seed(seed)
     x = torch.randn((n, (nq + 2 * nkv) * 128 + pad), generator=g, device="cuda").to(dtype)[:, : (nq + 2 * nkv) * 128]
     out = [torch.full((n + 1, h, 128), 7.0, dtype=torch.bfloat16, device="cuda") for h in (nq, nkv, nkv)]
-    return rkv.Context(1, nq, nkv, 64, 64), x, out
+    return rkv.Context(1, 1, 1, 64, 64), x, out     # (the heads are the tensors')
 
 
 def check(x, pos, outs, nq, nkv, f, amp, layout):
@@ -64,6 +64,15 @@ def test_rope(rkv, n, rot, layout, dtype):
     if dtype == torch.bfloat16:
         assert torch.equal(v[:n].reshape(n, -1), x[:, (nq + nkv) * 128:])
     assert ctx.device_status() == 0
+
+
+def test_rope_any_heads(rkv):
+    for nq, nkv in ((28, 8), (32, 1), (1, 3)):
+        ctx, x, (q, k, v) = make(rkv, 6, nq, nkv, torch.bfloat16, nq)
+        pos = torch.arange(6, dtype=torch.int32, device="cuda") + 5000
+        ctx.rope(x, pos, rkv.RopeTable(80, 10000.0), q[:6], k[:6], v[:6])
+        f, amp = QO.rope_frequencies(80, 10000.0)
+        check(x, pos.cpu().numpy(), (q, k, v), nq, nkv, f, amp, "half")
 
 
 @pytest.mark.parametrize("kw", [dict(scaling="linear", factor=4.0), dict(scaling="bands", factor=8.0),
