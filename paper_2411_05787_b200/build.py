@@ -1,17 +1,21 @@
 """Builds the C-ABI CUDA libraries in-tree with nvcc for sm_100a:
-librkv.so (the RefreshKV attention path) and libllama_harness.so (the decoder kernels of the end-to-end workload)."""
+librkv.so (the RefreshKV attention path) and libllama_harness.so (the decoder kernels of the end-to-end workload);
+and, with the host compiler, _rkv_calls.so (the binding's checked calls, linked to librkv.so beside it)."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "librkv.so")
 HARNESS_LIB = os.path.join(PKG, "libllama_harness.so")
 TARGETS = {LIB: "csrc", HARNESS_LIB: "csrc_harness"}
+CALLS_LIB = os.path.join(PKG, "_rkv_calls.so")
+CALLS_SRC = os.path.join(PKG, "csrc_py", "rkv_calls.c")
 
 
 def sources(sub: str = "csrc") -> list:
@@ -43,11 +47,27 @@ def _compile(lib: str, verbose: bool) -> None:
         sys.stderr.write(r.stdout + r.stderr)
 
 
+def calls_need_build() -> bool:
+    return not os.path.exists(CALLS_LIB) or any(
+        os.path.getmtime(d) > os.path.getmtime(CALLS_LIB) for d in [CALLS_SRC] + glob.glob(os.path.join(ROOT, "include", "*.h")))
+
+
+def _compile_calls() -> None:
+    cmd = [os.environ.get("CC", "gcc"), "-std=c11", "-O2", "-Wall", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
+           "-I", sysconfig.get_paths()["include"], "-o", CALLS_LIB, CALLS_SRC, "-L", PKG, "-l:librkv.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("the host compiler failed:\n" + r.stdout + r.stderr)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ and csrc_harness/ into their shared libraries; returns librkv's path."""
+    """Compile every .cu under csrc/ and csrc_harness/ into their shared libraries, and the binding's extension;
+    returns librkv's path."""
     for lib in TARGETS:
         if force or needs_build(lib):
             _compile(lib, verbose)
+    if force or calls_need_build():
+        _compile_calls()
     return LIB
 
 

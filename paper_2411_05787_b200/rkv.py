@@ -131,6 +131,11 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+try:
+    from . import _rkv_calls as _calls     # links the librkv.so loaded above
+except ImportError as e:
+    raise ImportError(f"the binding's extension cannot be loaded ({e}): build it first "
+                      "(python -m paper_2411_05787_b200.build)") from e
 
 
 class RkvError(RuntimeError):
@@ -150,7 +155,6 @@ def _ptr(t):
     return t.data_ptr()
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream    # cudaStream_t of a device's current stream
 _current_device = torch._C._cuda_getDevice
 
 
@@ -216,6 +220,11 @@ class RopeTable:
         self.freqs = torch.tensor(signed, dtype=torch.int64).to(device)
 
 
+# what the extension's checks compare with; the last: cudaStream_t of a device's current stream
+_calls.setup(torch.bfloat16, torch.float32, torch.int32, RkvQuantCache, RkvCache, RopeTable,
+             torch._C._cuda_getCurrentRawStream)
+
+
 def small_step_noalloc(cfg: RkvConfig, q, small: RkvCache, out, active=None, max_len_hint=0, device_status=None,
                        stream=None):
     """Partial step for callers that may not allocate device memory (no context; see include/rkv.h).
@@ -241,12 +250,13 @@ class Context:
             raise RkvError(rc)
         self._h = handle
         self.device = torch.cuda.current_device()
-        self.cfg_n_seq, self.q_numel = n_seq, n_seq * n_q_heads * 128
+        self._key = (handle.value, n_seq, n_q_heads, n_kv_heads, self.device)     # what _rkv_calls knows of the context
 
     def close(self):
         if getattr(self, "_h", None):
             lib.rkv_destroy(self._h)
             self._h = None
+            self._key = (0,) + self._key[1:]
 
     def __del__(self):
         try:
@@ -290,22 +300,22 @@ class Context:
 
     def select_topk(self, q, full: RkvCache | RkvQuantCache, k_small, k_max, topk_idx, active=None, scores=None,
                     q_last_full=None, stream=None):
-        stride = scores.shape[-1] if scores is not None else 0
         if isinstance(full, RkvQuantCache):
-            at, stride = self._scores(scores)
-            return self._call(lib.rkv_quant_select_topk, stream, self._q(q), self._cache(full), self._seq(k_small), k_max,
-                              self._seq(active), at, stride, self._idx(topk_idx, k_max), self._q(q_last_full))
+            args = (self._key, q, full, k_small, k_max, topk_idx, active, scores, q_last_full, stream)
+            return self._done(_calls.quant_select_topk(*args), _calls.quant_select_topk, *args)
+        stride = scores.shape[-1] if scores is not None else 0
         self._check(lib.rkv_select_topk(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                                         _ptr(scores), stride, _ptr(topk_idx), _ptr(q_last_full), _stream(stream)))
 
     def score_keys(self, q, full: RkvCache | RkvQuantCache, k_small, k_max, active=None, scores=None, q_last_full=None,
                    stream=None):
         """The score pass alone; the next select_topk (scores=None, q_last_full=None) launches the selection alone."""
-        stride = scores.shape[-1] if scores is not None else 0
         if isinstance(full, RkvQuantCache):
-            at, stride = self._scores(scores)
-            return self._call(lib.rkv_quant_score_keys, stream, self._q(q), self._cache(full), self._seq(k_small), k_max,
-                              self._seq(active), at, stride, self._q(q_last_full))
+            rc = _calls.quant_score_keys(self._key, q, full, k_small, k_max, active, scores, q_last_full, stream)
+            if rc:
+                self._done(rc, _calls.quant_score_keys, self._key, q, full, k_small, k_max, active, scores, q_last_full, stream)
+            return
+        stride = scores.shape[-1] if scores is not None else 0
         self._check(lib.rkv_score_keys(self._h, _ptr(q), ctypes.byref(full), _ptr(k_small), k_max, _ptr(active),
                                        _ptr(scores), stride, _ptr(q_last_full), _stream(stream)))
 
@@ -343,117 +353,48 @@ class Context:
                                                     max_len_hint, _stream(stream)))
 
     # ------------------------------------------------------------------ the full cache in 8 bits, rotary positions
-    # These calls run in decode loops, where the host's time per launch counts: the checks use the tensors' cheapest
-    # accessors, each once.
-    def _call(self, fn, stream, *args):
-        """One call on the context's device, whichever is current, and on its current stream unless one is given."""
-        stream = _raw_stream(self.device) if stream is None else _stream(stream)
-        if _current_device() == self.device:
-            rc = fn(self._h, *args, stream)
-        else:
+    # These calls run in decode loops, where the host's time per launch counts: _rkv_calls checks their arguments
+    # (ValueError for what does not fit) and calls the library with them.
+    def _done(self, rc, call, *args):
+        """rc of call(*args).  The library refuses to launch unless the context's device is current: then once more there."""
+        if rc == RKV_OK:
+            return
+        if self._key[0] and _current_device() != self.device:
             with torch.cuda.device(self.device):
-                rc = fn(self._h, *args, stream)
-        if rc != RKV_OK:
-            self._check(rc)
-
-    def _cache(self, full):
-        if full.device != self.device:
-            raise ValueError("the cache is on another device than the context")
-        if full.n_seq != self.cfg_n_seq:
-            raise ValueError("the cache holds another number of sequences than the context")
-        return ctypes.byref(full)
-
-    def _arg(self, t, dtype, numel, what):
-        """Device pointer of a contiguous tensor of this context's device (None: NULL)."""
-        if t is None:
-            return None
-        if t.dtype is not dtype or t.numel() != numel:
-            raise ValueError(f"{what}: {dtype} with {numel} elements expected, {t.dtype} with {t.numel()} given")
-        if t.get_device() != self.device:
-            raise ValueError(f"{what} is on another device than the context")
-        if not t.is_contiguous():
-            raise ValueError("librkv takes contiguous tensors")
-        return t.data_ptr()
-
-    def _q(self, t):
-        return self._arg(t, torch.bfloat16, self.q_numel, "queries and outputs [B, Hq, 128]")
-
-    def _seq(self, t):
-        return self._arg(t, torch.int32, self.cfg_n_seq, "a per-sequence argument")
-
-    def _idx(self, t, k_max):
-        return self._arg(t, torch.int32, self.cfg_n_seq * self.cfg.n_kv_heads * k_max, "topk_idx [B, Hkv, k_max]")
-
-    def _scores(self, t):
-        if t is None:
-            return None, 0
-        stride = t.shape[-1]
-        return self._arg(t, torch.float32, self.cfg_n_seq * self.cfg.n_kv_heads * stride, "scores [B, Hkv, stride]"), stride
-
-    def _new_rows(self, x, what):
-        n_seq, n_tok, n_kv, dim = x.shape if x.dim() == 4 else (0, 0, 0, 0)
-        if x.dtype is not torch.bfloat16 or n_seq != self.cfg_n_seq or n_kv != self.cfg.n_kv_heads or dim != 128 or n_tok < 1:
-            raise ValueError(f"{what} is a bfloat16 tensor [B, T, Hkv, 128]")
-        if x.get_device() != self.device:
-            raise ValueError(f"{what} is on another device than the context")
-        seq, tok, head, one = x.stride()
-        if one != 1 or (head != 128 and n_kv > 1):
-            raise ValueError("the heads of a new row lie side by side")
-        seq = seq if n_seq > 1 else 0       # (a stride that is never taken may have any value)
-        tok = tok if n_tok > 1 else 0
-        at = x.data_ptr()
-        if seq % 8 or tok % 8 or at % 16:
-            raise ValueError("new rows start on 16-byte boundaries")
-        return at, seq, tok, n_tok
+                rc = call(*args)
+        self._check(rc)
 
     def quant_store(self, k_new, v_new, full: RkvQuantCache, start=None, count=None, stream=None):
         """Append rows to an 8-bit cache.  k_new, v_new: bfloat16 [B, T, Hkv, 128]; sequences and tokens may be strided
         (a slice of a projection's output), the heads of a token lie side by side.  start, count: int32 [B] or None."""
-        k, k_seq, k_tok, n_tok = self._new_rows(k_new, "k_new")
-        v, v_seq, v_tok, n_tok_v = self._new_rows(v_new, "v_new")
-        if n_tok != n_tok_v:
-            raise ValueError("k_new and v_new hold the same number of rows")
-        self._call(lib.rkv_quant_store, stream, k, k_seq, k_tok, v, v_seq, v_tok, n_tok, self._seq(start),
-                   self._seq(count), self._cache(full))
+        rc = _calls.quant_store(self._key, k_new, v_new, full, start, count, stream)
+        if rc:
+            self._done(rc, _calls.quant_store, self._key, k_new, v_new, full, start, count, stream)
 
     def quant_full_attention(self, q, full: RkvQuantCache, out, active=None, max_len_hint=0, keep_logits=True, stream=None):
         """Attention over an 8-bit cache.  keep_logits: leave what score_keys / select_topk need in the workspace."""
-        self._call(lib.rkv_quant_full_attention, stream, self._q(q), self._cache(full), self._seq(active), self._q(out),
-                   1 if keep_logits else 0, max_len_hint)
+        rc = _calls.quant_full_attention(self._key, q, full, out, active, max_len_hint, keep_logits, stream)
+        if rc:
+            self._done(rc, _calls.quant_full_attention, self._key, q, full, out, active, max_len_hint, keep_logits, stream)
 
     def quant_full_step(self, q, full: RkvQuantCache, k_small, k_max, out, topk_idx, active=None, scores=None,
                         q_last_full=None, max_len_hint=0, stream=None):
-        at, stride = self._scores(scores)
-        self._call(lib.rkv_quant_full_step, stream, self._q(q), self._cache(full), self._seq(k_small), k_max,
-                   self._seq(active), self._q(out), at, stride, self._idx(topk_idx, k_max), self._q(q_last_full), max_len_hint)
+        args = (self._key, q, full, k_small, k_max, out, topk_idx, active, scores, q_last_full, max_len_hint, stream)
+        self._done(_calls.quant_full_step(*args), _calls.quant_full_step, *args)
 
     def quant_gather_small(self, topk_idx, k_small, k_max, full: RkvQuantCache, small: RkvCache, active=None, stream=None):
         """Rebuild of the bf16 small cache from the selected positions of an 8-bit full cache."""
-        self._call(lib.rkv_quant_gather_small, stream, self._idx(topk_idx, k_max), self._seq(k_small), k_max,
-                   self._cache(full), ctypes.byref(small), self._seq(active))
+        rc = _calls.quant_gather_small(self._key, topk_idx, k_small, k_max, full, small, active, stream)
+        if rc:
+            self._done(rc, _calls.quant_gather_small, self._key, topk_idx, k_small, k_max, full, small, active, stream)
 
     def rope(self, qkv, pos, table: RopeTable, q, k, v=None, stream=None):
         """Split the fused projection's rows [T, (Hq + 2 Hkv) * 128] (bfloat16 or float32; tokens may be strided) into
         q [T, Hq, 128] and k, v [T, Hkv, 128] (bfloat16), queries and keys turned by their positions.  pos: int32 [T].
         Hq and Hkv are those of q and k, whatever the context's.  v=None: the values are not copied."""
-        n, width = qkv.shape if qkv.dim() == 2 else (0, 0)
-        if q.dim() != 3 or k.dim() != 3:
-            raise ValueError("q is a tensor [T, Hq, 128], k and v are tensors [T, Hkv, 128]")
-        n_q, n_kv, dtype = q.shape[1], k.shape[1], qkv.dtype
-        if dtype not in (torch.bfloat16, torch.float32) or width != (n_q + 2 * n_kv) * 128 or n < 1:
-            raise ValueError("qkv is a bfloat16 or float32 tensor [T, (Hq + 2 Hkv) * 128]")
-        if qkv.get_device() != self.device or table.freqs.get_device() != self.device:
-            raise ValueError("qkv or the table is on another device than the context")
-        tok, one = qkv.stride()
-        tok = tok if n > 1 else 0
-        at = qkv.data_ptr()
-        if one != 1 or tok % (8 if dtype is torch.bfloat16 else 4) or at % 16:
-            raise ValueError("the projection's rows are contiguous and start on 16-byte boundaries")
-        self._call(lib.rkv_rope, stream, at, 1 if dtype is torch.bfloat16 else 0, tok, self._arg(pos, torch.int32, n, "pos [T]"),
-                   n, n_q, n_kv, table.freqs.data_ptr(), table.rot_dim, table.layout, table.amplitude,
-                   self._arg(q, torch.bfloat16, n * n_q * 128, "q [T, Hq, 128]"),
-                   self._arg(k, torch.bfloat16, n * n_kv * 128, "k [T, Hkv, 128]"),
-                   self._arg(v, torch.bfloat16, n * n_kv * 128, "v [T, Hkv, 128]"))
+        rc = _calls.rope(self._key, qkv, pos, table, q, k, v, stream)
+        if rc:
+            self._done(rc, _calls.rope, self._key, qkv, pos, table, q, k, v, stream)
 
     def should_refresh(self, q_now, q_last_full, threshold, flag, sim=None, keep=None, stream=None):
         self._check(lib.rkv_should_refresh(self._h, _ptr(q_now), _ptr(q_last_full), float(threshold), _ptr(flag),

@@ -52,8 +52,7 @@ def _fake(n_seq=2, n_q=8, n_kv=2):
     from paper_2411_05787_b200 import rkv
     c = object.__new__(rkv.Context)
     c.cfg = rkv.RkvConfig(n_seq, n_q, n_kv, 128, 256, 64, 0, 1, 0.0)
-    c.device, c._h = 0, None
-    c.cfg_n_seq, c.q_numel = n_seq, n_seq * n_q * 128
+    c.device, c._h, c._key = 0, None, (0, n_seq, n_q, n_kv, 0)
     return rkv, c
 
 
@@ -126,6 +125,29 @@ def test_attention_and_rebuild_refuse():
         ctx.quant_full_attention(q, _cache(rkv, n_seq=3), q)
     idx = torch.zeros((2, 2, 4), dtype=torch.int32)
     with pytest.raises(ValueError):
-        ctx.quant_gather_small(idx, torch.zeros(2, dtype=torch.int32), 5, _cache(rkv), None)
+        ctx.quant_gather_small(idx, torch.zeros(2, dtype=torch.int32), 5, _cache(rkv), rkv.RkvCache())
     with pytest.raises(ValueError):
-        ctx.quant_gather_small(idx.long(), torch.zeros(2, dtype=torch.int32), 4, _cache(rkv), None)
+        ctx.quant_gather_small(idx.long(), torch.zeros(2, dtype=torch.int32), 4, _cache(rkv), rkv.RkvCache())
+
+
+def test_extension_refuses_wrong_kinds():
+    """What is no tensor, no cache of the right class, no context's key."""
+    rkv, ctx = _fake()
+    q = torch.zeros((2, 8, 128), dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        ctx.quant_full_attention(q, rkv.RkvCache(), q)
+    with pytest.raises(TypeError):
+        ctx.quant_gather_small(torch.zeros((2, 2, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), 4, _cache(rkv), _cache(rkv))
+    with pytest.raises(ValueError):
+        ctx.quant_full_attention(None, _cache(rkv), q)
+    with pytest.raises(AttributeError):
+        ctx.quant_full_attention([1, 2], _cache(rkv), q)
+    with pytest.raises(TypeError):
+        rkv._calls.quant_store(ctx._key)
+    with pytest.raises(TypeError):
+        rkv._calls.quant_store((0, 1), q, q, _cache(rkv), None, None, None)
+    idx, ks = torch.zeros((2, 2, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(TypeError):
+        ctx.quant_gather_small(idx, ks, "4", _cache(rkv), rkv.RkvCache())
+    with pytest.raises(ValueError):
+        ctx.quant_gather_small(idx, ks, 1 << 40, _cache(rkv), rkv.RkvCache())

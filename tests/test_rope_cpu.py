@@ -68,8 +68,7 @@ def test_unknown_names_are_refused(rkv):
 def test_call_refusals(rkv):
     ctx = object.__new__(rkv.Context)
     ctx.cfg = rkv.RkvConfig(1, 4, 2, 128, 256, 64, 0, 1, 0.0)
-    ctx.device, ctx._h = 0, None
-    ctx.cfg_n_seq, ctx.q_numel = 1, 4 * 128
+    ctx.device, ctx._h, ctx._key = 0, None, (0, 1, 4, 2, 0)
     table = rkv.RopeTable(device="cpu")
     bf = dict(dtype=torch.bfloat16)
     qkv, pos = torch.zeros((3, 8 * 128), **bf), torch.zeros(3, dtype=torch.int32)
