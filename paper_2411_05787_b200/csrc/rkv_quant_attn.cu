@@ -46,6 +46,9 @@ constexpr int kQCluster = 8;                         // most CTAs that finish an
 constexpr float kPBase = 8192.f;                     // 2^13: the largest p'
 static_assert(kQuantBlock % kQBand == 0, "a warp's band must not straddle two blocks");
 
+constexpr int kMergeL = kQWarps * kMaxGroup * kQOPad;          // merge buffer, in floats: o [warps][8][kQOPad],
+constexpr int kMergeM = kMergeL + kQWarps * kMaxGroup;         // l [warps][8], m [8]
+constexpr int kMergeBytes = (kMergeM + kMaxGroup) * 4;
 constexpr int kBarsAt = kQStages * kQStageBytes;
 constexpr int kQAt = kBarsAt + 64;
 constexpr int kQsAt = kQAt + kMaxGroup * kQRow * 2;
@@ -85,6 +88,241 @@ __device__ __forceinline__ float2 ld_peer2(uint32_t addr) {
   return v;
 }
 
+// State and steps of an MMA warp.  One (sequence, KV head) at a time: queries(), tile() for each of its tiles, merge().
+template <bool kLogits>
+struct Consumer {
+  uint32_t qb[8][2];              // B fragments of Q^T: [16-channel segment][k half]
+  float qs0, qs1;                 // softmax scale over the queries' powers of two, for heads qc and qc + 1
+  float m0, m1, l0, l1;           // running maximum and sum of heads qc, qc + 1
+  float vref, vrcp;               // scale of the accumulators and its reciprocal
+  float o[8][4];                  // [16-channel segment]: (channel 16 s + 2 qd, heads qc, qc + 1), (the next channel, the same heads)
+
+  __device__ __forceinline__ void reset() {
+    m0 = m1 = -INFINITY;
+    l0 = l1 = 0.f;
+    vref = 1.17549435e-38f;       // 2^-126
+    vrcp = 8.50705917e37f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  }
+
+  // qv: this thread's 16 bytes of the group's query rows (16 threads to a head; zeros for heads beyond the group)
+  __device__ __forceinline__ void queries(uint4 qv, float scale, __half* sm_q, float* sm_qs, int tid) {
+    const int h = tid >> 4, lane = tid & 31;
+    uint32_t m = __vmaxu2(__vmaxu2(qv.x & 0x7fff7fffu, qv.y & 0x7fff7fffu), __vmaxu2(qv.z & 0x7fff7fffu, qv.w & 0x7fff7fffu));
+    m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    // 2^e brings the largest magnitude into [2^14, 2^15); nothing is done for a row that is not finite or zero
+    int e = 14 - ((int)(m >> 7) - 127);
+    if (m >= 0x7f80u || m == 0u) e = 0;
+    if (e > 126) e = 126;
+    const float up = pow2f(e);
+    const uint32_t x[4] = {qv.x, qv.y, qv.z, qv.w};
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = pack_f16(__uint_as_float(x[i] << 16) * up, __uint_as_float(x[i] & 0xffff0000u) * up);
+    *reinterpret_cast<uint4*>(sm_q + h * kQRow + (tid & 15) * 8) = make_uint4(y[0], y[1], y[2], y[3]);
+    if ((tid & 15) == 0) sm_qs[h] = scale * pow2f(-e);
+    consumer_bar_n<32 * kQWarps>();
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {   // channels 16 s + 4 t .. + 3 of head qd, t = lane & 3
+      const uint2 f = *reinterpret_cast<const uint2*>(sm_q + (lane >> 2) * kQRow + 16 * s + 4 * (lane & 3));
+      qb[s][0] = f.x;
+      qb[s][1] = f.y;
+    }
+    qs0 = sm_qs[(lane & 3) * 2];
+    qs1 = sm_qs[(lane & 3) * 2 + 1];
+  }
+
+  // The warp's band of one tile: codes at kbase (K) and kbase + kQHalfBytes (V), its first position pos_base < n, the
+  // two scales of its block.  lg0: logit scratch of the (sequence, KV head), position-major, at this lane's heads.
+  __device__ __forceinline__ void tile(uint32_t kbase, int band0, int pos_base, int n, float ks, float vs, float* lg0, int gp,
+                                       uint64_t keep_policy, int lane) {
+    const float ninf = -INFINITY;
+    const int qd = lane >> 2, qc = (lane & 3) * 2;   // row of an 8-row group; first of the two heads this lane holds
+          float c[kQBlocks][4], c2[kQBlocks][4];   // two accumulator chains per block
+#pragma unroll
+          for (int i = 0; i < kQBlocks; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[i][j] = c2[i][j] = 0.f;
+#pragma unroll
+          for (int cs = 0; cs < 4; ++cs) {   // 32 channels
+#pragma unroll
+            for (int i = 0; i < kQBlocks; ++i) {
+              const int krow = band0 + 16 * i + (lane & 15), piece = 2 * cs + (lane >> 4);
+              uint32_t a[4];
+              ldsm_x4(a, kbase + krow * kHeadDim + ((piece ^ (krow & 7)) << 4));
+              mma_f16(c[i], codes_lo_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[0]), codes_hi_f16x2(a[1]),
+                      qb[2 * cs][0], qb[2 * cs][1]);
+              mma_f16(c2[i], codes_lo_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[2]), codes_hi_f16x2(a[3]),
+                      qb[2 * cs + 1][0], qb[2 * cs + 1][1]);
+            }
+          }
+          // one factor per head and tile; kept finite, so that a zero product stays zero (NaN scales pass)
+          float f0 = ks * qs0, f1 = ks * qs1;
+          f0 = f0 > FLT_MAX ? FLT_MAX : f0;
+          f1 = f1 > FLT_MAX ? FLT_MAX : f1;
+          float sc[kQBlocks][4];
+          float t0 = ninf, t1 = ninf;
+#pragma unroll
+          for (int i = 0; i < kQBlocks; ++i) {
+            const int r0 = pos_base + 16 * i + qd, r1 = r0 + 8;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[i][j] = (c[i][j] + c2[i][j]) * ((j & 1) ? f1 : f0);
+            if (kLogits) {
+              if ((qc < gp)) {
+                if (r0 < n) st_keep_f2(lg0 + (int64_t)r0 * gp, sc[i][0], sc[i][1], keep_policy);
+                if (r1 < n) st_keep_f2(lg0 + (int64_t)r1 * gp, sc[i][2], sc[i][3], keep_policy);
+              }
+            }
+            if (r0 >= n) sc[i][0] = sc[i][1] = ninf;
+            if (r1 >= n) sc[i][2] = sc[i][3] = ninf;
+            t0 = fmaxf(t0, fmaxf(sc[i][0], sc[i][2]));
+            t1 = fmaxf(t1, fmaxf(sc[i][1], sc[i][3]));
+          }
+#pragma unroll
+          for (int sh = 4; sh <= 16; sh <<= 1) {
+            t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, sh));
+            t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, sh));
+          }
+          const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+          if (__any_sync(0xffffffffu, (n0 > m0) || (n1 > m1))) {
+            const float a0 = (n0 == m0) ? 1.f : ex2((m0 - n0) * kLog2e);
+            const float a1 = (n1 == m1) ? 1.f : ex2((m1 - n1) * kLog2e);
+            l0 *= a0;
+            l1 *= a1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              o[i][0] *= a0;
+              o[i][1] *= a1;
+              o[i][2] *= a0;
+              o[i][3] *= a1;
+            }
+            m0 = n0;
+            m1 = n1;
+          }
+          if (vs > vref) {   // the same for the whole warp
+            uint32_t up = (__float_as_uint(vs) + 0x7fffffu) & 0x7f800000u;   // the next power of two, 2^126 at most
+            if (up > 0x7e800000u) up = 0x7e800000u;
+            const float a = vref * __uint_as_float(0x7f000000u - up);
+            vref = __uint_as_float(up);
+            vrcp = __uint_as_float(0x7f000000u - up);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[i][j] *= a;
+          }
+          const float vf = vs * vrcp * kPBase;
+          const float nm0 = (m0 == ninf) ? 0.f : -m0 * kLog2e;
+          const float nm1 = (m1 == ninf) ? 0.f : -m1 * kLog2e;
+          const uint32_t vbase = kbase + kQHalfBytes;
+#pragma unroll
+          for (int i = 0; i < kQBlocks; ++i) {
+            const int pos_i = pos_base + 16 * i;
+            if (pos_i >= n) continue;   // the whole block lies past the end
+            const float p0 = ex2(fmaf(sc[i][0], kLog2e, nm0)), p1 = ex2(fmaf(sc[i][1], kLog2e, nm1));
+            const float p2 = ex2(fmaf(sc[i][2], kLog2e, nm0)), p3 = ex2(fmaf(sc[i][3], kLog2e, nm1));
+            l0 += p0 + p2;
+            l1 += p1 + p3;
+            // P^T as the B operand: the two 8x8 [position][head] blocks transposed inside the warp
+            const uint32_t b0 = movmatrix_t(pack_f16(p0 * vf, p1 * vf)), b1 = movmatrix_t(pack_f16(p2 * vf, p3 * vf));
+            const bool tail = pos_i + 16 > n;
+            // rows past the end may hold anything (even NaN): their codes are cleared so that 0 * x stays 0.  A register
+            // holds positions 2 t, 2 t + 1 (t = lane & 3) of the first or of the second eight.
+            uint32_t mk0 = 0xffffffffu, mk1 = 0xffffffffu;
+            if (tail) {
+              const int pa = pos_i + qc;
+              mk0 = (pa < n ? 0x0000ffffu : 0u) | (pa + 1 < n ? 0xffff0000u : 0u);
+              mk1 = (pa + 8 < n ? 0x0000ffffu : 0u) | (pa + 9 < n ? 0xffff0000u : 0u);
+            }
+            const int vrow = band0 + 16 * i + (lane & 15);
+#pragma unroll
+            for (int sp = 0; sp < 4; ++sp) {   // two 16-channel segments
+              const int piece = 2 * sp + (lane >> 4);
+              uint32_t a[4];
+              ldsm_x4_t(a, vbase + vrow * kHeadDim + ((piece ^ (vrow & 7)) << 4));
+              if (tail) {
+                a[0] &= mk0;
+                a[1] &= mk1;
+                a[2] &= mk0;
+                a[3] &= mk1;
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j) a[j] = __byte_perm(a[j], 0u, 0x3120);   // (channel, two positions) in each half
+              mma_f16(o[2 * sp], codes_lo_f16x2(a[0]), codes_hi_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[1]), b0, b1);
+              mma_f16(o[2 * sp + 1], codes_lo_f16x2(a[2]), codes_hi_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[3]), b0, b1);
+            }
+          }
+  }
+
+  // The four warps' accumulators, scaled to the CTA-wide maximum, into sm (kMergeBytes); sm_wm: [warps][8].
+  __device__ __forceinline__ void merge(float* sm, float* sm_wm, int warp, int lane) {
+    const float ninf = -INFINITY;
+    const int qd = lane >> 2, qc = (lane & 3) * 2;
+#pragma unroll
+    for (int sh = 4; sh <= 16; sh <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
+    }
+    if (lane < 4) *reinterpret_cast<float2*>(sm_wm + warp * kMaxGroup + qc) = make_float2(m0, m1);
+    consumer_bar_n<32 * kQWarps>();   // every warp's maxima are visible, and nobody reads the stages any more
+    float* sm_l = sm + kMergeL;
+    float* sm_M = sm + kMergeM;
+    float M0 = ninf, M1 = ninf;
+#pragma unroll
+    for (int w = 0; w < kQWarps; ++w) {
+      const float2 mw = *reinterpret_cast<const float2*>(sm_wm + w * kMaxGroup + qc);
+      M0 = fmaxf(M0, mw.x);
+      M1 = fmaxf(M1, mw.y);
+    }
+    const float e0 = (m0 == ninf) ? 0.f : ex2((m0 - M0) * kLog2e);
+    const float e1 = (m1 == ninf) ? 0.f : ex2((m1 - M1) * kLog2e);
+    const float unit = vref * (1.f / kPBase);
+    float* base = sm + (warp * kMaxGroup + qc) * kQOPad + 2 * qd;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      *reinterpret_cast<float2*>(base + 16 * s) = make_float2(o[s][0] * e0 * unit, o[s][2] * e0 * unit);
+      *reinterpret_cast<float2*>(base + kQOPad + 16 * s) = make_float2(o[s][1] * e1 * unit, o[s][3] * e1 * unit);
+    }
+    if (lane < 4) {
+      sm_l[warp * kMaxGroup + qc] = l0 * e0;
+      sm_l[warp * kMaxGroup + qc + 1] = l1 * e1;
+      if (warp == 0) {
+        sm_M[qc] = M0;
+        sm_M[qc + 1] = M1;
+      }
+    }
+    consumer_bar_n<32 * kQWarps>();
+  }
+};
+
+// Sums over the warps of what merge() left: o into to[head][128]; (m, l) of head tid to two places each.
+__device__ __forceinline__ void publish(const float* sm, int G, int tid, float* to) {
+  for (int item = tid; item < G * 32; item += 32 * kQWarps) {   // (head, four channels)
+    const float* src = sm + (item >> 5) * kQOPad + (item & 31) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kQWarps; ++w) {
+      const float4 v = *reinterpret_cast<const float4*>(src + w * kMaxGroup * kQOPad);
+      acc.x += v.x;
+      acc.y += v.y;
+      acc.z += v.z;
+      acc.w += v.w;
+    }
+    *reinterpret_cast<float4*>(to + (item >> 5) * kHeadDim + (item & 31) * 4) = acc;
+  }
+}
+__device__ __forceinline__ float2 head_ml(const float* sm, int G, int h) {   // heads beyond the group: (-inf, 0)
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (h < G) {
+    ml.x = sm[kMergeM + h];
+#pragma unroll
+    for (int w = 0; w < kQWarps; ++w) ml.y += sm[kMergeL + w * kMaxGroup + h];
+  }
+  return ml;
+}
+
 // kCluster: the CTAs of a (sequence, KV head) are one thread-block cluster and finish the output themselves.
 template <bool kLogits, bool kCluster>
 __global__ void __launch_bounds__(kQThreads, 2)
@@ -109,7 +347,6 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
   const int G = p.group;
   const int64_t head0 = ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim;
-  const int qd = lane >> 2, qc = (lane & 3) * 2;   // row of an 8-row group; first of the two heads this lane holds
   // geometry: never written by a kernel, read above the dependency wait
   const int cap = __ldg(p.cap + b);
   const int64_t roff = __ldg(p.row_offset + b);
@@ -169,37 +406,12 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   __half* sm_q = reinterpret_cast<__half*>(smem + kQAt);
   float* sm_qs = reinterpret_cast<float*>(smem + kQsAt);
   float* sm_wm = reinterpret_cast<float*>(smem + kWmAt);
-  uint32_t qb[8][2];              // B fragments of Q^T: [16-channel segment][k half]
-  float qs0 = 0.f, qs1 = 0.f;     // softmax scale over the queries' powers of two, for heads qc and qc + 1
+  Consumer<kLogits> mma;
   if (warp < kQWarps) {
     uint4 qv = make_uint4(0u, 0u, 0u, 0u);
-    const int h = tid >> 4;       // 16 lanes to a head's row
-    if (h < G) qv = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + head0) + tid);
+    if (tid < G * 16) qv = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + head0) + tid);
     load_scales(0);
-    uint32_t m = __vmaxu2(__vmaxu2(qv.x & 0x7fff7fffu, qv.y & 0x7fff7fffu), __vmaxu2(qv.z & 0x7fff7fffu, qv.w & 0x7fff7fffu));
-    m = max(m & 0xffffu, m >> 16);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    // 2^e brings the largest magnitude into [2^14, 2^15); nothing is done for a row that is not finite or zero
-    int e = 14 - ((int)(m >> 7) - 127);
-    if (m >= 0x7f80u || m == 0u) e = 0;
-    if (e > 126) e = 126;
-    const float up = pow2f(e);
-    const uint32_t x[4] = {qv.x, qv.y, qv.z, qv.w};
-    uint32_t y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = pack_f16(__uint_as_float(x[i] << 16) * up, __uint_as_float(x[i] & 0xffff0000u) * up);
-    *reinterpret_cast<uint4*>(sm_q + h * kQRow + (tid & 15) * 8) = make_uint4(y[0], y[1], y[2], y[3]);
-    if ((tid & 15) == 0) sm_qs[h] = p.scale * pow2f(-e);
-    consumer_bar_n<32 * kQWarps>();
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {   // channels 16 s + 4 t .. + 3 of head qd, t = lane & 3
-      const uint2 f = *reinterpret_cast<const uint2*>(sm_q + qd * kQRow + 16 * s + 4 * (lane & 3));
-      qb[s][0] = f.x;
-      qb[s][1] = f.y;
-    }
-    qs0 = sm_qs[qc];
-    qs1 = sm_qs[qc + 1];
+    mma.queries(qv, p.scale, sm_q, sm_qs, tid);
   }
 
   auto drain_spec = [&] {   // tiles requested ahead of the length must land before the CTA may go
@@ -259,19 +471,10 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 
   // ---------------------------------------------------------------- MMA warps
-  const float ninf = -INFINITY;
-  float m0 = ninf, m1 = ninf, l0 = 0.f, l1 = 0.f;
-  float vref = 1.17549435e-38f, vrcp = 8.50705917e37f;   // 2^-126 and its reciprocal
-  float o[8][4];   // [16-channel segment]: (channel 16 s + 2 qd, heads qc, qc + 1), (the next channel, the same heads)
-#pragma unroll
-  for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  float* lg0 = nullptr;   // logit scratch, position-major: [position][gp] floats
+  mma.reset();
+  float* lg0 = kLogits ? p.logits + bg * p.logit_stride * p.gp + (lane & 3) * 2 : nullptr;
   uint64_t keep_policy = 0;
-  if (kLogits) {
-    lg0 = p.logits + bg * p.logit_stride * p.gp + qc;
-    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep_policy));
-  }
-  const bool lg_on = kLogits && qc < p.gp;
+  if (kLogits) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep_policy));
 
   const int n_wait = n_tiles > n_spec ? n_tiles : n_spec;   // tiles requested ahead of the length are always consumed
   for (int t = 0; t < n_wait; ++t) {
@@ -283,196 +486,28 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       break;
     }
     const int pos_base = tile_pos(t) + band0;
-    if (t < n_tiles && pos_base < n) {
-      const uint32_t kbase = smem_base + s * kQStageBytes;
-      float c[kQBlocks][4], c2[kQBlocks][4];   // two accumulator chains per block
-#pragma unroll
-      for (int i = 0; i < kQBlocks; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[i][j] = c2[i][j] = 0.f;
-#pragma unroll
-      for (int cs = 0; cs < 4; ++cs) {   // 32 channels
-#pragma unroll
-        for (int i = 0; i < kQBlocks; ++i) {
-          const int krow = band0 + 16 * i + (lane & 15), piece = 2 * cs + (lane >> 4);
-          uint32_t a[4];
-          ldsm_x4(a, kbase + krow * kHeadDim + ((piece ^ (krow & 7)) << 4));
-          mma_f16(c[i], codes_lo_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[0]), codes_hi_f16x2(a[1]),
-                  qb[2 * cs][0], qb[2 * cs][1]);
-          mma_f16(c2[i], codes_lo_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[2]), codes_hi_f16x2(a[3]),
-                  qb[2 * cs + 1][0], qb[2 * cs + 1][1]);
-        }
-      }
-      // one factor per head and tile; kept finite, so that a zero product stays zero (NaN scales pass)
-      float f0 = ks * qs0, f1 = ks * qs1;
-      f0 = f0 > FLT_MAX ? FLT_MAX : f0;
-      f1 = f1 > FLT_MAX ? FLT_MAX : f1;
-      float sc[kQBlocks][4];
-      float t0 = ninf, t1 = ninf;
-#pragma unroll
-      for (int i = 0; i < kQBlocks; ++i) {
-        const int r0 = pos_base + 16 * i + qd, r1 = r0 + 8;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sc[i][j] = (c[i][j] + c2[i][j]) * ((j & 1) ? f1 : f0);
-        if (kLogits) {
-          if (lg_on) {
-            if (r0 < n) st_keep_f2(lg0 + (int64_t)r0 * p.gp, sc[i][0], sc[i][1], keep_policy);
-            if (r1 < n) st_keep_f2(lg0 + (int64_t)r1 * p.gp, sc[i][2], sc[i][3], keep_policy);
-          }
-        }
-        if (r0 >= n) sc[i][0] = sc[i][1] = ninf;
-        if (r1 >= n) sc[i][2] = sc[i][3] = ninf;
-        t0 = fmaxf(t0, fmaxf(sc[i][0], sc[i][2]));
-        t1 = fmaxf(t1, fmaxf(sc[i][1], sc[i][3]));
-      }
-#pragma unroll
-      for (int sh = 4; sh <= 16; sh <<= 1) {
-        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, sh));
-        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, sh));
-      }
-      const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
-      if (__any_sync(0xffffffffu, (n0 > m0) || (n1 > m1))) {
-        const float a0 = (n0 == m0) ? 1.f : ex2((m0 - n0) * kLog2e);
-        const float a1 = (n1 == m1) ? 1.f : ex2((m1 - n1) * kLog2e);
-        l0 *= a0;
-        l1 *= a1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          o[i][0] *= a0;
-          o[i][1] *= a1;
-          o[i][2] *= a0;
-          o[i][3] *= a1;
-        }
-        m0 = n0;
-        m1 = n1;
-      }
-      if (vs > vref) {   // the same for the whole warp
-        uint32_t up = (__float_as_uint(vs) + 0x7fffffu) & 0x7f800000u;   // the next power of two, 2^126 at most
-        if (up > 0x7e800000u) up = 0x7e800000u;
-        const float a = vref * __uint_as_float(0x7f000000u - up);
-        vref = __uint_as_float(up);
-        vrcp = __uint_as_float(0x7f000000u - up);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[i][j] *= a;
-      }
-      const float vf = vs * vrcp * kPBase;
-      const float nm0 = (m0 == ninf) ? 0.f : -m0 * kLog2e;
-      const float nm1 = (m1 == ninf) ? 0.f : -m1 * kLog2e;
-      const uint32_t vbase = kbase + kQHalfBytes;
-#pragma unroll
-      for (int i = 0; i < kQBlocks; ++i) {
-        const int pos_i = pos_base + 16 * i;
-        if (pos_i >= n) continue;   // the whole block lies past the end
-        const float p0 = ex2(fmaf(sc[i][0], kLog2e, nm0)), p1 = ex2(fmaf(sc[i][1], kLog2e, nm1));
-        const float p2 = ex2(fmaf(sc[i][2], kLog2e, nm0)), p3 = ex2(fmaf(sc[i][3], kLog2e, nm1));
-        l0 += p0 + p2;
-        l1 += p1 + p3;
-        // P^T as the B operand: the two 8x8 [position][head] blocks transposed inside the warp
-        const uint32_t b0 = movmatrix_t(pack_f16(p0 * vf, p1 * vf)), b1 = movmatrix_t(pack_f16(p2 * vf, p3 * vf));
-        const bool tail = pos_i + 16 > n;
-        // rows past the end may hold anything (even NaN): their codes are cleared so that 0 * x stays 0.  A register
-        // holds positions 2 t, 2 t + 1 (t = lane & 3) of the first or of the second eight.
-        uint32_t mk0 = 0xffffffffu, mk1 = 0xffffffffu;
-        if (tail) {
-          const int pa = pos_i + qc;
-          mk0 = (pa < n ? 0x0000ffffu : 0u) | (pa + 1 < n ? 0xffff0000u : 0u);
-          mk1 = (pa + 8 < n ? 0x0000ffffu : 0u) | (pa + 9 < n ? 0xffff0000u : 0u);
-        }
-        const int vrow = band0 + 16 * i + (lane & 15);
-#pragma unroll
-        for (int sp = 0; sp < 4; ++sp) {   // two 16-channel segments
-          const int piece = 2 * sp + (lane >> 4);
-          uint32_t a[4];
-          ldsm_x4_t(a, vbase + vrow * kHeadDim + ((piece ^ (vrow & 7)) << 4));
-          if (tail) {
-            a[0] &= mk0;
-            a[1] &= mk1;
-            a[2] &= mk0;
-            a[3] &= mk1;
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) a[j] = __byte_perm(a[j], 0u, 0x3120);   // (channel, two positions) in each half
-          mma_f16(o[2 * sp], codes_lo_f16x2(a[0]), codes_hi_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[1]), b0, b1);
-          mma_f16(o[2 * sp + 1], codes_lo_f16x2(a[2]), codes_hi_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[3]), b0, b1);
-        }
-      }
-    }
+    if (t < n_tiles && pos_base < n)
+      mma.tile(smem_base + s * kQStageBytes, band0, pos_base, n, ks, vs, lg0, p.gp, keep_policy, lane);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_empty + 8 * s);
   }
 
-#pragma unroll
-  for (int sh = 4; sh <= 16; sh <<= 1) {
-    l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
-    l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
-  }
-
-  // ------------------------------------------------ merge the MMA warps: accumulators scaled to the CTA-wide maximum
-  if (lane < 4) *reinterpret_cast<float2*>(sm_wm + warp * kMaxGroup + qc) = make_float2(m0, m1);
-  consumer_bar_n<32 * kQWarps>();   // every warp's maxima are visible, and the stage memory is free
-  float* sm_o = reinterpret_cast<float*>(smem);              // [warps][8][kQOPad]
-  float* sm_l = sm_o + kQWarps * kMaxGroup * kQOPad;         // [warps][8]
-  float* sm_M = sm_l + kQWarps * kMaxGroup;                  // [8]
-  {
-    float M0 = ninf, M1 = ninf;
-#pragma unroll
-    for (int w = 0; w < kQWarps; ++w) {
-      const float2 mw = *reinterpret_cast<const float2*>(sm_wm + w * kMaxGroup + qc);
-      M0 = fmaxf(M0, mw.x);
-      M1 = fmaxf(M1, mw.y);
-    }
-    const float e0 = (m0 == ninf) ? 0.f : ex2((m0 - M0) * kLog2e);
-    const float e1 = (m1 == ninf) ? 0.f : ex2((m1 - M1) * kLog2e);
-    const float unit = vref * (1.f / kPBase);
-    float* base = sm_o + (warp * kMaxGroup + qc) * kQOPad + 2 * qd;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      *reinterpret_cast<float2*>(base + 16 * s) = make_float2(o[s][0] * e0 * unit, o[s][2] * e0 * unit);
-      *reinterpret_cast<float2*>(base + kQOPad + 16 * s) = make_float2(o[s][1] * e1 * unit, o[s][3] * e1 * unit);
-    }
-    if (lane < 4) {
-      sm_l[warp * kMaxGroup + qc] = l0 * e0;
-      sm_l[warp * kMaxGroup + qc + 1] = l1 * e1;
-      if (warp == 0) {
-        sm_M[qc] = M0;
-        sm_M[qc + 1] = M1;
-      }
-    }
-  }
-  consumer_bar_n<32 * kQWarps>();
+  float* sm_merge = reinterpret_cast<float*>(smem);   // (the stages are free by then)
+  mma.merge(sm_merge, sm_wm, warp, lane);
   float* sm_sum = reinterpret_cast<float*>(smem + kQStageBytes);   // cluster: this CTA's share, [8][128] and [8][2]
   float* sm_ml = sm_sum + kMaxGroup * kHeadDim;
-  for (int item = tid; item < G * 32; item += 32 * kQWarps) {   // (head, four channels)
-    const float* src = sm_o + (item >> 5) * kQOPad + (item & 31) * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kQWarps; ++w) {
-      const float4 v = *reinterpret_cast<const float4*>(src + w * kMaxGroup * kQOPad);
-      acc.x += v.x;
-      acc.y += v.y;
-      acc.z += v.z;
-      acc.w += v.w;
-    }
-    *reinterpret_cast<float4*>((kCluster ? sm_sum : part) + (item >> 5) * kHeadDim + (item & 31) * 4) = acc;
-  }
+  publish(sm_merge, G, tid, kCluster ? sm_sum : part);
   if (tid < kMaxGroup) {
-    float M = ninf, L = 0.f;
-    if (tid < G) {
-      M = sm_M[tid];
-#pragma unroll
-      for (int w = 0; w < kQWarps; ++w) L += sm_l[w * kMaxGroup + tid];
-    }
+    const float2 v = head_ml(sm_merge, G, tid);
     if (kCluster) {
-      *reinterpret_cast<float2*>(sm_ml + 2 * tid) = make_float2(M, L);
+      *reinterpret_cast<float2*>(sm_ml + 2 * tid) = v;
     } else {
-      part[kMaxGroup * kHeadDim + tid] = M;
-      part[kMaxGroup * kHeadDim + kMaxGroup + tid] = L;
+      part[kMaxGroup * kHeadDim + tid] = v.x;
+      part[kMaxGroup * kHeadDim + kMaxGroup + tid] = v.y;
     }
     if (kLogits || !kCluster) {
-      ml[(int64_t)tid * p.max_splits] = M;
-      ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = L;
+      ml[(int64_t)tid * p.max_splits] = v.x;
+      ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = v.y;
     }
   }
   if (kCluster) {
@@ -486,6 +521,7 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       const uint32_t at = smem_u32(sm_sum + hh * kHeadDim + ch), ml_at = smem_u32(sm_ml + 2 * hh);
       float4 v[kQCluster];
       float2 e[kQCluster];
+      const float ninf = -INFINITY;
       float M = ninf, L = 0.f;
 #pragma unroll
       for (int r = 0; r < kQCluster; ++r) {
