@@ -40,7 +40,7 @@ int splits_for(const rkv_config* c) {
   return s < rkv::kMaxSplits ? (s < 1 ? 1 : s) : rkv::kMaxSplits;
 }
 
-struct WsLayout { size_t partials, ml_t, tickets, len_tickets, win_keys, keys, hist, anchor, logits, status, total; int64_t logit_stride; };
+struct WsLayout { size_t partials, ml_t, tickets, len_tickets, win_keys, keys, hist, anchor, counts, logits, status, total; int64_t logit_stride; };
 
 WsLayout ws_layout(const rkv_config* c) {
   WsLayout w;
@@ -57,6 +57,7 @@ WsLayout ws_layout(const rkv_config* c) {
   w.keys = off;     off = up(off + bg * (size_t)w.logit_stride * sizeof(uint32_t));
   w.hist = off;     off = up(off + bg * (size_t)rkv::kSelectBins * sizeof(uint32_t));
   w.anchor = off;   off = up(off + bg * sizeof(int32_t));
+  w.counts = off;   off = up(off + bg * sizeof(int32_t));
   const int gp = group <= 4 ? 4 : 8;   // position-major logits, padded to a vector width
   w.logits = off;   off = up(off + bg * gp * (size_t)w.logit_stride * sizeof(float));
   w.status = off;   off = up(off + sizeof(int32_t));
@@ -269,25 +270,33 @@ rkv_status run_attention(rkv_ctx* ctx, const void* q, const rkv_cache* cache, co
   return RKV_OK;
 }
 
-// Up to this length bound the CTAs of a (sequence, KV head) are a cluster that finishes the output itself (no fold
-// launch), at the price of eight CTAs at most.  Measured for 8 KV heads, cluster against splits and fold: 4.1 / 5.0 us at
-// 1000 positions, 4.85 / 5.1 at 2048, 6.6 / 6.05 at 4096, 9.9 / 7.1 at 8192.
-constexpr int kQuantClusterMaxLen = 2048;
-// The pass over the 8-bit cache: the same splits and workspace as the streaming form above, tiles of 128 positions
-// dealt out in turn.
+// The pass over the 8-bit cache, in one of three forms (all write the same workspace):
+//   splits    one sequence: its tiles of 128 positions are dealt out in turn to as many CTAs per KV head as fit one wave
+//             (two to an SM); a fold launch - or the score pass - finishes the output
+//   cluster   short contexts: 1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves.
+//             Measured for 8 KV heads, cluster against splits: 4.1 / 5.0 us at 1000 positions, 4.85 / 5.1 at 2048, 6.6 / 6.05
+//             at 4096, 9.9 / 7.1 at 8192
+//   balanced  longer batches: equal runs of tiles across heads and sequences, then its own fold
+constexpr int kQuantClusterMaxLen = 2048, kQuantClusterMaxBatch = 1024;
+struct QuantPass { int gx; bool finished; const int32_t* counts; };   // what the second half has to know
+
 rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cache* cache, const int32_t* active,
-                               void* out, int n_max, bool logits, cudaStream_t st, int* gx_out, bool* finished) {
+                               void* out, int n_max, bool logits, bool fold_out, cudaStream_t st, QuantPass* pass) {
   if (!aligned16(q) || !aligned16(out)) return RKV_ERR_INVALID_ARG;
   CUtensorMap tm_k, tm_v;
   rkv_status s = tensor_map(ctx, cache->k, cache->n_rows, &tm_k, true);
   if (s != RKV_OK) return s;
   s = tensor_map(ctx, cache->v, cache->n_rows, &tm_v, true);
   if (s != RKV_OK) return s;
-  int gx = 1;
-  choose_chunk(ctx, n_max, true, &gx);
+  const int n_seq = ctx->cfg.n_seq;
+  const int64_t bg = (int64_t)n_seq * ctx->cfg.n_kv_heads, slots = 2 * ctx->sm_count;
   const int tiles = (n_max + rkv::kQuantTile - 1) / rkv::kQuantTile;
+  int gx = (int)(slots / bg);
+  if (gx > ctx->max_splits) gx = ctx->max_splits;
   if (gx > tiles) gx = tiles;
-  const bool cluster = n_max <= kQuantClusterMaxLen || gx <= 8;
+  if (gx < 1) gx = 1;
+  const bool balanced = n_seq > 1 && n_seq <= rkv::kQuantMaxSeq && n_max > kQuantClusterMaxBatch;
+  const bool cluster = !balanced && (n_max <= kQuantClusterMaxLen || gx <= 8);
   if (cluster) gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
   rkv::QuantAttnParams p;
   memset(&p, 0, sizeof(p));
@@ -303,31 +312,46 @@ rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cach
   p.ml_t = ctx->ml_t;
   p.logits = logits ? ctx->logits : nullptr;
   p.hist = ctx->hist;
+  p.counts = ctx->split_counts;
   p.status = ctx->status;
   p.n_rows = cache->n_rows;
   p.logit_stride = ctx->logit_stride;
+  p.n_seq = n_seq;
   p.n_q_heads = ctx->cfg.n_q_heads;
   p.n_kv_heads = ctx->cfg.n_kv_heads;
   p.group = ctx->group;
   p.gp = ctx->gp;
   p.max_splits = ctx->max_splits;
   p.max_len = n_max;
-  p.spec = (active == nullptr && ctx->cfg.n_seq == 1) ? 1 : 0;
+  p.scale = ctx->cfg.softmax_scale;
+  p.spec = (active == nullptr && n_seq == 1) ? 1 : 0;
   // as in the bf16 pass: one tile ahead of the wait behind the short merge kernel, the whole ring behind others
   if (p.spec != 0 && ctx->early_read && rkv::early_read_safe(st, cache)) p.early = rkv::last_launch_was_fold(st) ? 1 : 2;
-  p.scale = ctx->cfg.softmax_scale;
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_ATTN_FULL);
-    const bool one_wave = (int64_t)gx * ctx->cfg.n_kv_heads * ctx->cfg.n_seq <= 2 * ctx->sm_count;
-    e = rkv::launch_quant_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, one_wave, st);
+    if (balanced) {
+      const int64_t most = bg * tiles;   // tiles there can be
+      e = rkv::launch_quant_balanced(p, tm_k, tm_v, (int)(most < slots ? most : slots), st);
+    } else {
+      e = rkv::launch_quant_attention(p, tm_k, tm_v, n_seq, gx, cluster, gx * bg <= slots, st);
+    }
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit attention launch");
   ctx->launches += 1;
   if (logits) ctx->hist_dirty = false;   // (the pass has cleared it)
   rkv::note_launch(st, nullptr, nullptr);
-  *gx_out = gx;
-  *finished = cluster;
+  *pass = {balanced ? ctx->max_splits : gx, cluster || balanced || fold_out, balanced ? ctx->split_counts : nullptr};
+  if (cluster || (!balanced && !fold_out)) return RKV_OK;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_FOLD);
+    e = balanced ? rkv::launch_quant_fold(p, st)
+                 : rkv::launch_fold(ctx->partials, ctx->ml_t, cache->len, cache->cap, active, out, n_seq, ctx->cfg.n_q_heads,
+                                    ctx->cfg.n_kv_heads, rkv::kQuantTile, ctx->max_splits, n_max, gx, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "fold launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr, true);
   return RKV_OK;
 }
 
@@ -458,6 +482,7 @@ rkv_status rkv_create(const rkv_config* cfg, rkv_ctx** out) {
   ctx->keys = reinterpret_cast<uint32_t*>(ctx->workspace + w.keys);
   ctx->hist = reinterpret_cast<uint32_t*>(ctx->workspace + w.hist);   // zeroed with the rest of the workspace above
   ctx->anchor = reinterpret_cast<int32_t*>(ctx->workspace + w.anchor);
+  ctx->split_counts = reinterpret_cast<int32_t*>(ctx->workspace + w.counts);
   ctx->hist_dirty = false;
   ctx->pending_keys.valid = false;
   ctx->pending_full.valid = false;
@@ -502,7 +527,7 @@ static rkv_status full_attention_part(rkv_ctx* ctx, const void* q, const rkv_cac
     ctx->launches += 1;
     rkv::note_launch(st, nullptr, nullptr, true);
   }
-  ctx->pending_full = {true, chunk, gx, n_max, full->k, active};
+  ctx->pending_full = {true, chunk, gx, n_max, full->k, active, nullptr};
   return RKV_OK;
 }
 
@@ -518,6 +543,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
     return RKV_ERR_INVALID_ARG;
   if (k_max < 1 || k_max > ctx->cfg.max_small) return RKV_ERR_INVALID_ARG;
   int n_max, chunk, gx;
+  const int32_t* counts = nullptr;
   if (stage == kStageSelect) {
     if (!ctx->pending_keys.valid || ctx->pending_keys.k_max != k_max) return RKV_ERR_INVALID_ARG;
     n_max = ctx->pending_keys.n_max;
@@ -526,6 +552,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   } else {
     if (!ctx->pending_full.valid) return RKV_ERR_INVALID_ARG;   // no attention pass to take the logits from
     n_max = ctx->pending_full.n_max, chunk = ctx->pending_full.chunk, gx = ctx->pending_full.gx;
+    counts = ctx->pending_full.counts;
     if (scores != nullptr && score_stride < n_max) return RKV_ERR_INVALID_ARG;
     ctx->pending_full.valid = false;
     ctx->pending_keys.valid = false;
@@ -569,6 +596,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   cp.chunk = chunk;
   cp.max_splits = ctx->max_splits;
   cp.grid_splits = gx;
+  cp.split_counts = counts;
   cp.pool_half = (ctx->cfg.pool_kernel - 1) / 2;
   SelectParams sp;
   memset(&sp, 0, sizeof(sp));
@@ -632,29 +660,20 @@ static rkv_status full_step_impl(rkv_ctx* ctx, const void* q, const rkv_cache* f
 }
 
 // The 8-bit cache's first half: as full_attention_part.  Without kept logits there is nothing for a second half.
+// fold_out: finish out here in every form; otherwise *finished says whether the score pass has to.
 static rkv_status quant_attention_part(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full, const int32_t* active,
                                        void* out, int32_t max_len_hint, bool logits, bool fold_out, cudaStream_t st,
                                        bool* finished) {
   if (!ctx || !q || !quant_ok(full) || !out || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
   const int n_max = max_len_hint == 0 ? ctx->cfg.max_len : max_len_hint;
   if (n_max < 1 || n_max > ctx->cfg.max_len) return RKV_ERR_INVALID_ARG;
-  int gx = 1;
   ctx->pending_full.valid = false;
   ctx->pending_keys.valid = false;
-  rkv_status s = run_quant_attention(ctx, q, full, active, out, n_max, logits, st, &gx, finished);
+  QuantPass pass;
+  rkv_status s = run_quant_attention(ctx, q, full, active, out, n_max, logits, fold_out, st, &pass);
   if (s != RKV_OK) return s;
-  if (fold_out && !*finished) {
-    cudaError_t e;
-    {
-      LaunchScope scope(ctx, st, RKV_KERNEL_FOLD);
-      e = rkv::launch_fold(ctx->partials, ctx->ml_t, full->len, full->cap, active, out, ctx->cfg.n_seq,
-                           ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads, rkv::kQuantTile, ctx->max_splits, n_max, gx, st);
-    }
-    if (e != cudaSuccess) return cuda_fail(ctx, e, "fold launch");
-    ctx->launches += 1;
-    rkv::note_launch(st, nullptr, nullptr, true);
-  }
-  if (logits) ctx->pending_full = {true, rkv::kQuantTile, gx, n_max, full->k, active};
+  if (logits) ctx->pending_full = {true, rkv::kQuantTile, pass.gx, n_max, full->k, active, pass.counts};
+  *finished = pass.finished;
   return RKV_OK;
 }
 

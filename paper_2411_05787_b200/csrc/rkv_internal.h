@@ -27,6 +27,7 @@ constexpr int kSelectMaxKeysPerCta = 40960;   // max_len <= kSelectCluster * thi
 constexpr int kSelectBins = 4096;      // bins of the per-(sequence, KV head) score histogram in the workspace
 constexpr int kSelectMaxSlice = 8192;  // most positions one CTA of the score pass takes
 constexpr int kQuantBlock = 64;        // positions that share a scale in the 8-bit cache
+constexpr int kQuantMaxSeq = 256;      // sequences of a batch that the balanced pass over the 8-bit cache takes
 constexpr int kQuantTile = 128;        // positions per pipeline stage of the pass over the 8-bit cache
 
 struct PartialLayout {                 // split-K partial of one (b, g, split)
@@ -96,6 +97,7 @@ struct ScoreParams {
   int32_t slice, n_slices;    // positions per CTA; CTAs per (sequence, KV head)
   int32_t chunk, max_splits;  // split geometry of the attention launch that produced the partials
   int32_t grid_splits;        // CTAs per (sequence, KV head) that launch had
+  const int32_t* split_counts;   // [B*Hkv] partials of each head, or null: they follow from the length, chunk and grid_splits
   int32_t pool_half;          // (pool_kernel - 1) / 2
 };
 
@@ -141,9 +143,10 @@ struct QuantAttnParams {
   void* out;                  // bf16 [B][Hq][128]: written here for empty sequences only
   float* partials; float* ml_t; float* logits;  // as in AttnParams
   uint32_t* hist;             // [B*Hkv][kSelectBins]: cleared when logits are kept
+  int32_t* counts;            // [B*Hkv]: partials of each head (balanced form)
   int32_t* status;
   int64_t n_rows, logit_stride;
-  int32_t n_q_heads, n_kv_heads, group, gp, max_splits, max_len;
+  int32_t n_seq, n_q_heads, n_kv_heads, group, gp, max_splits, max_len;
   int32_t spec;               // 1: first tiles may be requested before the length is read (one sequence, no mask)
   int32_t early;              // how many of them before the dependency wait (AttnParams::early)
   float scale;
@@ -156,6 +159,9 @@ cudaError_t launch_quant_store(const QuantNew& rows, const int32_t* start, const
 cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small, int k_max, const QuantDev& full,
                                 const CacheDev& small_cache, const int32_t* active, int n_seq, int n_kv_heads,
                                 int32_t* status, cudaStream_t st);
+cudaError_t launch_quant_balanced(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_cta,
+                                  cudaStream_t st);
+cudaError_t launch_quant_fold(const QuantAttnParams& p, cudaStream_t st);   // out from the balanced form's partials
 cudaError_t prepare_quant_attention();
 cudaError_t launch_rope(const void* qkv, bool is_bf16, int64_t tok_stride, const int32_t* pos, int n_tok, int n_q,
                         int n_kv, const uint64_t* freqs, int rot, bool interleaved, float amp, void* q, void* k, void* v,
@@ -289,6 +295,7 @@ struct rkv_ctx {
   uint32_t* keys;      // key of every position of the last score pass
   uint32_t* hist;      // per (sequence, KV head) histogram of those keys; all zero between selections
   int32_t* anchor;     // per (sequence, KV head): start of the histogram's window
+  int32_t* split_counts;   // per (sequence, KV head): partials of the last balanced pass over an 8-bit cache
   bool hist_dirty;     // a score pass was launched whose selection (which clears the histogram) was not
   float* logits;
   int32_t* status;
@@ -302,7 +309,7 @@ struct rkv_ctx {
   int select_keys_per_cta;   // keys one CTA of a selection cluster takes (about): fewer = shorter chain, more = fewer CTAs
   int score_slice;           // positions per CTA of the score pass; 0: chosen per launch
   // geometry of the last rkv_full_attention, for the rkv_select_topk that completes it
-  struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; } pending_full;
+  struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; const int32_t* counts; } pending_full;
   // ... and of the last rkv_score_keys, for the rkv_select_topk that launches the selection alone
   struct { bool valid; int n_max, k_max; const void* full_k; const int32_t* active; } pending_keys;
   int gp;              // floats per position in the logit scratch

@@ -55,6 +55,12 @@ constexpr int kQsAt = kQAt + kMaxGroup * kQRow * 2;
 constexpr int kWmAt = kQsAt + kMaxGroup * 4;
 constexpr int kQSmem = kWmAt + kQWarps * kMaxGroup * 4 + 1024;   // + alignment of the stages
 constexpr int kQSmemPair = kQSmem + 20 * 1024;       // as much as lets only two CTAs onto an SM
+// the balanced form: its merge buffer beside the stages (the next head's tiles are in them), and the sequences' tables
+constexpr int kBMergeAt = kWmAt + kQWarps * kMaxGroup * 4;
+constexpr int kBTablesAt = (kBMergeAt + kMergeBytes + 15) & ~15;
+constexpr int kBSmem = kBTablesAt + kQuantMaxSeq * (8 + 4 * 4) + 16 + 1024;
+static_assert(2 * (kBSmem + 1024) <= 228 * 1024, "two CTAs per SM");
+static_assert((kQuantMaxSeq & (kQuantMaxSeq - 1)) == 0, "binary search over the sequences");
 static_assert(2 * (kQSmemPair + 1024) <= 228 * 1024 && 3 * (kQSmemPair + 1024) > 228 * 1024, "two CTAs per SM, no third");
 
 __device__ __forceinline__ void tma_load_codes(uint32_t dst, const CUtensorMap* tm, int row, uint32_t bar,
@@ -554,6 +560,296 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 }
 
+
+// ---------------------------------------------------------------------------------------------- batches: balanced form
+// The tiles of all heads of all sequences, in order, are cut into equal runs, one per CTA, in a single wave: whatever the
+// lengths, every CTA streams the same number of tiles up to one.  (With a fixed number of CTAs per (sequence, KV head) a
+// ragged batch waits for its longest sequence, and the waves a finer cut needs cost more than they balance: 16 sequences
+// of up to 3000 positions, 8 heads: 16.4 us with two CTAs a head, 23.4 with 24.)  The lengths are on the device, so every
+// CTA sums them up itself.  A run covers the end of one head and the beginning of the next, or several whole ones; each
+// piece leaves one split partial, slot = CTA - first CTA of that head, and the head's first CTA records how many there
+// are.  The copy warp walks the tiles without stopping at heads; the next head's queries and scales are requested while
+// the current one's tiles are worked on.
+struct Piece {   // the tiles of one (sequence, KV head) in a CTA's run
+  int b, g, tile, count;
+};
+
+__device__ __forceinline__ Piece piece_at(int x, int end, int b, const int* pref, const int* tiles) {
+  while (pref[b + 1] <= x) ++b;            // (sequences without tiles are stepped over)
+  Piece s;
+  s.b = b;
+  const int rem = x - pref[b];
+  s.g = rem / tiles[b];
+  s.tile = rem - s.g * tiles[b];
+  s.count = min(tiles[b] - s.tile, end - x);
+  return s;
+}
+
+template <bool kLogits>
+__global__ void __launch_bounds__(kQThreads, 2)
+quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                      const QuantAttnParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+  const uint32_t bar_full = smem_base + kBarsAt, bar_empty = bar_full + 8 * kQStages;
+  __half* sm_q = reinterpret_cast<__half*>(smem + kQAt);
+  float* sm_qs = reinterpret_cast<float*>(smem + kQsAt);
+  float* sm_wm = reinterpret_cast<float*>(smem + kWmAt);
+  float* sm_merge = reinterpret_cast<float*>(smem + kBMergeAt);
+  int64_t* sm_row = reinterpret_cast<int64_t*>(smem + kBTablesAt);            // first row of a sequence
+  int* sm_cap = reinterpret_cast<int*>(sm_row + kQuantMaxSeq);
+  int* sm_len = sm_cap + kQuantMaxSeq;
+  int* sm_tiles = sm_len + kQuantMaxSeq;                                      // of one head
+  int* sm_pref = sm_tiles + kQuantMaxSeq;                                     // tiles of all heads of the sequences before
+  int* sm_most = sm_pref + kQuantMaxSeq + 1;
+  if (tid == 0) {
+    for (int s = 0; s < kQStages; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, kQWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid == 32 * kQWarps) {
+    prefetch_tensormap(&tm_k);
+    prefetch_tensormap(&tm_v);
+  }
+  for (int b = tid; b < p.n_seq; b += kQThreads) {   // geometry: never written by a kernel, read above the dependency wait
+    sm_row[b] = __ldg(p.row_offset + b);
+    sm_cap[b] = __ldg(p.cap + b);
+  }
+  pdl_wait();
+  pdl_launch();   // after the wait: at most one predecessor is ever in flight behind a kernel of this library
+  const int n_bg = p.n_seq * p.n_kv_heads;
+  int flags = 0;
+  for (int b = tid; b < p.n_seq; b += kQThreads) {   // (each entry by the thread that wrote its geometry)
+    const int act = (p.active != nullptr) ? __ldcg(p.active + b) : 1;
+    int n = __ldcg(p.len + b);
+    const int cap = sm_cap[b], lim = cap < p.max_len ? cap : p.max_len;
+    if (act == 0) {
+      n = 0;
+    } else if (!quant_layout_ok(sm_row[b], cap, p.n_kv_heads, p.n_rows)) {
+      flags |= RKV_DEV_BAD_LAYOUT;
+      n = 0;
+    } else if (n > lim) {
+      flags |= RKV_DEV_LEN_CLAMPED;
+      n = lim;
+    }
+    if (n < 0) n = 0;
+    sm_len[b] = n;
+    sm_tiles[b] = (n + kQuantTile - 1) / kQuantTile;
+  }
+  if (cta == 0 && flags != 0) atomicOr(p.status, flags);
+  if (kLogits)    // the score pass that may follow adds to the keys' histograms: they start from zero
+    for (int bg = cta; bg < n_bg; bg += gridDim.x)
+      for (int i = tid; i < kSelectBins; i += kQThreads) p.hist[(int64_t)bg * kSelectBins + i] = 0u;
+  __syncthreads();
+  if (warp == 0) {
+    int sum = 0, most = 0;
+    for (int b0 = 0; b0 < p.n_seq; b0 += 32) {
+      const int b = b0 + lane, mine = b < p.n_seq ? sm_tiles[b] : 0;
+      most = max(most, mine);
+      int inc = mine * p.n_kv_heads;
+#pragma unroll
+      for (int sh = 1; sh < 32; sh <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, inc, sh);
+        if (lane >= sh) inc += up;
+      }
+      if (b < p.n_seq) sm_pref[b] = sum + inc - mine * p.n_kv_heads;
+      sum += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) {
+      sm_pref[p.n_seq] = sum;
+      *sm_most = most;
+    }
+  }
+  __syncthreads();
+  const int total = sm_pref[p.n_seq], most = *sm_most;
+  for (int i = cta * kQThreads + tid; i < n_bg; i += gridDim.x * kQThreads)
+    if (sm_tiles[i / p.n_kv_heads] == 0) p.counts[i] = 0;
+  // No more CTAs than tiles, and no more than leave any head at most max_splits partials (a head of m tiles touches at
+  // most m C / total + 2 runs; without the second bound it touches at most m).
+  int C = min((int)gridDim.x, total);
+  if (most > p.max_splits) C = min(C, (int)((int64_t)(p.max_splits - 2) * total / most));
+  if (cta >= C) return;
+  const int t0 = (int)((int64_t)total * cta / C), t1 = (int)((int64_t)total * (cta + 1) / C);
+  int b = 0;   // the last sequence whose tiles begin at or before t0
+  for (int step = kQuantMaxSeq / 2; step > 0; step >>= 1)
+    if (b + step < p.n_seq && sm_pref[b + step] <= t0) b += step;
+
+  if (warp == kQWarps) {
+    // ------------------------------------------------------------ copy warp
+    if (lane == 0) {
+      uint64_t policy;
+      asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+      int it = 0;
+      for (int x = t0; x < t1;) {
+        const Piece s = piece_at(x, t1, b, sm_pref, sm_tiles);
+        b = s.b;
+        const int row = (int)(sm_row[b] + (int64_t)s.g * sm_cap[b]) + s.tile * kQuantTile;
+        for (int i = 0; i < s.count; ++i, ++it) {
+          const int st = it % kQStages, use = it / kQStages;
+          if (use > 0 && !mbar_wait(bar_empty + 8 * st, (use - 1) & 1)) {
+            atomicOr(p.status, RKV_DEV_TIMEOUT);
+            return;
+          }
+          const uint32_t dst = smem_base + st * kQStageBytes, bar = bar_full + 8 * st;
+          mbar_expect_tx(bar, kQStageBytes);
+          tma_load_codes(dst, &tm_k, row + i * kQuantTile, bar, policy);
+          tma_load_codes(dst + kQHalfBytes, &tm_v, row + i * kQuantTile, bar, policy);
+        }
+        x += s.count;
+      }
+    }
+    return;
+  }
+
+  // ---------------------------------------------------------------- MMA warps
+  const int G = p.group, band0 = kQBand * warp;
+  Consumer<kLogits> mma;
+  uint64_t keep_policy = 0;
+  if (kLogits) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep_policy));
+  auto load_query = [&](const Piece& s) {
+    uint4 qv = make_uint4(0u, 0u, 0u, 0u);
+    const int64_t head0 = ((int64_t)s.b * p.n_q_heads + (int64_t)s.g * G) * kHeadDim;
+    if (tid < G * 16) qv = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + head0) + tid);
+    return qv;
+  };
+  // lane i: the scales of the warp's half block in the piece's tile  first + i
+  auto load_scales = [&](const Piece& s, int first, float& ks, float& vs) {
+    ks = vs = 0.f;
+    const int64_t pos = (int64_t)(s.tile + first + lane) * kQuantTile + band0;
+    if (first + lane < s.count && pos < sm_cap[s.b]) {
+      const int64_t blk = (sm_row[s.b] + (int64_t)s.g * sm_cap[s.b] + pos) / kQuantBlock;
+      ks = __ldcg(p.k_scale + blk);
+      vs = __ldcg(p.v_scale + blk);
+    }
+  };
+  Piece s = piece_at(t0, t1, b, sm_pref, sm_tiles);
+  uint4 qv = load_query(s);
+  float ks_all, vs_all;
+  load_scales(s, 0, ks_all, vs_all);
+  int it = 0;
+  for (int x = t0; x < t1;) {
+    mma.reset();
+    mma.queries(qv, p.scale, sm_q, sm_qs, tid);
+    const int x_next = x + s.count;
+    Piece next = s;
+    float ks_next = 0.f, vs_next = 0.f;
+    if (x_next < t1) {   // on their way while this piece's tiles are worked on
+      next = piece_at(x_next, t1, s.b, sm_pref, sm_tiles);
+      qv = load_query(next);
+      load_scales(next, 0, ks_next, vs_next);
+    }
+    const int n = sm_len[s.b];
+    const int bg = s.b * p.n_kv_heads + s.g;
+    float* lg0 = kLogits ? p.logits + (int64_t)bg * p.logit_stride * p.gp + (lane & 3) * 2 : nullptr;
+    for (int i = 0; i < s.count; ++i, ++it) {
+      const int st = it % kQStages;
+      if (i > 0 && (i & 31) == 0) load_scales(s, i, ks_all, vs_all);
+      const float ks = __shfl_sync(0xffffffffu, ks_all, i & 31), vs = __shfl_sync(0xffffffffu, vs_all, i & 31);
+      if (!mbar_wait(bar_full + 8 * st, (it / kQStages) & 1)) {
+        if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+        break;
+      }
+      const int pos_base = (s.tile + i) * kQuantTile + band0;
+      if (pos_base < n)
+        mma.tile(smem_base + st * kQStageBytes, band0, pos_base, n, ks, vs, lg0, p.gp, keep_policy, lane);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_empty + 8 * st);
+    }
+    mma.merge(sm_merge, sm_wm, warp, lane);
+    // runs [total c / C, total (c + 1) / C): tile y lies in the one of c = ((y + 1) C - 1) / total
+    const int64_t head_at = sm_pref[s.b] + (int64_t)s.g * sm_tiles[s.b];
+    const int first = (int)(((head_at + 1) * C - 1) / total);
+    const int slot = cta - first;
+    float* part = p.partials + ((int64_t)bg * p.max_splits + slot) * PartialLayout::kFloats;
+    publish(sm_merge, G, tid, part);
+    if (tid < kMaxGroup) {
+      const float2 v = head_ml(sm_merge, G, tid);
+      float* ml = p.ml_t + (int64_t)bg * 16 * p.max_splits + slot;
+      ml[(int64_t)tid * p.max_splits] = v.x;
+      ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = v.y;
+    }
+    if (tid == 0 && s.tile == 0)
+      p.counts[bg] = (int)(((head_at + sm_tiles[s.b]) * C - 1) / total) - first + 1;
+    x = x_next;
+    s = next;
+    ks_all = ks_next;
+    vs_all = vs_next;
+  }
+}
+
+// The output from the balanced form's partials: one CTA per (head, sequence), warp w takes the partials w, w + 4, ..., a lane
+// four channels.  The number of partials, their (m, l) and the first sixteen of them come in one round trip.
+constexpr int kFoldWarps = 4, kFoldAhead = 4;
+__global__ void __launch_bounds__(32 * kFoldWarps) quant_fold_kernel(const float* __restrict__ partials,
+                                                                     const float* __restrict__ ml_t,
+                                                                     const int32_t* __restrict__ counts,
+                                                                     const int32_t* __restrict__ active, __nv_bfloat16* out,
+                                                                     int n_q_heads, int n_kv_heads, int group, int max_splits) {
+  __shared__ float sm_w[kMaxSplits], sm_red[2][kFoldWarps];
+  __shared__ __align__(16) float sm_o[kFoldWarps][kHeadDim];
+  const int h = blockIdx.x, g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t bg = (int64_t)b * n_kv_heads + g;
+  const float* po = partials + bg * max_splits * PartialLayout::kFloats + h * kHeadDim + 4 * lane;
+  const float* pm = ml_t + (bg * 16 + h) * max_splits;
+  const float* pl = pm + (int64_t)kMaxGroup * max_splits;
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  const int act = active != nullptr ? __ldcg(active + b) : 1;
+  const int count = __ldcg(counts + bg);
+  float m = tid < max_splits ? __ldcg(pm + tid) : -INFINITY, l = tid < max_splits ? __ldcg(pl + tid) : 0.f;
+  auto load = [&](int s) { return __ldcg(reinterpret_cast<const float4*>(po + (int64_t)s * PartialLayout::kFloats)); };
+  float4 v[kFoldAhead];
+#pragma unroll
+  for (int k = 0; k < kFoldAhead; ++k) {
+    const int s = warp + kFoldWarps * k;
+    v[k] = s < max_splits ? load(s) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  if (act == 0) return;
+  __nv_bfloat16* to = out + ((int64_t)b * n_q_heads + (int64_t)g * group + h) * kHeadDim;
+  if (count <= 0) {   // nothing cached: the output is defined as zero
+    to[tid] = __float2bfloat16(0.f);
+    return;
+  }
+  if (tid >= count) {   // slots of older passes
+    m = -INFINITY;
+    l = 0.f;
+  }
+  float M = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  if (lane == 0) sm_red[0][warp] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sm_red[0][0], sm_red[0][1]), fmaxf(sm_red[0][2], sm_red[0][3]));
+  const float w = (m == -INFINITY) ? 0.f : ex2((m - M) * kLog2e);
+  sm_w[tid] = w;
+  float L = l * w;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+  if (lane == 0) sm_red[1][warp] = L;
+  __syncthreads();
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& x, float e) {
+    acc.x = fmaf(x.x, e, acc.x);
+    acc.y = fmaf(x.y, e, acc.y);
+    acc.z = fmaf(x.z, e, acc.z);
+    acc.w = fmaf(x.w, e, acc.w);
+  };
+#pragma unroll
+  for (int k = 0; k < kFoldAhead; ++k)
+    if (warp + kFoldWarps * k < count) add(v[k], sm_w[warp + kFoldWarps * k]);
+#pragma unroll 8
+  for (int s = warp + kFoldWarps * kFoldAhead; s < count; s += kFoldWarps) add(load(s), sm_w[s]);
+  *reinterpret_cast<float4*>(&sm_o[warp][4 * lane]) = acc;
+  __syncthreads();
+  L = (sm_red[1][0] + sm_red[1][1]) + (sm_red[1][2] + sm_red[1][3]);
+  to[tid] = __float2bfloat16(((sm_o[0][tid] + sm_o[1][tid]) + (sm_o[2][tid] + sm_o[3][tid])) / L);
+}
+
 }  // namespace
 
 cudaError_t prepare_quant_attention() {
@@ -561,7 +857,22 @@ cudaError_t prepare_quant_attention() {
   for (auto kernel : {quant_attn_kernel<true, false>, quant_attn_kernel<false, false>, quant_attn_kernel<true, true>,
                       quant_attn_kernel<false, true>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kQSmemPair);
+  for (auto kernel : {quant_balanced_kernel<true>, quant_balanced_kernel<false>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBSmem);
   return e;
+}
+
+cudaError_t launch_quant_balanced(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_cta,
+                                  cudaStream_t st) {
+  return launch_ex(p.logits != nullptr ? quant_balanced_kernel<true> : quant_balanced_kernel<false>, dim3(n_cta),
+                   dim3(kQThreads), (size_t)kBSmem, st, 1, tm_k, tm_v, p);
+}
+
+cudaError_t launch_quant_fold(const QuantAttnParams& p, cudaStream_t st) {
+  static_assert(kMaxSplits <= 32 * kFoldWarps && kHeadDim == 32 * kFoldWarps, "one thread per partial, one per channel");
+  return launch_ex(quant_fold_kernel, dim3(p.group, p.n_kv_heads, p.n_seq), dim3(32 * kFoldWarps), 0, st, 1, p.partials, p.ml_t,
+                   p.counts, p.active, static_cast<__nv_bfloat16*>(p.out), p.n_q_heads, p.n_kv_heads, p.group,
+                   p.max_splits);
 }
 
 cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,

@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(NTS) score_kernel(const ScoreParams p) {
   const int len = __ldcg(a_len);
   const int cap = __ldg(a_cap);
   const int k_small = __ldcg(a_ks);
+  const int counted = p.split_counts != nullptr ? __ldcg(p.split_counts + bg) : gx;
   float wm[4], wl[4];                          // (m, l) for splits lane, lane + 32, ...
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(NTS) score_kernel(const ScoreParams p) {
   const Sizes sz = clamp_sizes(len, cap, p.max_len, k_small, p.k_max);
   const int n = sz.n;
   if (lo >= n) return;
-  int n_splits = (n + p.chunk - 1) / p.chunk;
+  int n_splits = p.split_counts != nullptr ? counted : (n + p.chunk - 1) / p.chunk;
   if (n_splits > gx) n_splits = gx;
 
   // log-sum-exp of every head of the group, one warp per head

@@ -271,6 +271,44 @@ def test_attention_and_scores(mods, lens, group):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("n_seq,n_kv,group,most", [(2, 1, 4, 40000), (3, 2, 7, 2500), (40, 3, 2, 1500), (256, 1, 8, 1100),
+                                                   (257, 1, 1, 1100), (300, 2, 4, 900)])
+def test_attention_ragged_batches(mods, n_seq, n_kv, group, most):
+    """Batches whose heads share CTAs: lengths from nothing to the longest, masked sequences, runs that end inside heads,
+    one head with more tiles than it may leave partials, and more sequences than the balanced form takes."""
+    rkv, runner, synth = mods
+    rng = np.random.default_rng(n_seq)
+    lens = [most] + [int(x) for x in np.exp(rng.uniform(0, np.log(most), n_seq - 1))]
+    for i in range(3, n_seq, 7):
+        lens[i] = 0
+    c = filled(synth, lens, n_kv, n_seq)
+    q = normal(gen(n_seq), n_seq, n_kv * group, 128).to(torch.bfloat16)
+    on = [0 if i % 5 == 4 else 1 for i in range(n_seq)]
+    ctx = context(rkv, n_seq, n_kv * group, n_kv, most)
+    cs = struct(rkv, c)
+    ref = reference(Host(c, n_kv), q, n_kv, lens)
+    for active, hint in ((None, 0), (i32(on), most)):
+        out = torch.full_like(q, 7.0)
+        scores = torch.full((n_seq, n_kv, most), -1.0, device="cuda")
+        ctx.quant_full_attention(q, cs, out, active=active, max_len_hint=hint)
+        ctx.score_keys(q, cs, i32([1] * n_seq), 1, active=active, scores=scores)
+        alone = torch.full_like(q, 7.0)
+        ctx.quant_full_attention(q, cs, alone, active=active, max_len_hint=hint, keep_logits=False)
+        assert torch.equal(out, alone)
+        for b, n in enumerate(lens):
+            if active is not None and not on[b]:
+                assert (out[b] == 7).all() and (scores[b] == -1).all()
+            elif n == 0:
+                assert (out[b] == 0).all()
+            else:
+                check_out(out[b], ref[b], f"sequence {b}")
+                check_scores(scores[b], ref[b][2], group, f"sequence {b}")
+                assert (scores[b, :, n:] == -1).all()
+    out = torch.full_like(q, 7.0)
+    ctx.quant_full_attention(q, cs, out, active=i32([0] * n_seq))
+    assert (out == 7).all() and ctx.device_status() == 0
+
+
 def test_attention_masked_batch_leaves_the_others(mods):
     rkv, runner, synth = mods
     lens, n_kv, group = [500, 900, 0, 64, 2000], 2, 4
@@ -347,12 +385,14 @@ def test_attention_extremes(mods, what):
     assert ctx.device_status() == 0
 
 
-def test_attention_flags(mods):
+@pytest.mark.parametrize("max_len", [512, 4096])
+def test_attention_flags(mods, max_len):
+    """(The bound decides the form: clusters, or runs balanced over the batch.)"""
     rkv, runner, synth = mods
     lens = [300, 300, 300]
     c = filled(synth, lens, 1, 41, caps=[320] * 3)
     q = normal(gen(1), 3, 4, 128).to(torch.bfloat16)
-    ctx = context(rkv, 3, 4, 1, 512)
+    ctx = context(rkv, 3, 4, 1, max_len)
     out = torch.full_like(q, 7.0)
     ref = reference(Host(c, 1), q, 1, lens)
     c.row_offset[1] += 32
