@@ -273,11 +273,13 @@ rkv_status run_attention(rkv_ctx* ctx, const void* q, const rkv_cache* cache, co
 // The pass over the 8-bit cache, in one of three forms (all write the same workspace):
 //   splits    one sequence: its tiles of 128 positions are dealt out in turn to as many CTAs per KV head as fit one wave
 //             (two to an SM); a fold launch - or the score pass - finishes the output
-//   cluster   short contexts: 1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves.
-//             Measured for 8 KV heads, cluster against splits: 4.1 / 5.0 us at 1000 positions, 4.85 / 5.1 at 2048, 6.6 / 6.05
-//             at 4096, 9.9 / 7.1 at 8192
-//   balanced  longer batches: equal runs of tiles across heads and sequences, then its own fold
-constexpr int kQuantClusterMaxLen = 2048, kQuantClusterMaxBatch = 1024;
+//   cluster   1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves.  For one sequence
+//             up to 2048 positions (8 KV heads, cluster against splits: 4.1 / 5.0 us at 1000, 4.85 / 5.1 at 2048, 6.6 / 6.05 at
+//             4096, 9.9 / 7.1 at 8192), for a batch while no CTA can get more than 8 tiles
+//   balanced  longer batches: equal runs of tiles across heads and sequences, then its own fold.  Cluster against
+//             balanced, 8 KV heads, sequences of one length / ragged below it: 8 x 2048 (4 tiles a CTA) 10.0 / 8.8 and 13.1 /
+//             10.5 us; 8 x 4096 (8 tiles) 14.7 / 13.2 and 18.1 / 13.1; 8 x 8192 (16 tiles) 24.6 / 21.4 and 27.4 / 16.9
+constexpr int kQuantClusterMaxLen = 2048, kQuantClusterMaxTiles = 8;
 struct QuantPass { int gx; bool finished; const int32_t* counts; };   // what the second half has to know
 
 rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cache* cache, const int32_t* active,
@@ -295,9 +297,13 @@ rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cach
   if (gx > ctx->max_splits) gx = ctx->max_splits;
   if (gx > tiles) gx = tiles;
   if (gx < 1) gx = 1;
-  const bool balanced = n_seq > 1 && n_seq <= rkv::kQuantMaxSeq && n_max > kQuantClusterMaxBatch;
-  const bool cluster = !balanced && (n_max <= kQuantClusterMaxLen || gx <= 8);
-  if (cluster) gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
+  const int cluster_gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
+  const int64_t most = bg * tiles;   // tiles there can be
+  const int64_t runs = most < slots ? most : slots;
+  const bool balanced = n_seq > 1 && tiles > kQuantClusterMaxTiles * cluster_gx && n_seq <= rkv::kQuantMaxSeq &&
+                        (most + bg) * (slots + 1) < (int64_t(1) << 32);   // (the kernel cuts the runs in 32 bits)
+  const bool cluster = !balanced && (n_seq > 1 || n_max <= kQuantClusterMaxLen || gx <= 8);
+  if (cluster) gx = cluster_gx;
   rkv::QuantAttnParams p;
   memset(&p, 0, sizeof(p));
   p.q = q;
@@ -331,8 +337,7 @@ rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cach
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_ATTN_FULL);
     if (balanced) {
-      const int64_t most = bg * tiles;   // tiles there can be
-      e = rkv::launch_quant_balanced(p, tm_k, tm_v, (int)(most < slots ? most : slots), st);
+      e = rkv::launch_quant_balanced(p, tm_k, tm_v, (int)runs, st);
     } else {
       e = rkv::launch_quant_attention(p, tm_k, tm_v, n_seq, gx, cluster, gx * bg <= slots, st);
     }

@@ -563,25 +563,33 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
 // ---------------------------------------------------------------------------------------------- batches: balanced form
 // The tiles of all heads of all sequences, in order, are cut into equal runs, one per CTA, in a single wave: whatever the
-// lengths, every CTA streams the same number of tiles up to one.  (With a fixed number of CTAs per (sequence, KV head) a
+// lengths, every CTA has the same work up to a tile (beginning and ending a head costs about as much as a tile, so a
+// head of m tiles counts as m + 1 units, the first of them empty).  (With a fixed number of CTAs per (sequence, KV head) a
 // ragged batch waits for its longest sequence, and the waves a finer cut needs cost more than they balance: 16 sequences
 // of up to 3000 positions, 8 heads: 16.4 us with two CTAs a head, 23.4 with 24.)  The lengths are on the device, so every
 // CTA sums them up itself.  A run covers the end of one head and the beginning of the next, or several whole ones; each
 // piece leaves one split partial, slot = CTA - first CTA of that head, and the head's first CTA records how many there
 // are.  The copy warp walks the tiles without stopping at heads; the next head's queries and scales are requested while
 // the current one's tiles are worked on.
-struct Piece {   // the tiles of one (sequence, KV head) in a CTA's run
-  int b, g, tile, count;
+struct Piece {   // the tiles of one (sequence, KV head) in a CTA's run, and the unit behind them
+  int b, g, tile, count, next;
 };
 
+// The first piece with tiles at or behind unit x of a run that ends at `end`; count = 0 when there is none.
 __device__ __forceinline__ Piece piece_at(int x, int end, int b, const int* pref, const int* tiles) {
-  while (pref[b + 1] <= x) ++b;            // (sequences without tiles are stepped over)
   Piece s;
-  s.b = b;
-  const int rem = x - pref[b];
-  s.g = rem / tiles[b];
-  s.tile = rem - s.g * tiles[b];
-  s.count = min(tiles[b] - s.tile, end - x);
+  s.count = 0;
+  while (x < end && s.count == 0) {
+    while (pref[b + 1] <= x) ++b;          // (sequences without tiles are stepped over)
+    const int units = tiles[b] + 1, rem = x - pref[b];
+    s.b = b;
+    s.g = rem / units;
+    const int unit = rem - s.g * units;
+    s.next = min(x + units - unit, end);
+    s.tile = max(unit - 1, 0);
+    s.count = s.next - x - (unit == 0 ? 1 : 0);
+    x = s.next;
+  }
   return s;
 }
 
@@ -602,7 +610,7 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
   int* sm_cap = reinterpret_cast<int*>(sm_row + kQuantMaxSeq);
   int* sm_len = sm_cap + kQuantMaxSeq;
   int* sm_tiles = sm_len + kQuantMaxSeq;                                      // of one head
-  int* sm_pref = sm_tiles + kQuantMaxSeq;                                     // tiles of all heads of the sequences before
+  int* sm_pref = sm_tiles + kQuantMaxSeq;                                     // units of all heads of the sequences before
   int* sm_most = sm_pref + kQuantMaxSeq + 1;
   if (tid == 0) {
     for (int s = 0; s < kQStages; ++s) {
@@ -650,13 +658,14 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     for (int b0 = 0; b0 < p.n_seq; b0 += 32) {
       const int b = b0 + lane, mine = b < p.n_seq ? sm_tiles[b] : 0;
       most = max(most, mine);
-      int inc = mine * p.n_kv_heads;
+      const int units = mine > 0 ? (mine + 1) * p.n_kv_heads : 0;
+      int inc = units;
 #pragma unroll
       for (int sh = 1; sh < 32; sh <<= 1) {
         const int up = __shfl_up_sync(0xffffffffu, inc, sh);
         if (lane >= sh) inc += up;
       }
-      if (b < p.n_seq) sm_pref[b] = sum + inc - mine * p.n_kv_heads;
+      if (b < p.n_seq) sm_pref[b] = sum + inc - units;
       sum += __shfl_sync(0xffffffffu, inc, 31);
     }
     most = __reduce_max_sync(0xffffffffu, most);
@@ -666,16 +675,16 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     }
   }
   __syncthreads();
-  const int total = sm_pref[p.n_seq], most = *sm_most;
+  const uint32_t total = sm_pref[p.n_seq], most = *sm_most;   // (total * gridDim.x fits 32 bits: checked on the host)
   for (int i = cta * kQThreads + tid; i < n_bg; i += gridDim.x * kQThreads)
     if (sm_tiles[i / p.n_kv_heads] == 0) p.counts[i] = 0;
-  // No more CTAs than tiles, and no more than leave any head at most max_splits partials (a head of m tiles touches at
-  // most m C / total + 2 runs; without the second bound it touches at most m).
-  int C = min((int)gridDim.x, total);
-  if (most > p.max_splits) C = min(C, (int)((int64_t)(p.max_splits - 2) * total / most));
-  if (cta >= C) return;
-  const int t0 = (int)((int64_t)total * cta / C), t1 = (int)((int64_t)total * (cta + 1) / C);
-  int b = 0;   // the last sequence whose tiles begin at or before t0
+  // No more CTAs than units, and no more than leave any head at most max_splits partials (a head of m tiles touches at
+  // most (m + 1) C / total + 2 runs; and at most m, each with a tile of it).
+  uint32_t C = min(gridDim.x, total);
+  if (most > (uint32_t)p.max_splits) C = min(C, (uint32_t)(p.max_splits - 2) * total / (most + 1));
+  if ((uint32_t)cta >= C) return;
+  const int t0 = (int)(total * (uint32_t)cta / C), t1 = (int)(total * (uint32_t)(cta + 1) / C);
+  int b = 0;   // the last sequence whose units begin at or before t0
   for (int step = kQuantMaxSeq / 2; step > 0; step >>= 1)
     if (b + step < p.n_seq && sm_pref[b + step] <= t0) b += step;
 
@@ -685,10 +694,8 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       uint64_t policy;
       asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
       int it = 0;
-      for (int x = t0; x < t1;) {
-        const Piece s = piece_at(x, t1, b, sm_pref, sm_tiles);
-        b = s.b;
-        const int row = (int)(sm_row[b] + (int64_t)s.g * sm_cap[b]) + s.tile * kQuantTile;
+      for (Piece s = piece_at(t0, t1, b, sm_pref, sm_tiles); s.count > 0; s = piece_at(s.next, t1, s.b, sm_pref, sm_tiles)) {
+        const int row = (int)(sm_row[s.b] + (int64_t)s.g * sm_cap[s.b]) + s.tile * kQuantTile;
         for (int i = 0; i < s.count; ++i, ++it) {
           const int st = it % kQStages, use = it / kQStages;
           if (use > 0 && !mbar_wait(bar_empty + 8 * st, (use - 1) & 1)) {
@@ -700,7 +707,6 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
           tma_load_codes(dst, &tm_k, row + i * kQuantTile, bar, policy);
           tma_load_codes(dst + kQHalfBytes, &tm_v, row + i * kQuantTile, bar, policy);
         }
-        x += s.count;
       }
     }
     return;
@@ -728,18 +734,17 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     }
   };
   Piece s = piece_at(t0, t1, b, sm_pref, sm_tiles);
+  if (s.count == 0) return;
   uint4 qv = load_query(s);
   float ks_all, vs_all;
   load_scales(s, 0, ks_all, vs_all);
   int it = 0;
-  for (int x = t0; x < t1;) {
+  for (;;) {
     mma.reset();
     mma.queries(qv, p.scale, sm_q, sm_qs, tid);
-    const int x_next = x + s.count;
-    Piece next = s;
+    const Piece next = piece_at(s.next, t1, s.b, sm_pref, sm_tiles);
     float ks_next = 0.f, vs_next = 0.f;
-    if (x_next < t1) {   // on their way while this piece's tiles are worked on
-      next = piece_at(x_next, t1, s.b, sm_pref, sm_tiles);
+    if (next.count > 0) {   // on their way while this piece's tiles are worked on
       qv = load_query(next);
       load_scales(next, 0, ks_next, vs_next);
     }
@@ -761,9 +766,9 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       if (lane == 0) mbar_arrive(bar_empty + 8 * st);
     }
     mma.merge(sm_merge, sm_wm, warp, lane);
-    // runs [total c / C, total (c + 1) / C): tile y lies in the one of c = ((y + 1) C - 1) / total
-    const int64_t head_at = sm_pref[s.b] + (int64_t)s.g * sm_tiles[s.b];
-    const int first = (int)(((head_at + 1) * C - 1) / total);
+    // runs [total c / C, total (c + 1) / C): unit y lies in the one of c = ((y + 1) C - 1) / total
+    const uint32_t units = sm_tiles[s.b] + 1, head_at = sm_pref[s.b] + s.g * units;
+    const int first = (int)(((head_at + 2) * C - 1) / total);   // the run of the head's first tile
     const int slot = cta - first;
     float* part = p.partials + ((int64_t)bg * p.max_splits + slot) * PartialLayout::kFloats;
     publish(sm_merge, G, tid, part);
@@ -774,8 +779,8 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = v.y;
     }
     if (tid == 0 && s.tile == 0)
-      p.counts[bg] = (int)(((head_at + sm_tiles[s.b]) * C - 1) / total) - first + 1;
-    x = x_next;
+      p.counts[bg] = (int)(((head_at + units) * C - 1) / total) - first + 1;
+    if (next.count == 0) return;
     s = next;
     ks_all = ks_next;
     vs_all = vs_next;

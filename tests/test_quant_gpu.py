@@ -271,8 +271,8 @@ def test_attention_and_scores(mods, lens, group):
     assert ctx.device_status() == 0
 
 
-@pytest.mark.parametrize("n_seq,n_kv,group,most", [(2, 1, 4, 40000), (3, 2, 7, 2500), (40, 3, 2, 1500), (256, 1, 8, 1100),
-                                                   (257, 1, 1, 1100), (300, 2, 4, 900)])
+@pytest.mark.parametrize("n_seq,n_kv,group,most", [(2, 1, 4, 40000), (3, 2, 7, 2500), (3, 2, 7, 9000), (40, 3, 2, 1500),
+                                                   (40, 3, 2, 2500), (256, 1, 8, 1100), (257, 1, 1, 1100), (300, 2, 4, 900)])
 def test_attention_ragged_batches(mods, n_seq, n_kv, group, most):
     """Batches whose heads share CTAs: lengths from nothing to the longest, masked sequences, runs that end inside heads,
     one head with more tiles than it may leave partials, and more sequences than the balanced form takes."""
@@ -385,7 +385,7 @@ def test_attention_extremes(mods, what):
     assert ctx.device_status() == 0
 
 
-@pytest.mark.parametrize("max_len", [512, 4096])
+@pytest.mark.parametrize("max_len", [512, 16384])
 def test_attention_flags(mods, max_len):
     """(The bound decides the form: clusters, or runs balanced over the batch.)"""
     rkv, runner, synth = mods
