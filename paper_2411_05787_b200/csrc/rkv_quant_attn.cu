@@ -147,119 +147,122 @@ struct Consumer {
                                        uint64_t keep_policy, int lane) {
     const float ninf = -INFINITY;
     const int qd = lane >> 2, qc = (lane & 3) * 2;   // row of an 8-row group; first of the two heads this lane holds
-          float c[kQBlocks][4], c2[kQBlocks][4];   // two accumulator chains per block
+    // this lane's row of the band in 16-byte piece  lane >> 4, swizzled (piece ^ row & 7; rows of 128 bytes): piece
+    // 2 j + (lane >> 4) is at ^ (j << 5)
+    const uint32_t at = kbase + (band0 + (lane & 15)) * kHeadDim + (((lane >> 4) ^ (lane & 7)) << 4);
+    const bool full = pos_base + kQBand <= n;
+    float c[kQBlocks][4], c2[kQBlocks][4];   // two accumulator chains per block
 #pragma unroll
-          for (int i = 0; i < kQBlocks; ++i)
+    for (int i = 0; i < kQBlocks; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) c[i][j] = c2[i][j] = 0.f;
+      for (int j = 0; j < 4; ++j) c[i][j] = c2[i][j] = 0.f;
 #pragma unroll
-          for (int cs = 0; cs < 4; ++cs) {   // 32 channels
+    for (int cs = 0; cs < 4; ++cs) {   // 32 channels
 #pragma unroll
-            for (int i = 0; i < kQBlocks; ++i) {
-              const int krow = band0 + 16 * i + (lane & 15), piece = 2 * cs + (lane >> 4);
-              uint32_t a[4];
-              ldsm_x4(a, kbase + krow * kHeadDim + ((piece ^ (krow & 7)) << 4));
-              mma_f16(c[i], codes_lo_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[0]), codes_hi_f16x2(a[1]),
-                      qb[2 * cs][0], qb[2 * cs][1]);
-              mma_f16(c2[i], codes_lo_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[2]), codes_hi_f16x2(a[3]),
-                      qb[2 * cs + 1][0], qb[2 * cs + 1][1]);
-            }
-          }
-          // one factor per head and tile; kept finite, so that a zero product stays zero (NaN scales pass)
-          float f0 = ks * qs0, f1 = ks * qs1;
-          f0 = f0 > FLT_MAX ? FLT_MAX : f0;
-          f1 = f1 > FLT_MAX ? FLT_MAX : f1;
-          float sc[kQBlocks][4];
-          float t0 = ninf, t1 = ninf;
+      for (int i = 0; i < kQBlocks; ++i) {
+        uint32_t a[4];
+        ldsm_x4(a, (at ^ (cs << 5)) + 16 * i * kHeadDim);
+        uint32_t lo[4], hi[4];
 #pragma unroll
-          for (int i = 0; i < kQBlocks; ++i) {
-            const int r0 = pos_base + 16 * i + qd, r1 = r0 + 8;
+        for (int j = 0; j < 4; ++j) e4m3x4_to_f16x4(a[j], lo[j], hi[j]);
+        mma_f16(c[i], lo[0], lo[1], hi[0], hi[1], qb[2 * cs][0], qb[2 * cs][1]);
+        mma_f16(c2[i], lo[2], lo[3], hi[2], hi[3], qb[2 * cs + 1][0], qb[2 * cs + 1][1]);
+      }
+    }
+    // one factor per head and tile; kept finite, so that a zero product stays zero (NaN scales pass)
+    float f0 = ks * qs0, f1 = ks * qs1;
+    f0 = f0 > FLT_MAX ? FLT_MAX : f0;
+    f1 = f1 > FLT_MAX ? FLT_MAX : f1;
+    float sc[kQBlocks][4];
+    float t0 = ninf, t1 = ninf;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sc[i][j] = (c[i][j] + c2[i][j]) * ((j & 1) ? f1 : f0);
-            if (kLogits) {
-              if ((qc < gp)) {
-                if (r0 < n) st_keep_f2(lg0 + (int64_t)r0 * gp, sc[i][0], sc[i][1], keep_policy);
-                if (r1 < n) st_keep_f2(lg0 + (int64_t)r1 * gp, sc[i][2], sc[i][3], keep_policy);
-              }
-            }
-            if (r0 >= n) sc[i][0] = sc[i][1] = ninf;
-            if (r1 >= n) sc[i][2] = sc[i][3] = ninf;
-            t0 = fmaxf(t0, fmaxf(sc[i][0], sc[i][2]));
-            t1 = fmaxf(t1, fmaxf(sc[i][1], sc[i][3]));
-          }
+    for (int i = 0; i < kQBlocks; ++i) {
+      const int r0 = pos_base + 16 * i + qd, r1 = r0 + 8;
 #pragma unroll
-          for (int sh = 4; sh <= 16; sh <<= 1) {
-            t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, sh));
-            t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, sh));
-          }
-          const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
-          if (__any_sync(0xffffffffu, (n0 > m0) || (n1 > m1))) {
-            const float a0 = (n0 == m0) ? 1.f : ex2((m0 - n0) * kLog2e);
-            const float a1 = (n1 == m1) ? 1.f : ex2((m1 - n1) * kLog2e);
-            l0 *= a0;
-            l1 *= a1;
+      for (int j = 0; j < 4; ++j) sc[i][j] = (c[i][j] + c2[i][j]) * ((j & 1) ? f1 : f0);
+      if (kLogits && qc < gp) {
+        if (r0 < n) st_keep_f2(lg0 + (int64_t)r0 * gp, sc[i][0], sc[i][1], keep_policy);
+        if (r1 < n) st_keep_f2(lg0 + (int64_t)r1 * gp, sc[i][2], sc[i][3], keep_policy);
+      }
+      if (!full) {
+        if (r0 >= n) sc[i][0] = sc[i][1] = ninf;
+        if (r1 >= n) sc[i][2] = sc[i][3] = ninf;
+      }
+      t0 = fmaxf(t0, fmaxf(sc[i][0], sc[i][2]));
+      t1 = fmaxf(t1, fmaxf(sc[i][1], sc[i][3]));
+    }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              o[i][0] *= a0;
-              o[i][1] *= a1;
-              o[i][2] *= a0;
-              o[i][3] *= a1;
-            }
-            m0 = n0;
-            m1 = n1;
-          }
-          if (vs > vref) {   // the same for the whole warp
-            uint32_t up = (__float_as_uint(vs) + 0x7fffffu) & 0x7f800000u;   // the next power of two, 2^126 at most
-            if (up > 0x7e800000u) up = 0x7e800000u;
-            const float a = vref * __uint_as_float(0x7f000000u - up);
-            vref = __uint_as_float(up);
-            vrcp = __uint_as_float(0x7f000000u - up);
+    for (int sh = 4; sh <= 16; sh <<= 1) {
+      t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, sh));
+      t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, sh));
+    }
+    const float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+    if (__any_sync(0xffffffffu, (n0 > m0) || (n1 > m1))) {
+      const float a0 = (n0 == m0) ? 1.f : ex2((m0 - n0) * kLog2e);
+      const float a1 = (n1 == m1) ? 1.f : ex2((m1 - n1) * kLog2e);
+      l0 *= a0;
+      l1 *= a1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i) {
+        o[i][0] *= a0;
+        o[i][1] *= a1;
+        o[i][2] *= a0;
+        o[i][3] *= a1;
+      }
+      m0 = n0;
+      m1 = n1;
+    }
+    if (vs > vref) {   // the same for the whole warp
+      uint32_t up = (__float_as_uint(vs) + 0x7fffffu) & 0x7f800000u;   // the next power of two, 2^126 at most
+      if (up > 0x7e800000u) up = 0x7e800000u;
+      const float a = vref * __uint_as_float(0x7f000000u - up);
+      vref = __uint_as_float(up);
+      vrcp = __uint_as_float(0x7f000000u - up);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) o[i][j] *= a;
-          }
-          const float vf = vs * vrcp * kPBase;
-          const float nm0 = (m0 == ninf) ? 0.f : -m0 * kLog2e;
-          const float nm1 = (m1 == ninf) ? 0.f : -m1 * kLog2e;
-          const uint32_t vbase = kbase + kQHalfBytes;
+      for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int i = 0; i < kQBlocks; ++i) {
-            const int pos_i = pos_base + 16 * i;
-            if (pos_i >= n) continue;   // the whole block lies past the end
-            const float p0 = ex2(fmaf(sc[i][0], kLog2e, nm0)), p1 = ex2(fmaf(sc[i][1], kLog2e, nm1));
-            const float p2 = ex2(fmaf(sc[i][2], kLog2e, nm0)), p3 = ex2(fmaf(sc[i][3], kLog2e, nm1));
-            l0 += p0 + p2;
-            l1 += p1 + p3;
-            // P^T as the B operand: the two 8x8 [position][head] blocks transposed inside the warp
-            const uint32_t b0 = movmatrix_t(pack_f16(p0 * vf, p1 * vf)), b1 = movmatrix_t(pack_f16(p2 * vf, p3 * vf));
-            const bool tail = pos_i + 16 > n;
-            // rows past the end may hold anything (even NaN): their codes are cleared so that 0 * x stays 0.  A register
-            // holds positions 2 t, 2 t + 1 (t = lane & 3) of the first or of the second eight.
-            uint32_t mk0 = 0xffffffffu, mk1 = 0xffffffffu;
-            if (tail) {
-              const int pa = pos_i + qc;
-              mk0 = (pa < n ? 0x0000ffffu : 0u) | (pa + 1 < n ? 0xffff0000u : 0u);
-              mk1 = (pa + 8 < n ? 0x0000ffffu : 0u) | (pa + 9 < n ? 0xffff0000u : 0u);
-            }
-            const int vrow = band0 + 16 * i + (lane & 15);
+        for (int j = 0; j < 4; ++j) o[i][j] *= a;
+    }
+    const float vf = vs * vrcp * kPBase;
+    const float nm0 = (m0 == ninf) ? 0.f : -m0 * kLog2e;
+    const float nm1 = (m1 == ninf) ? 0.f : -m1 * kLog2e;
 #pragma unroll
-            for (int sp = 0; sp < 4; ++sp) {   // two 16-channel segments
-              const int piece = 2 * sp + (lane >> 4);
-              uint32_t a[4];
-              ldsm_x4_t(a, vbase + vrow * kHeadDim + ((piece ^ (vrow & 7)) << 4));
-              if (tail) {
-                a[0] &= mk0;
-                a[1] &= mk1;
-                a[2] &= mk0;
-                a[3] &= mk1;
-              }
+    for (int i = 0; i < kQBlocks; ++i) {
+      const int pos_i = pos_base + 16 * i;
+      if (pos_i >= n) continue;   // the whole block lies past the end
+      const float p0 = ex2(fmaf(sc[i][0], kLog2e, nm0)), p1 = ex2(fmaf(sc[i][1], kLog2e, nm1));
+      const float p2 = ex2(fmaf(sc[i][2], kLog2e, nm0)), p3 = ex2(fmaf(sc[i][3], kLog2e, nm1));
+      l0 += p0 + p2;
+      l1 += p1 + p3;
+      // P^T as the B operand: the two 8x8 [position][head] blocks transposed inside the warp
+      const uint32_t b0 = movmatrix_t(pack_f16(p0 * vf, p1 * vf)), b1 = movmatrix_t(pack_f16(p2 * vf, p3 * vf));
+      const bool tail = pos_i + 16 > n;
+      // rows past the end may hold anything (even NaN): their codes are cleared so that 0 * x stays 0.  A register
+      // holds positions 2 t, 2 t + 1 (t = lane & 3) of the first or of the second eight.
+      uint32_t mk0 = 0xffffffffu, mk1 = 0xffffffffu;
+      if (tail) {
+        const int pa = pos_i + qc;
+        mk0 = (pa < n ? 0x0000ffffu : 0u) | (pa + 1 < n ? 0xffff0000u : 0u);
+        mk1 = (pa + 8 < n ? 0x0000ffffu : 0u) | (pa + 9 < n ? 0xffff0000u : 0u);
+      }
 #pragma unroll
-              for (int j = 0; j < 4; ++j) a[j] = __byte_perm(a[j], 0u, 0x3120);   // (channel, two positions) in each half
-              mma_f16(o[2 * sp], codes_lo_f16x2(a[0]), codes_hi_f16x2(a[0]), codes_lo_f16x2(a[1]), codes_hi_f16x2(a[1]), b0, b1);
-              mma_f16(o[2 * sp + 1], codes_lo_f16x2(a[2]), codes_hi_f16x2(a[2]), codes_lo_f16x2(a[3]), codes_hi_f16x2(a[3]), b0, b1);
-            }
-          }
+      for (int sp = 0; sp < 4; ++sp) {   // two 16-channel segments
+        uint32_t a[4];
+        ldsm_x4_t(a, (at ^ (sp << 5)) + kQHalfBytes + 16 * i * kHeadDim);
+        if (tail) {
+          a[0] &= mk0;
+          a[1] &= mk1;
+          a[2] &= mk0;
+          a[3] &= mk1;
+        }
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          e4m3x4_to_f16x4(__byte_perm(a[j], 0u, 0x3120), lo[j], hi[j]);   // (channel, two positions) in each half
+        mma_f16(o[2 * sp], lo[0], hi[0], lo[1], hi[1], b0, b1);
+        mma_f16(o[2 * sp + 1], lo[2], hi[2], lo[3], hi[3], b0, b1);
+      }
+    }
   }
 
   // The four warps' accumulators, scaled to the CTA-wide maximum, into sm (kMergeBytes); sm_wm: [warps][8].
