@@ -303,7 +303,8 @@ rkv_status rkv_append_small_step_evict(rkv_ctx* ctx, const void* q, const void* 
  * sequence as it is.  Rows of the buffer outside start .. start + count - 1 keep their values.
  *   k_new, v_new   bf16; head g of row t of sequence b starts at  b * seq_stride + t * tok_stride + g * 128  (elements;
  *                  strides are multiples of 8, so that rows can lie inside a projection's output)
- *   n_tok          host value >= 1: rows per sequence in k_new and v_new; count[b] above it is cut to it
+ *   n_tok          host value >= 1: rows per sequence in k_new and v_new (a padded batch's longest); count[b] above it
+ *                  is cut to it
  *   start, count   int32 [B] or NULL
  */
 rkv_status rkv_quant_store(rkv_ctx* ctx, const void* k_new, int64_t k_seq_stride, int64_t k_tok_stride,
@@ -316,8 +317,9 @@ rkv_status rkv_quant_store(rkv_ctx* ctx, const void* k_new, int64_t k_seq_stride
  * leaves the logits and softmax statistics in the workspace, and rkv_quant_select_topk (or rkv_quant_score_keys, then
  * rkv_quant_select_topk) completes the step exactly as rkv_select_topk / rkv_score_keys complete rkv_full_attention;
  * keep_logits == 0 is attention alone, without the writes that the scores need.  rkv_quant_full_step is
- * rkv_full_step over an 8-bit cache.  Other arguments as in those calls.  Two kernels (attention, fold), or three
- * (attention, scores with the fold, selection).
+ * rkv_full_step over an 8-bit cache.  Other arguments as in those calls.  The attention is one launch, or two where its
+ * split partials are folded by a second (contexts above 2048 positions, batches with more than eight tiles of 128
+ * positions for each CTA); scores and selection are one more each, as for a bf16 cache.
  */
 rkv_status rkv_quant_full_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cache* full /*host struct*/,
                                     const int32_t* active, void* out, int32_t keep_logits, int32_t max_len_hint,

@@ -344,7 +344,6 @@ rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cach
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit attention launch");
   ctx->launches += 1;
-  if (logits) ctx->hist_dirty = false;   // (the pass has cleared it)
   rkv::note_launch(st, nullptr, nullptr);
   *pass = {balanced ? ctx->max_splits : gx, cluster || balanced || fold_out, balanced ? ctx->split_counts : nullptr};
   if (cluster || (!balanced && !fold_out)) return RKV_OK;
@@ -532,7 +531,7 @@ static rkv_status full_attention_part(rkv_ctx* ctx, const void* q, const rkv_cac
     ctx->launches += 1;
     rkv::note_launch(st, nullptr, nullptr, true);
   }
-  ctx->pending_full = {true, chunk, gx, n_max, full->k, active, nullptr};
+  ctx->pending_full = {true, chunk, gx, n_max, full->k, active, nullptr, false};
   return RKV_OK;
 }
 
@@ -549,6 +548,10 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   if (k_max < 1 || k_max > ctx->cfg.max_small) return RKV_ERR_INVALID_ARG;
   int n_max, chunk, gx;
   const int32_t* counts = nullptr;
+  // A pass over an 8-bit cache clears the histogram itself.  What the host knew of it before stays what it knows after
+  // the selection has cleared it again: under stream capture nothing of this has run yet.
+  const bool clears = stage == kStageSelect ? ctx->pending_keys.clears : ctx->pending_full.clears;
+  const bool dirty_before = stage == kStageSelect ? ctx->pending_keys.dirty_before : ctx->hist_dirty;
   if (stage == kStageSelect) {
     if (!ctx->pending_keys.valid || ctx->pending_keys.k_max != k_max) return RKV_ERR_INVALID_ARG;
     n_max = ctx->pending_keys.n_max;
@@ -565,7 +568,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   // two launches: the score pass over all positions (keys, scores, histogram; folds out[] when asked to), then
   // the selection proper, one small cluster per (sequence, KV head)
   const int bg = ctx->cfg.n_seq * ctx->cfg.n_kv_heads;
-  if (ctx->hist_dirty && stage != kStageSelect) {   // an earlier score pass was never followed by its selection, which clears the histogram
+  if (ctx->hist_dirty && !clears && stage != kStageSelect) {   // an earlier score pass was never followed by its selection, which clears the histogram
     cudaError_t e0 = cudaMemsetAsync(ctx->hist, 0, (size_t)bg * rkv::kSelectBins * sizeof(uint32_t), st);
     if (e0 != cudaSuccess) return cuda_fail(ctx, e0, "histogram reset");
     ctx->hist_dirty = false;
@@ -632,7 +635,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
     if (e != cudaSuccess) return cuda_fail(ctx, e, "score launch");
     ctx->launches += 1;
     if (stage == kStageScore) {
-      ctx->pending_keys = {true, n_max, k_max, full->k, active};
+      ctx->pending_keys = {true, n_max, k_max, full->k, active, clears, dirty_before};
       rkv::note_launch(st, nullptr, nullptr);
       return RKV_OK;
     }
@@ -642,7 +645,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
     e = rkv::launch_select(sp, ctx->cfg.n_seq, cluster, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "select launch");
-  ctx->hist_dirty = false;
+  ctx->hist_dirty = clears && dirty_before;
   ctx->launches += 1;
   rkv::note_launch(st, nullptr, nullptr);
   return RKV_OK;
@@ -677,7 +680,7 @@ static rkv_status quant_attention_part(rkv_ctx* ctx, const void* q, const rkv_qu
   QuantPass pass;
   rkv_status s = run_quant_attention(ctx, q, full, active, out, n_max, logits, fold_out, st, &pass);
   if (s != RKV_OK) return s;
-  if (logits) ctx->pending_full = {true, rkv::kQuantTile, pass.gx, n_max, full->k, active, pass.counts};
+  if (logits) ctx->pending_full = {true, rkv::kQuantTile, pass.gx, n_max, full->k, active, pass.counts, true};
   *finished = pass.finished;
   return RKV_OK;
 }
@@ -728,7 +731,7 @@ rkv_status rkv_quant_store(rkv_ctx* ctx, const void* k_new, int64_t k_seq_stride
   if (!ctx || !k_new || !v_new || !quant_ok(full) || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
   if (!aligned16(k_new) || !aligned16(v_new) || ((k_seq_stride | k_tok_stride | v_seq_stride | v_tok_stride) & 7) != 0)
     return RKV_ERR_INVALID_ARG;   // the kernel reads 16 bytes at a time
-  if (n_tok < 1 || n_tok > full->n_rows) return RKV_ERR_INVALID_ARG;
+  if (n_tok < 1) return RKV_ERR_INVALID_ARG;
   const rkv::QuantNew rows = {k_new, v_new, k_seq_stride, k_tok_stride, v_seq_stride, v_tok_stride, n_tok};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;

@@ -309,9 +309,9 @@ struct rkv_ctx {
   int select_keys_per_cta;   // keys one CTA of a selection cluster takes (about): fewer = shorter chain, more = fewer CTAs
   int score_slice;           // positions per CTA of the score pass; 0: chosen per launch
   // geometry of the last rkv_full_attention, for the rkv_select_topk that completes it
-  struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; const int32_t* counts; } pending_full;
+  struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; const int32_t* counts; bool clears; } pending_full;
   // ... and of the last rkv_score_keys, for the rkv_select_topk that launches the selection alone
-  struct { bool valid; int n_max, k_max; const void* full_k; const int32_t* active; } pending_keys;
+  struct { bool valid; int n_max, k_max; const void* full_k; const int32_t* active; bool clears, dirty_before; } pending_keys;
   int gp;              // floats per position in the logit scratch
   std::string last_error;
   std::map<std::pair<uint64_t, int64_t>, CUtensorMap> tmaps;   // (base address, rows) -> tensor map

@@ -62,7 +62,7 @@ __device__ __forceinline__ uint2 encode8(uint4 w, float inv) {
 // Codes of rows below `rows` of a block again, under a scale 1 / ratio times as large.
 __device__ __forceinline__ void encode_again(uint8_t* block, int rows, float ratio, int tid) {
   for (int i = tid; i < rows * 8; i += kStoreThreads) {
-    uint4 w = reinterpret_cast<const uint4*>(block)[i];
+    uint4 w = __ldcg(reinterpret_cast<const uint4*>(block) + i);
     uint32_t* x = reinterpret_cast<uint32_t*>(&w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

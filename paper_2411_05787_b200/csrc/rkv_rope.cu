@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
   };
   load(hsub);
   if (tid < half) {
-    const long long pos = __ldg(p.pos + tok);
+    const long long pos = __ldcg(p.pos + tok);
     const unsigned long long t = (unsigned long long)pos * __ldg(p.freqs + tid);
     float s, c;
     sincospif((float)(int)(t >> 32) * 4.656612873e-10f, &s, &c);   // 2^-31: half turns

@@ -487,6 +487,44 @@ def test_selection_after_scores_without_one(mods):
     assert ctx.device_status(side) == 0
 
 
+@pytest.mark.parametrize("halves", [False, True])
+def test_captured_quant_step_leaves_the_bf16_selection_alone(mods, halves):
+    """One context for a bf16 and an 8-bit cache: scores without a selection leave keys in the histogram; a full step over
+    the 8-bit cache that is only captured has not cleared them, and the bf16 full step behind it must."""
+    rkv, runner, synth = mods
+    n = 3000
+    c = filled(synth, [n], 2, 3)
+    bf = synth.alloc_cache([n], [n], 2, torch.device("cuda"))
+    g = gen(5)
+    bf.k.copy_(normal(g, *bf.k.shape)); bf.v.copy_(normal(g, *bf.v.shape))
+    bs = rkv.cache_struct(bf.k, bf.v, bf.row_offset, bf.cap, bf.len)
+    cs = struct(rkv, c)
+    q = normal(g, 1, 8, 128).to(torch.bfloat16)
+    ctx = context(rkv, 1, 8, 2, 3072, 256)
+    out, k_small = torch.empty_like(q), i32([256])
+    idx, want = (torch.empty((1, 2, 256), dtype=torch.int32, device="cuda") for _ in range(2))
+    ctx.full_step(q, bs, k_small, 256, out, want)
+    ctx.full_attention(q, bs, out)
+    ctx.score_keys(q, bs, k_small, 256)                 # keys counted, nothing selected
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            if halves:
+                ctx.quant_full_attention(q, cs, out)
+                ctx.score_keys(q, cs, k_small, 256)
+                ctx.select_topk(None, cs, k_small, 256, idx)
+            else:
+                ctx.quant_full_step(q, cs, k_small, 256, out, idx)
+        idx.fill_(-7)
+        ctx.full_step(q, bs, k_small, 256, out, idx)
+        assert torch.equal(idx, want)
+        graph.replay()
+        ctx.full_step(q, bs, k_small, 256, out, idx)
+        assert torch.equal(idx, want)
+    assert ctx.device_status(side) == 0
+
+
 # -------------------------------------------------------------------------------------------------------------- rebuild
 @pytest.mark.parametrize("keep", [1, 63, 64, 65, 200, 1000])
 def test_rebuild_bit_exact(mods, keep):
