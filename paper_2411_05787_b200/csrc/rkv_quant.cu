@@ -11,9 +11,10 @@ namespace {
 //   code = rne(x / scale'),  needed(a) = the smallest power of two >= a / 448 (not below 2^-126).
 // One CTA per (block, KV head, sequence): all of its new rows, K and V, sit in registers (32 KB per CTA in flight,
 // 128 bytes a thread), the two maxima meet once in shared memory, then the codes leave as whole 128-byte rows.
-// HBM-bound for prompts (256 bytes read and 128 written per row and cache): 32768 rows of eight heads in 33.3 us,
-// 6.06 TB/s (512 threads a CTA 45.8 us, 128: 36.2); 2000-row chunks of four ragged sequences 4.5 us.  For single tokens
-// a chain of two round trips (sizes, then rows and scales), three when a block has to be encoded again: 2.3 us.
+// HBM-bound for prompts (256 bytes read and 128 written per row and cache): 32768 rows of eight heads in 33.4 us,
+// 6.02 TB/s (512 threads a CTA 45.8 us, 128: 36.2; without the bound of 64 registers, which costs the fourth CTA of an SM,
+// 36.1); 2000-row chunks of four ragged sequences 4.6 us.  For single tokens a chain of two round trips (sizes, then rows
+// and scales), three when a block has to be encoded again: 2.4 us.
 constexpr int kStoreThreads = 256;
 constexpr int kStorePer = kQuantBlock * 16 / kStoreThreads;   // 16-byte pieces of bf16 per thread and cache
 
@@ -73,7 +74,7 @@ __device__ __forceinline__ void encode_again(uint8_t* block, int rows, float rat
   }
 }
 
-__global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams p) {
+__global__ void __launch_bounds__(kStoreThreads, 4) store_kernel(const StoreParams p) {
   __shared__ uint32_t sm_max[2][kStoreThreads / 32];
   const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cap = p.cap[b];               // geometry: constant while calls are in flight
