@@ -3,7 +3,8 @@
 //   s[h][j] = scale ks(j) <q[h], K8[j]>,  p = softmax_j s,  out[h] = sum_j p[h][j] vs(j) V8[j],
 // K8, V8 e4m3 codes, ks, vs the scales of position j's block of 64.  The split partials, the softmax statistics and
 // the raw logits go to the same workspace, in the same layout, as those of the bf16 pass: the fold kernel, the score
-// pass and the selection behind it are the same kernels.
+// pass and the selection behind it are the same kernels.  (The first kernel below serves one sequence and short batches,
+// the second longer batches; the rule between them is where they are launched.)
 //
 // What bounds it: 256 bytes per position and KV head from HBM, half of the bf16 pass.  The shape is that pass's: one
 // CTA per (sequence, KV head, split), two to an SM, a copy warp that keeps a ring of two 32 KB stages full (one
@@ -12,15 +13,15 @@
 // slowly: 46.2 against 42.9 us at 131072 positions of eight heads), four MMA warps with 32 positions of a tile each,
 // i.e. half a block, so that a scale is one number per warp and tile.
 // Measured (attention alone, fold included): 131072 positions of eight heads 42.9 us, 6.26 TB/s; 32768: 14.7 us; 16
-// ragged sequences of up to 65535 positions, four heads of seven queries: 71.3 us, 5.76 TB/s; 1000: 4.1 us.
+// ragged sequences of up to 65535 positions, four heads of seven queries: 65.8 us, 6.25 TB/s; 1000: 4.1 us.
 //
 // Arithmetic.  Codes become halves exactly (cvt.e4m3x2) and the products run as m16n8k16 f16 MMAs with fp32
 // accumulators; the heads of the group are the N = 8 dimension.  fp8 MMAs would want q and p as e4m3, which is not
 // enough for either.  The queries are scaled by a power of two per head so that the largest element is near 2^15 and
 // every bf16 query element down to 2^-28 of it is exact as a half.  The probabilities meet V as halves
-//   p' = p vs / vref 2^13,   vref = the smallest power of two >= every vs this warp has seen,
-// so that they are normal halves (relative rounding 2^-11) down to p vs / vref = 2^-27 and never above 2^13; the
-// accumulators are rescaled when vref rises and carry vref 2^-13 until they are published.
+//   p' = p vs / vref 2^13,   vref = a power of two, at least this block's vs and at most 2^8 times as large,
+// so that they are normal halves (relative rounding 2^-11) down to p = 2^-19 at least, 2^-27 usually, and never above
+// 2^13; the accumulators are rescaled when vref moves and carry vref 2^-13 until they are published.
 // K codes are read with ldmatrix as they lie: a lane holds four consecutive channels of a row, and the order of the
 // channels in the k dimension is free as long as the query fragments use the same.  For V^T the transposed ldmatrix
 // moves pairs of channels; one byte permutation turns (two positions x two channels) into the two halves the A
@@ -44,6 +45,7 @@ constexpr int kQRow = 144;                           // halves per query row in 
 constexpr int kQOPad = 132;                          // floats per head row in the merge buffer
 constexpr int kQCluster = 8;                         // most CTAs that finish an output together
 constexpr float kPBase = 8192.f;                     // 2^13: the largest p'
+constexpr float kVrefSlack = 1.f / 256.f;            // how far a block's scale may be below the accumulators'
 static_assert(kQuantBlock % kQBand == 0, "a warp's band must not straddle two blocks");
 
 constexpr int kMergeL = kQWarps * kMaxGroup * kQOPad;          // merge buffer, in floats: o [warps][8][kQOPad],
@@ -110,6 +112,31 @@ struct Consumer {
     vrcp = 8.50705917e37f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  }
+
+  // A block of much smaller scale than the accumulators': they are brought down to it, as far as what they hold allows
+  // (up to 2^100), so that its probabilities stay normal halves and large values of little weight do not hide small ones
+  // of much.  Rare: the scales of a head's blocks seldom differ by more than a factor of a few.
+  __device__ __forceinline__ void lower_vref(float vs) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = fmaxf(m, fabsf(o[i][j]));
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
+    const int have = (int)(__float_as_uint(vref) >> 23);                       // exponent fields: powers of two
+    const int want = max((int)((__float_as_uint(vs) + 0x7fffffu) >> 23), 1);
+    int k = min(have - want, 126);
+    if (m > 0.f) k = min(k, 227 - (int)(__float_as_uint(m) >> 23));            // m 2^k <= 2^101
+    if (k <= 0) return;
+    const float a = pow2f(k);
+    vref = __uint_as_float((uint32_t)(have - k) << 23);
+    vrcp = __uint_as_float(0x7f000000u - __float_as_uint(vref));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] *= a;
   }
 
   // qv: this thread's 16 bytes of the group's query rows (16 threads to a head; zeros for heads beyond the group)
@@ -222,7 +249,7 @@ struct Consumer {
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[i][j] *= a;
-    }
+    } else if (vs < vref * kVrefSlack && vs > 0.f) lower_vref(vs);
     const float vf = vs * vrcp * kPBase;
     const float nm0 = (m0 == ninf) ? 0.f : -m0 * kLog2e;
     const float nm1 = (m1 == ninf) ? 0.f : -m1 * kLog2e;
@@ -306,7 +333,7 @@ struct Consumer {
   }
 };
 
-// Sums over the warps of what merge() left: o into to[head][128]; (m, l) of head tid to two places each.
+// Sums over the warps of what merge() left: o into to[head][128], (m, l) of one head.
 __device__ __forceinline__ void publish(const float* sm, int G, int tid, float* to) {
   for (int item = tid; item < G * 32; item += 32 * kQWarps) {   // (head, four channels)
     const float* src = sm + (item >> 5) * kQOPad + (item & 31) * 4;

@@ -385,6 +385,39 @@ def test_attention_extremes(mods, what):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("lens", [[700], [6000], [700, 350], [9000, 64, 4000]])
+@pytest.mark.parametrize("where", ["first", "last", "every other"])
+def test_attention_large_values_of_no_weight(mods, lens, where):
+    """Blocks whose values are 2^70 times as large as the others' and whose logits lie 100 nats below: they weigh nothing
+    (e^-100 2^70 = 2^-74), and must not cost the others their bits, wherever they stand."""
+    rkv, runner, synth = mods
+    n_kv, group = 2, 4
+    c = filled(synth, lens, n_kv, 61)
+    q = torch.zeros((len(lens), n_kv * group, 128), device="cuda")
+    q[..., 0], q[..., 1:] = 8.0, normal(gen(62), len(lens), n_kv * group, 127) * 0.2
+    q = q.to(torch.bfloat16)
+    k = c.k.view(torch.uint8)
+    low = int(QO.encode(np.array([-144.0]))[0])
+    for b, n in enumerate(lens):
+        blocks = (n + 63) // 64
+        for h in range(n_kv):
+            r, cap = head_rows(c, b, h)
+            k[r: r + n, 0] = 0
+            c.k_scale[r // 64: r // 64 + blocks] = 1.0
+            k[r: r + n, 1:] = 0x30                                     # 0.5: every other logit alike
+            for i in range(blocks):
+                if blocks > 1 and (i < 2 if where == "first" else i >= blocks - 2 if where == "last" else i % 2 == 0) and i != 1:
+                    k[r + 64 * i: r + min(64 * i + 64, n), 0] = low    # 8 * -144 / sqrt(128) = -101.8
+                    c.v_scale[r // 64 + i] *= 2.0 ** 70
+    ctx = context(rkv, len(lens), n_kv * group, n_kv, max(lens))
+    out = torch.empty_like(q)
+    ctx.quant_full_attention(q, struct(rkv, c), out)
+    ref = reference(Host(c, n_kv), q, n_kv, lens)
+    for b in range(len(lens)):
+        check_out(out[b], ref[b], f"sequence {b}")
+    assert ctx.device_status() == 0
+
+
 @pytest.mark.parametrize("max_len", [512, 16384])
 def test_attention_flags(mods, max_len):
     """(The bound decides the form: clusters, or runs balanced over the batch.)"""
