@@ -9,6 +9,12 @@ import torch
 from oracle import quant_oracle as QO
 
 
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    from paper_2411_05787_b200 import build
+    build.build()
+
+
 def test_grid_and_rounding_match_the_library_type():
     """The oracle's e4m3 grid and rounding against torch's conversion (an independent implementation)."""
     codes = torch.arange(256, dtype=torch.uint8)

@@ -533,7 +533,7 @@ def test_captured_quant_step_leaves_the_bf16_selection_alone(mods, halves):
     bs = rkv.cache_struct(bf.k, bf.v, bf.row_offset, bf.cap, bf.len)
     cs = struct(rkv, c)
     q = normal(g, 1, 8, 128).to(torch.bfloat16)
-    ctx = context(rkv, 1, 8, 2, 3072, 256)
+    ctx = context(rkv, 1, 8, 2, 3200, 256)
     out, k_small = torch.empty_like(q), i32([256])
     idx, want = (torch.empty((1, 2, 256), dtype=torch.int32, device="cuda") for _ in range(2))
     ctx.full_step(q, bs, k_small, 256, out, want)
@@ -698,7 +698,8 @@ def test_schedules_take_quant_layers(mods):
     for l, st in enumerate(plain):
         st.append(k[l], v[l])
         st.refresh(q[l])
-    for make, share in ((runner.DeferredRefresh, 4), (runner.OverlappedRefresh, 2)):
+    early = lambda ls: runner.DeferredRefresh(ls, early_scores=True)
+    for make, share in ((runner.DeferredRefresh, 4), (early, 4), (runner.OverlappedRefresh, 2)):
         ls = layers(share)
         torch.cuda.synchronize()
         make(ls).run(lambda l: q[l], lambda l: k[l], lambda l: v[l])
@@ -706,6 +707,48 @@ def test_schedules_take_quant_layers(mods):
         for a, b in zip(plain, ls):
             assert torch.equal(a.topk_idx, b.topk_idx) and torch.equal(a.small.k[: 128], b.small.k[: 128])
             assert (a.out.float() - b.out.float()).abs().max() <= 2.0 ** -8 * a.out.float().abs().max()   # (the fold's order)
+            assert b.ctx.device_status() == 0
+
+
+def test_checked_tokens_over_quant_layers(mods):
+    """The dynamic schedule's check token over a ragged batch: some sequences refresh, the others take the partial step,
+    under device masks, as the calls in order do."""
+    rkv, runner, synth = mods
+    n_q, n_kv, lens, layers = 8, 2, [900, 300, 1200], 3
+
+    def build(share):
+        g = gen(91)
+        ctxs = [context(rkv, 3, n_q, n_kv, 1280, 160) for _ in range(share)]
+        made = []
+        for l in range(layers):
+            st = runner.QuantLayerState(ctxs[l % share], synth.alloc_quant_cache([n + 8 for n in lens], n_kv, torch.device("cuda")),
+                                        [128, 64, 128], 8, n_q, n_kv)
+            x = normal(g, 3, max(lens), n_kv, 128).to(torch.bfloat16)
+            st.store_prompt(x, x, count=i32(lens))
+            st.refresh(normal(g, 3, n_q, 128).to(torch.bfloat16))
+            made.append(st)
+        return made
+
+    g = gen(92)
+    k, v = normal(g, layers, 3, n_kv, 128).to(torch.bfloat16), normal(g, layers, 3, n_kv, 128).to(torch.bfloat16)
+    plain = build(1)
+    q = torch.stack([st.q_last_full for st in plain])
+    q[:, 1] = normal(g, layers, n_q, 128).to(torch.bfloat16)            # the second sequence's query has moved on
+    for l, st in enumerate(plain):
+        st.check_trigger(q[l], 0.9)
+        assert st.flag.tolist() == [0, 1, 0]
+        st.append_partial(q[l], k[l], v[l], active=st.not_flag)
+        st.refresh(q[l], active=st.flag)
+    for make, share in ((runner.DeferredRefresh, layers), (runner.OverlappedRefresh, 2)):
+        ls = build(share)
+        torch.cuda.synchronize()
+        make(ls).run_checked(lambda l: q[l], lambda l: k[l], lambda l: v[l], 0.9)
+        torch.cuda.synchronize()
+        for a, b in zip(plain, ls):
+            assert b.full.len.tolist() == [n + 1 for n in lens] and torch.equal(a.small.len, b.small.len)
+            assert torch.equal(a.topk_idx, b.topk_idx) and torch.equal(a.small.k, b.small.k) and torch.equal(a.small.v, b.small.v)
+            assert torch.equal(a.full.k.view(torch.uint8), b.full.k.view(torch.uint8))
+            assert (a.out.float() - b.out.float()).abs().max() <= 2.0 ** -8 * a.out.float().abs().max()
             assert b.ctx.device_status() == 0
 
 

@@ -11,6 +11,8 @@ from oracle import quant_oracle as QO
 
 @pytest.fixture(scope="module")
 def rkv():
+    from paper_2411_05787_b200 import build
+    build.build()
     from paper_2411_05787_b200 import rkv
     return rkv
 
