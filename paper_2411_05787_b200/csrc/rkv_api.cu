@@ -277,8 +277,8 @@ rkv_status run_attention(rkv_ctx* ctx, const void* q, const rkv_cache* cache, co
 //             up to 2048 positions (8 KV heads, cluster against splits: 4.1 / 5.0 us at 1000, 4.85 / 5.1 at 2048, 6.6 / 6.05 at
 //             4096, 9.9 / 7.1 at 8192), for a batch while no CTA can get more than 8 tiles
 //   balanced  longer batches: equal runs of tiles across heads and sequences, then its own fold.  Cluster against
-//             balanced, 8 KV heads, sequences of one length / ragged below it: 8 x 2048 (4 tiles a CTA) 10.0 / 8.8 and 13.1 /
-//             10.5 us; 8 x 4096 (8 tiles) 14.7 / 13.2 and 18.1 / 13.1; 8 x 8192 (16 tiles) 24.6 / 21.4 and 27.4 / 16.9
+//             balanced, 8 KV heads, sequences of one length / ragged below it: 8 x 2048 (4 tiles a CTA) 9.0 / 8.1 and 13.1 /
+//             10.5 us; 8 x 4096 (8 tiles) 14.2 / 12.1 and 18.1 / 13.1; 8 x 8192 (16 tiles) 24.6 / 21.4 and 27.4 / 16.9
 constexpr int kQuantClusterMaxLen = 2048, kQuantClusterMaxTiles = 8;
 struct QuantPass { int gx; bool finished; const int32_t* counts; };   // what the second half has to know
 
@@ -330,7 +330,7 @@ rkv_status run_quant_attention(rkv_ctx* ctx, const void* q, const rkv_quant_cach
   p.max_splits = ctx->max_splits;
   p.max_len = n_max;
   p.scale = ctx->cfg.softmax_scale;
-  p.spec = (active == nullptr && n_seq == 1) ? 1 : 0;
+  p.spec = (active == nullptr && !balanced) ? 1 : 0;
   // as in the bf16 pass: one tile ahead of the wait behind the short merge kernel, the whole ring behind others
   if (p.spec != 0 && ctx->early_read && rkv::early_read_safe(st, cache)) p.early = rkv::last_launch_was_fold(st) ? 1 : 2;
   cudaError_t e;

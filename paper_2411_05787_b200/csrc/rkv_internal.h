@@ -147,7 +147,7 @@ struct QuantAttnParams {
   int32_t* status;
   int64_t n_rows, logit_stride;
   int32_t n_seq, n_q_heads, n_kv_heads, group, gp, max_splits, max_len;
-  int32_t spec;               // 1: first tiles may be requested before the length is read (one sequence, no mask)
+  int32_t spec;               // 1: first tiles may be requested before the length is read (no mask)
   int32_t early;              // how many of them before the dependency wait (AttnParams::early)
   float scale;
 };

@@ -402,15 +402,17 @@ quant_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   };
   uint64_t policy;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-  // One sequence and no mask: the first tiles are requested before the length has been read, as far as the host's
-  // bound says that there are any (rows past the buffer's end arrive as zeros; tiles past the length are ignored),
-  // and p.early of them before the dependency wait, when the launch before this one leaves the cache alone.
+  // Without a mask the first tiles are requested before the length has been read, as far as the host's bound says that
+  // there are any (rows past the buffer's end arrive as zeros; tiles past the length are ignored), and p.early of them
+  // before the dependency wait, when the launch before this one leaves the cache alone.  In a batch one tile only: a
+  // sequence may be much shorter than the bound (eight sequences of 2048 positions 10.0 -> 9.0 us, ragged 8.9 -> 8.1).
   int n_spec = 0, n_early = 0;
   if (p.spec != 0 && layout_ok) {
     const int room = cap < p.max_len ? cap : p.max_len;
     const int bound = (room + kQuantTile - 1) / kQuantTile;
     n_spec = bound > split ? (bound - split + n_cta - 1) / n_cta : 0;
-    if (n_spec > kQStages) n_spec = kQStages;
+    const int most = p.n_seq == 1 ? kQStages : 1;
+    if (n_spec > most) n_spec = most;
     n_early = p.early < n_spec ? p.early : n_spec;
   }
   if (tid == 32 * kQWarps)
