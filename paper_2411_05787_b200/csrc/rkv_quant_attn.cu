@@ -771,6 +771,7 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
   float ks_all, vs_all;
   load_scales(s, 0, ks_all, vs_all);
   int it = 0;
+  bool lost = false;
   for (;;) {
     mma.reset();
     mma.queries(qv, p.scale, sm_q, sm_qs, tid);
@@ -783,12 +784,13 @@ quant_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     const int n = sm_len[s.b];
     const int bg = s.b * p.n_kv_heads + s.g;
     float* lg0 = kLogits ? p.logits + (int64_t)bg * p.logit_stride * p.gp + (lane & 3) * 2 : nullptr;
-    for (int i = 0; i < s.count; ++i, ++it) {
+    for (int i = 0; i < s.count && !lost; ++i, ++it) {
       const int st = it % kQStages;
       if (i > 0 && (i & 31) == 0) load_scales(s, i, ks_all, vs_all);
       const float ks = __shfl_sync(0xffffffffu, ks_all, i & 31), vs = __shfl_sync(0xffffffffu, vs_all, i & 31);
       if (!mbar_wait(bar_full + 8 * st, (it / kQStages) & 1)) {
         if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+        lost = true;   // a copy that never came: no further waits, but the warps still meet at the merges
         break;
       }
       const int pos_base = (s.tile + i) * kQuantTile + band0;
