@@ -157,3 +157,37 @@ def test_extension_refuses_wrong_kinds():
         ctx.quant_gather_small(idx, ks, "4", _cache(rkv), rkv.RkvCache())
     with pytest.raises(ValueError):
         ctx.quant_gather_small(idx, ks, 1 << 40, _cache(rkv), rkv.RkvCache())
+
+
+def test_another_current_device_and_a_closed_context(monkeypatch):
+    """The library refuses to launch while another device is current: the call is made again on the context's own; a
+    refusal there, or of a closed context, is an error."""
+    import contextlib
+    rkv, ctx = _fake()
+    ctx._key, ctx.device = (1,) + ctx._key[1:4] + (1,), 1
+    made, on = [], []
+
+    @contextlib.contextmanager
+    def device(i):
+        on.append(i)
+        yield
+        on.pop()
+
+    monkeypatch.setattr(rkv, "_current_device", lambda: on[-1] if on else 0)
+    monkeypatch.setattr(torch.cuda, "device", device)
+
+    def call(rc_there):
+        def f(*args):
+            made.append((args, list(on)))
+            return rc_there if on else 1
+        return f
+
+    ctx._done(call(0)(7), call(0), 7)
+    assert made == [((7,), []), ((7,), [1])] and not on
+    with pytest.raises(rkv.RkvError):
+        ctx._done(1, call(1), 7)
+    made.clear()
+    ctx._key = (0,) + ctx._key[1:]
+    with pytest.raises(rkv.RkvError):
+        ctx._done(1, call(0), 7)
+    assert not made

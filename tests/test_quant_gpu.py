@@ -605,6 +605,15 @@ def test_rebuild_flags_and_any_scale(mods):
         want = torch.from_numpy(host.values("k", 0, 0, 200)[j]).float().to(torch.bfloat16)
         assert torch.equal(small.k[r].cpu(), want)
     assert (small.k[2:6] == 5).all()
+    small.cap[0] = 2                       # fewer rows than selected: cut and flagged
+    small.k.fill_(5.0)
+    ctx.quant_gather_small(i32([[[0, 1, 2, 3, 4, 5, 6, 7]]]), i32([8]), 8, struct(rkv, c), sc)
+    assert ctx.device_status() == rkv.DEV_LEN_CLAMPED
+    assert small.len.tolist() == [2] and (small.k[2:] == 5).all() and not (small.k[:2] == 5).all()
+    c.len[0] = 300                         # longer than the cache: cut and flagged
+    ctx.quant_gather_small(i32([[[199, 255, 256, 299, -1, -1, -1, -1]]]), i32([2]), 8, struct(rkv, c), sc)
+    assert ctx.device_status() == rkv.DEV_LEN_CLAMPED
+    c.len[0] = 200
     c.cap[0] = 250
     ctx.quant_gather_small(idx, i32([8]), 8, struct(rkv, c), sc)
     assert ctx.device_status() == rkv.DEV_BAD_LAYOUT
