@@ -76,22 +76,31 @@ __device__ __forceinline__ void encode_again(uint8_t* block, int rows, float rat
 
 __global__ void __launch_bounds__(kStoreThreads, 4) store_kernel(const StoreParams p) {
   __shared__ uint32_t sm_max[2][kStoreThreads / 32];
+  __shared__ int sm_sizes[3];
   const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cap = p.cap[b];               // geometry: constant while calls are in flight
   const int64_t roff = p.row_offset[b];
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
-  const int len = __ldcg(p.len + b);
-  int start = p.start != nullptr ? __ldcg(p.start + b) : len;
-  int count = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
-  // Everyone draws a ticket once it has read the length; the last one writes the new length.  (The increment is made
-  // to depend on the length, so that it cannot be issued before the load has returned.)
+  // One thread reads the sizes for its CTA and then draws a ticket, the last of which writes the new length: a ticket says
+  // that nobody in its CTA will read the sizes again.  (The increment depends on all of them - start may be the lengths
+  // themselves - so it cannot be issued before they have arrived; every warp, of idle CTAs too, takes them from shared
+  // memory.  Were each warp to read for itself, one that comes late could take the new length for its start.)
   int ticket = -1;
   if (tid == 0) {
+    const int l = __ldcg(p.len + b);
+    const int s = p.start != nullptr ? __ldcg(p.start + b) : l;
+    const int c = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
+    sm_sizes[0] = l;
+    sm_sizes[1] = s;
+    sm_sizes[2] = c;
     int one;
-    asm volatile("{\n\t.reg .b32 t;\n\tand.b32 t, %1, 0;\n\tadd.s32 %0, t, 1;\n\t}" : "=r"(one) : "r"(len));
+    asm volatile("{\n\t.reg .b32 t;\n\tand.b32 t, %1, 0;\n\tadd.s32 %0, t, 1;\n\t}" : "=r"(one) : "r"(l ^ s ^ c));
     ticket = atomicAdd(p.tickets + b, one);
   }
+  __syncthreads();
+  const int len = sm_sizes[0];
+  int start = sm_sizes[1], count = sm_sizes[2];
   int flags = 0;
   if (!quant_layout_ok(roff, cap, p.n_kv_heads, p.n_rows)) {
     flags = RKV_DEV_BAD_LAYOUT;
