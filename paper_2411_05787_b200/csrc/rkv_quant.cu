@@ -82,23 +82,19 @@ __global__ void __launch_bounds__(kStoreThreads, 4) store_kernel(const StorePara
   const int64_t roff = p.row_offset[b];
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
-  // One thread reads the sizes for its CTA and then draws a ticket, the last of which writes the new length: a ticket says
-  // that nobody in its CTA will read the sizes again.  (The increment depends on all of them - start may be the lengths
-  // themselves - so it cannot be issued before they have arrived; every warp, of idle CTAs too, takes them from shared
-  // memory.  Were each warp to read for itself, one that comes late could take the new length for its start.)
-  int ticket = -1;
+  // One thread reads the sizes for its CTA; behind the barrier, where it has had them to hand on, it draws a ticket, the
+  // last of which writes the new length.  So a ticket says that nobody in its CTA will read the sizes again - every warp,
+  // of idle CTAs too, takes them from shared memory - also where start is the tensor of the lengths itself.  (Were each
+  // warp to read for itself, one that comes late could take the new length for its start.)
   if (tid == 0) {
     const int l = __ldcg(p.len + b);
-    const int s = p.start != nullptr ? __ldcg(p.start + b) : l;
-    const int c = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
     sm_sizes[0] = l;
-    sm_sizes[1] = s;
-    sm_sizes[2] = c;
-    int one;
-    asm volatile("{\n\t.reg .b32 t;\n\tand.b32 t, %1, 0;\n\tadd.s32 %0, t, 1;\n\t}" : "=r"(one) : "r"(l ^ s ^ c));
-    ticket = atomicAdd(p.tickets + b, one);
+    sm_sizes[1] = p.start != nullptr ? __ldcg(p.start + b) : l;
+    sm_sizes[2] = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
   }
   __syncthreads();
+  int ticket = -1;
+  if (tid == 0) ticket = atomicAdd(p.tickets + b, 1);
   const int len = sm_sizes[0];
   int start = sm_sizes[1], count = sm_sizes[2];
   int flags = 0;
