@@ -198,6 +198,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   // per-sequence sizes and (MMA warps) the query fragments: independent loads, one round trip
   const int act = (p.active != nullptr) ? __ldcg(p.active + b) : 1;
   int n = __ldcg(p.len + b);
+  const int zero = (int)blockDim.y - 1;   // (blocks are one row of threads, which the compiler does not know)
   // The G query rows go through shared memory: G * 16 coalesced 16-byte loads for the whole CTA instead of
   // sixteen 4-byte loads per lane (the memory pipe's request rate, not its latency, is what those cost).
   uint32_t* sm_q = reinterpret_cast<uint32_t*>(smem_gen + kStg * kStageBytes + 16 * kStg + 16 + kRecvFloats * 4);
@@ -264,7 +265,11 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   if (!kAppend && q_row) *reinterpret_cast<uint4*>(sm_q + (tid >> 4) * kQPad + (tid & 15) * 4) = qv;
   uint32_t qb[8][2];              // B fragments of Q^T: [k = channel][n = head]
   if (warp < kMW) {
-    consumer_bar();               // the query rows are in shared memory
+    if (kAppend && !kCluster) {   // (with the copy warp, see below)
+      asm volatile("bar.sync 1, %0;" ::"r"(32 * kMW + 32 + (n & zero)) : "memory");
+    } else {
+      consumer_bar();             // the query rows are in shared memory
+    }
     // four 8x8 blocks [head][8 channels] per instruction: block m of load i is channels 32 i + 8 m .. + 7
     const uint32_t q_at = smem_u32(sm_q) + (uint32_t)(lane & 7) * (kQPad * 4) + (uint32_t)(lane >> 3) * 16u;
 #pragma unroll
@@ -276,6 +281,13 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       qb[2 * i + 1][0] = r[2];
       qb[2 * i + 1][1] = r[3];
     }
+  }
+  // Streaming form: the copy warp, too, has to have read the old length before this CTA's ticket is drawn behind the
+  // barrier above, where it arrives without waiting.  (The barrier's count depends on the length just loaded, so that no
+  // warp can arrive before its load has returned.)
+  if (kAppend && !kCluster && warp == kMW) {
+    __syncwarp();
+    asm volatile("bar.arrive 1, %0;" ::"r"(32 * kMW + 32 + (n & zero)) : "memory");
   }
   // Fused append: the lengths are bumped by the last ticket holder of the sequence.  A ticket is taken only
   // after the old lengths have been read by everyone it stands for - one per cluster, taken behind the cluster
@@ -290,8 +302,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   if (!kCluster && ticket_due) {
     // (the increment is made to depend on the lengths just loaded, so that the atomic cannot be issued before
     // those loads have returned: a ticket says "this CTA HAS read the old lengths")
-    int one;
-    asm volatile("{\n\t.reg .b32 t;\n\tand.b32 t, %1, 0;\n\tadd.s32 %0, t, 1;\n\t}" : "=r"(one) : "r"(n ^ new_len_f ^ new_len_s));
+    const int one = 1 + ((n ^ new_len_f ^ new_len_s) & zero);
     ticket_old = atomicAdd(p.len_tickets + b, one);
   }
   auto take_len_ticket = [&] {
