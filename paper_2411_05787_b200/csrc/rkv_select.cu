@@ -356,7 +356,10 @@ __global__ void __launch_bounds__(NTS) score_kernel(const ScoreParams p) {
     float M = -INFINITY;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (lane + 32 * k >= n_splits) wm[k] = -INFINITY;
+      if (lane + 32 * k >= n_splits) {   // slots of older passes: their sums may be anything, NaN too
+        wm[k] = -INFINITY;
+        wl[k] = 0.f;
+      }
       M = fmaxf(M, wm[k]);
     }
     M = warp_max_f(M);

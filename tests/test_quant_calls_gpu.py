@@ -1,9 +1,12 @@
 """The 8-bit cache's calls where they meet other calls: lengths read while they are about to change, workspaces that an
 earlier call has left its traces in, sequences that one call refuses and the next one reads."""
+import numpy as np
 import pytest
 import torch
 
-from test_quant_gpu import Host, context, gen, i32, normal, struct
+from oracle import rkv_oracle as O
+from test_quant_gpu import (Host, check_out, check_scores, context, f64, filled, gen, head_rows, i32, normal, reference as
+                            quant_reference, struct)
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +40,79 @@ def test_store_reads_lengths_before_they_change(mods, given):
             host.store(k, v, count=count)
         host.check()
     assert ctx.device_status() == 0
+
+
+# ------------------------------------------------------------------------------------- traces of earlier calls
+FORMS = {                     # sequences, positions the context takes, lengths of the healthy call
+    "bf16": (1, 20000, [700]),
+    "splits": (1, 20000, [700]),
+    "cluster": (1, 2048, [130]),
+    "balanced": (3, 20000, [900, 300, 64]),
+}
+
+
+def bf16_cache(synth, lens, caps, n_kv, seed):
+    c = synth.alloc_cache(caps, lens, n_kv, torch.device("cuda"), fill=0.0)
+    for x in (c.k, c.v):
+        x.copy_(normal(gen(seed + x.shape[0]), *x.shape).to(torch.bfloat16))
+    return c
+
+
+def reference(c, form, q, n_kv, lens):
+    if form != "bf16":
+        return quant_reference(Host(c, n_kv), q, n_kv, lens)
+    ref = []
+    for b, n in enumerate(lens):
+        rows = [int(c.row_offset[b]) + h * int(c.cap[b]) for h in range(n_kv)]
+        k, v = (np.stack([f64(x[r: r + n]) for r in rows]) for x in (c.k, c.v))
+        out, p, _ = O.decode_attention(f64(q[b]), k, v)
+        ref.append((out, O.decode_attention(f64(q[b]), k, np.abs(v))[0], p))
+    return ref
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_scores_behind_a_pass_with_nan(mods, form):
+    """A long pass over a cache with a NaN row far behind, then, on the same context, a healthy one over fewer positions:
+    its scores and its selection know nothing of the first."""
+    rkv, runner, synth = mods
+    n_seq, most, lens = FORMS[form]
+    n_kv, group, keep = 2, 4, 50
+    ctx = context(rkv, n_seq, n_kv * group, n_kv, most)
+    q = normal(gen(7), n_seq, n_kv * group, 128).to(torch.bfloat16)
+    out, idx = torch.empty_like(q), torch.empty((n_seq, n_kv, keep), dtype=torch.int32, device="cuda")
+    scores = torch.full((n_seq, n_kv, most), -1.0, device="cuda")
+    k_small = i32([keep] * n_seq)
+
+    def step(c):
+        if form == "bf16":
+            ctx.full_attention(q, rkv.cache_struct(c.k, c.v, c.row_offset, c.cap, c.len), out)
+            cs = rkv.cache_struct(c.k, c.v, c.row_offset, c.cap, c.len)
+        else:
+            cs = struct(rkv, c)
+            ctx.quant_full_attention(q, cs, out)
+        ctx.select_topk(q, cs, k_small, keep, idx, scores=scores)
+
+    long = [most] * n_seq
+    if form == "bf16":
+        c = bf16_cache(synth, long, long, n_kv, 3)
+        c.k[:] = torch.where(torch.arange(c.k.shape[0], device="cuda")[:, None] % most > most // 2, torch.nan, c.k)
+    else:
+        c = filled(synth, long, n_kv, 3, caps=[(most + 63) // 64 * 64] * n_seq)
+        for b in range(n_seq):
+            for h in range(n_kv):
+                r, cap = head_rows(c, b, h)
+                c.k.view(torch.uint8)[r + most // 2: r + most] = 0x7f
+    step(c)
+    assert ctx.device_status() & rkv.DEV_NONFINITE
+    c = bf16_cache(synth, lens, lens, n_kv, 4) if form == "bf16" else filled(synth, lens, n_kv, 4)
+    scores.fill_(-1.0)
+    step(c)
+    assert ctx.device_status() == 0
+    ref = reference(c, form, q, n_kv, lens)
+    for b, n in enumerate(lens):
+        check_scores(scores[b], ref[b][2], group, f"sequence {b}")
+        assert (scores[b, :, n:] == -1).all()
+        want = ref[b][2].reshape(n_kv, group, -1).max(axis=1)
+        for h in range(n_kv):
+            why = O.check_topk_set(want[h], min(keep, n), idx[b, h, : min(keep, n)].cpu().numpy())
+            assert why is None, why
