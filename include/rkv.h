@@ -68,7 +68,8 @@ typedef enum {
                                      a lost copy cannot hang the GPU                                          */
 
 #define RKV_DEV_BAD_LAYOUT 32     /* a sequence of an rkv_quant_cache whose row_offset or cap is no multiple of 64, or
-                                     whose rows leave the buffer: nothing is read or written for it (attention: zeros) */
+                                     whose rows leave the buffer: nothing is read or written for it, but the attention's
+                                     output is zeros and the selection's indices are all -1                   */
 
 /* score aggregation over the query heads of a group (Sec. 2.2 footnote; App. A.3, Table 6) */
 typedef enum { RKV_AGG_MAX = 0, RKV_AGG_MEAN = 1, RKV_AGG_FIRST = 2 } rkv_agg;

@@ -548,8 +548,8 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   if (k_max < 1 || k_max > ctx->cfg.max_small) return RKV_ERR_INVALID_ARG;
   int n_max, chunk, gx;
   const int32_t* counts = nullptr;
-  // A pass over an 8-bit cache clears the histogram itself.  What the host knew of it before stays what it knows after
-  // the selection has cleared it again: under stream capture nothing of this has run yet.
+  // clears: the pass was one over an 8-bit cache, which clears the histogram itself.  What the host knew of it before
+  // stays what it knows after the selection has cleared it again: under stream capture nothing of this has run yet.
   const bool clears = stage == kStageSelect ? ctx->pending_keys.clears : ctx->pending_full.clears;
   const bool dirty_before = stage == kStageSelect ? ctx->pending_keys.dirty_before : ctx->hist_dirty;
   if (stage == kStageSelect) {
@@ -606,6 +606,8 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   cp.grid_splits = gx;
   cp.split_counts = counts;
   cp.pool_half = (ctx->cfg.pool_kernel - 1) / 2;
+  cp.row_offset = full->row_offset;
+  cp.quant_rows = clears ? full->n_rows : 0;
   SelectParams sp;
   memset(&sp, 0, sizeof(sp));
   sp.keys = ctx->keys;
@@ -625,6 +627,8 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   const int cluster = rkv::select_cluster_for(n_max, ctx->select_keys_per_cta);
   sp.keys_per_thread = rkv::select_keys_per_thread(n_max, cluster);
   sp.per_fixed = ctx->cfg.n_seq == 1 ? 1 : 0;
+  sp.row_offset = full->row_offset;
+  sp.quant_rows = clears ? full->n_rows : 0;
   cudaError_t e;
   if (stage != kStageSelect) {
     ctx->hist_dirty = true;

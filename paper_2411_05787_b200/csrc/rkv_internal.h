@@ -99,6 +99,8 @@ struct ScoreParams {
   int32_t grid_splits;        // CTAs per (sequence, KV head) that launch had
   const int32_t* split_counts;   // [B*Hkv] partials of each head, or null: they follow from the length, chunk and grid_splits
   int32_t pool_half;          // (pool_kernel - 1) / 2
+  const int64_t* row_offset;  // read for an 8-bit cache, whose attention pass leaves sequences of a bad layout out
+  int64_t quant_rows;         // rows of the 8-bit cache's buffers; 0: a bf16 cache
 };
 
 struct SelectParams {
@@ -117,6 +119,8 @@ struct SelectParams {
   int32_t k_max, max_len;
   int32_t keys_per_thread;    // keys per thread of a selection CTA at the host's length bound
   int32_t per_fixed;          // 1: slices are rank * keys_per_thread * threads (one sequence); 0: cut by each sequence's own length
+  const int64_t* row_offset;  // as in ScoreParams
+  int64_t quant_rows;
 };
 
 struct CacheDev {

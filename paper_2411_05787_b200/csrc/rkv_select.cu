@@ -37,6 +37,7 @@
 #include <cstddef>
 
 #include "rkv_internal.h"
+#include "rkv_quant.cuh"
 
 namespace rkv {
 namespace {
@@ -313,6 +314,7 @@ __global__ void __launch_bounds__(NTS) score_kernel(const ScoreParams p) {
   const int len = __ldcg(a_len);
   const int cap = __ldg(a_cap);
   const int k_small = __ldcg(a_ks);
+  const int64_t roff = p.quant_rows > 0 ? __ldg(p.row_offset + b) : 0;
   const int counted = p.split_counts != nullptr ? __ldcg(p.split_counts + bg) : gx;
   float wm[4], wl[4];                          // (m, l) for splits lane, lane + 32, ...
 #pragma unroll
@@ -344,6 +346,7 @@ __global__ void __launch_bounds__(NTS) score_kernel(const ScoreParams p) {
   if (q_copy) qv = __ldcg(a_q);
 
   if (act == 0) return;
+  if (p.quant_rows > 0 && !quant_layout_ok(roff, cap, p.n_kv_heads, p.quant_rows)) return;   // (the attention pass has flagged it)
   if (q_copy) reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.q_last_full) + hrow0)[tid] = qv;
   const Sizes sz = clamp_sizes(len, cap, p.max_len, k_small, p.k_max);
   const int n = sz.n;
@@ -660,6 +663,7 @@ __global__ void __launch_bounds__(NT, 2) select_kernel(const SelectParams p) {
   const int len = __ldcg(a_len);
   const int cap = __ldg(a_cap);
   const int k_small = __ldcg(a_ks);
+  const int64_t roff = p.quant_rows > 0 ? __ldg(p.row_offset + b) : 0;
   const float anchor = (float)__ldcg(a_anchor);
   uint4 hv[2];                                 // thread t: bins 8 t .. 8 t + 7
   hv[0] = __ldcg(hg);
@@ -669,7 +673,8 @@ __global__ void __launch_bounds__(NT, 2) select_kernel(const SelectParams p) {
 #pragma unroll
   for (int u = 0; u < KU; ++u) kq[u] = kq_on[u] ? __ldcg(kg4 + u * NT + tid) : pad4;
   if (act == 0) return;   // same decision in all CTAs of the cluster
-  const Sizes sz = clamp_sizes(len, cap, p.max_len, k_small, p.k_max);
+  const bool sound = p.quant_rows == 0 || quant_layout_ok(roff, cap, p.n_kv_heads, p.quant_rows);
+  const Sizes sz = clamp_sizes(sound ? len : 0, cap, p.max_len, k_small, p.k_max);   // a bad layout: nothing to select
   const int n = sz.n, kk = sz.kk;
   for (int i = kk + rank * NT + tid; i < p.k_max; i += C * NT) idx_out[i] = -1;   // padding
   if (n == 0) return;

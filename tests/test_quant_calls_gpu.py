@@ -116,3 +116,56 @@ def test_scores_behind_a_pass_with_nan(mods, form):
         for h in range(n_kv):
             why = O.check_topk_set(want[h], min(keep, n), idx[b, h, : min(keep, n)].cpu().numpy())
             assert why is None, why
+
+
+@pytest.mark.parametrize("bad", ["cap", "offset", "outside"])
+@pytest.mark.parametrize("form", ["splits", "cluster", "cluster batch", "balanced"])
+def test_second_half_of_a_bad_layout(mods, form, bad):
+    """A sequence whose layout does not suit the blocks is left alone by the scores and by the record of its query, and
+    none of its positions is selected, although the workspace still holds a healthy pass over it."""
+    rkv, runner, synth = mods
+    n_seq, most = {"splits": (1, 20000), "cluster": (1, 2048), "cluster batch": (3, 2048), "balanced": (3, 20000)}[form]
+    n_kv, group, keep, lens, b = 2, 4, 50, [1900, 300, 700][:n_seq], n_seq // 2
+    c = filled(synth, lens, n_kv, 9)
+    ctx = context(rkv, n_seq, n_kv * group, n_kv, most)
+    q = normal(gen(7), n_seq, n_kv * group, 128).to(torch.bfloat16)
+    ref = quant_reference(Host(c, n_kv), q, n_kv, lens)
+    cs, k_small = struct(rkv, c), i32([keep] * n_seq)
+
+    def buffers():
+        return (torch.full_like(q, 7.0), torch.full((n_seq, n_kv, keep), -2, dtype=torch.int32, device="cuda"),
+                torch.full((n_seq, n_kv, most), -1.0, device="cuda"), torch.full_like(q, 5.0))
+
+    def in_one_call(out, idx, scores, last):
+        ctx.quant_full_step(q, cs, k_small, keep, out, idx, scores=scores, q_last_full=last)
+
+    def in_halves(out, idx, scores, last):
+        ctx.quant_full_attention(q, cs, out)
+        ctx.select_topk(q, cs, k_small, keep, idx, scores=scores, q_last_full=last)
+
+    def in_three(out, idx, scores, last):
+        ctx.quant_full_attention(q, cs, out)
+        ctx.score_keys(q, cs, k_small, keep, scores=scores, q_last_full=last)
+        ctx.select_topk(None, cs, k_small, keep, idx)
+
+    for call in (in_one_call, in_halves, in_three):
+        call(*buffers())                                    # every sequence in order: logits and statistics of all
+        assert ctx.device_status() == 0
+        t = {"cap": c.cap, "offset": c.row_offset, "outside": c.row_offset}[bad]
+        kept = int(t[b])
+        t[b] = {"cap": kept + 32, "offset": kept + 32, "outside": c.n_rows}[bad]
+        out, idx, scores, last = buffers()
+        call(out, idx, scores, last)
+        assert ctx.device_status() == rkv.DEV_BAD_LAYOUT
+        t[b] = kept
+        for i, n in enumerate(lens):
+            if i == b:
+                assert (out[i] == 0).all() and (idx[i] == -1).all() and (scores[i] == -1).all() and (last[i] == 5).all()
+                continue
+            check_out(out[i], ref[i], f"sequence {i}")
+            check_scores(scores[i], ref[i][2], group, f"sequence {i}")
+            assert torch.equal(last[i], q[i])
+            want = ref[i][2].reshape(n_kv, group, -1).max(axis=1)
+            for h in range(n_kv):
+                why = O.check_topk_set(want[h], keep, idx[i, h].cpu().numpy())
+                assert why is None, why
