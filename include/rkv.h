@@ -339,7 +339,8 @@ rkv_status rkv_quant_full_step(rkv_ctx* ctx, const void* q, const rkv_quant_cach
 /*
  * Rebuild of the bf16 small cache from an 8-bit full cache: rkv_gather_small with
  *   small.K[b][g][r] = bf16(code * scale) of full's position topk_idx[b][g][r]    (same for V),
- * exact for scales that are powers of two.  Bad indices, active masks and lengths as there.
+ * exact for scales that are powers of two.  Bad indices, active masks and lengths as there; a sequence whose rows leave
+ * the small cache's buffers is left out and sets RKV_DEV_BAD_LAYOUT.
  */
 rkv_status rkv_quant_gather_small(rkv_ctx* ctx, const int32_t* topk_idx, const int32_t* k_small, int32_t k_max,
                                   const rkv_quant_cache* full /*host struct*/, const rkv_cache* small_cache /*host struct*/,

@@ -760,8 +760,8 @@ rkv_status rkv_quant_gather_small(rkv_ctx* ctx, const int32_t* topk_idx, const i
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_GATHER);
-    e = rkv::launch_quant_gather(topk_idx, k_small, k_max, dev_of(full), dev_of(small_cache), active, ctx->cfg.n_seq,
-                                 ctx->cfg.n_kv_heads, ctx->status, st);
+    e = rkv::launch_quant_gather(topk_idx, k_small, k_max, dev_of(full), dev_of(small_cache), small_cache->n_rows, active,
+                                 ctx->cfg.n_seq, ctx->cfg.n_kv_heads, ctx->status, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "8-bit gather launch");
   ctx->launches += 1;

@@ -161,8 +161,8 @@ cudaError_t launch_quant_attention(const QuantAttnParams& p, const CUtensorMap& 
 cudaError_t launch_quant_store(const QuantNew& rows, const int32_t* start, const int32_t* count, const QuantDev& c,
                                int n_seq, int n_kv_heads, int32_t* tickets, int32_t* status, cudaStream_t st);
 cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small, int k_max, const QuantDev& full,
-                                const CacheDev& small_cache, const int32_t* active, int n_seq, int n_kv_heads,
-                                int32_t* status, cudaStream_t st);
+                                const CacheDev& small_cache, int64_t small_rows, const int32_t* active, int n_seq,
+                                int n_kv_heads, int32_t* status, cudaStream_t st);
 cudaError_t launch_quant_balanced(const QuantAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_cta,
                                   cudaStream_t st);
 cudaError_t launch_quant_fold(const QuantAttnParams& p, cudaStream_t st);   // out from the balanced form's partials

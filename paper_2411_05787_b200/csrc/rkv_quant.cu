@@ -240,7 +240,7 @@ __device__ __forceinline__ uint4 decode8(uint2 w, float scale) {
 
 __global__ void __launch_bounds__(kGatherThreads) quant_gather_kernel(const int32_t* __restrict__ topk_idx,
                                                                      const int32_t* __restrict__ k_small, int k_max,
-                                                                     QuantDev full, CacheDev small_cache,
+                                                                     QuantDev full, CacheDev small_cache, int64_t small_rows,
                                                                      const int32_t* __restrict__ active, int n_kv_heads,
                                                                      int32_t* status) {
   const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x;
@@ -251,7 +251,8 @@ __global__ void __launch_bounds__(kGatherThreads) quant_gather_kernel(const int3
   const int cap_s = small_cache.cap[b], cap_f = full.cap[b];
   const int64_t roff_f = full.row_offset[b];
   const int64_t src0 = roff_f + (int64_t)g * cap_f;
-  const int64_t dst0 = small_cache.row_offset[b] + (int64_t)g * cap_s;
+  const int64_t roff_s = small_cache.row_offset[b];
+  const int64_t dst0 = roff_s + (int64_t)g * cap_s;
   const int32_t* idx = topk_idx + (int64_t)(b * n_kv_heads + g) * k_max;
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
@@ -265,7 +266,8 @@ __global__ void __launch_bounds__(kGatherThreads) quant_gather_kernel(const int3
     j[u] = r < k_max ? __ldcg(idx + r) : -1;
   }
   if (act == 0) return;
-  if (!quant_layout_ok(roff_f, cap_f, n_kv_heads, full.n_rows)) {
+  const bool fits = roff_s >= 0 && cap_s >= 0 && roff_s + (int64_t)n_kv_heads * cap_s <= small_rows;
+  if (!fits || !quant_layout_ok(roff_f, cap_f, n_kv_heads, full.n_rows)) {
     if (tid == 0 && blockIdx.x == 0) atomicOr(status, RKV_DEV_BAD_LAYOUT);
     return;
   }
@@ -347,11 +349,11 @@ cudaError_t launch_quant_store(const QuantNew& rows, const int32_t* start, const
 }
 
 cudaError_t launch_quant_gather(const int32_t* topk_idx, const int32_t* k_small, int k_max, const QuantDev& full,
-                                const CacheDev& small_cache, const int32_t* active, int n_seq, int n_kv_heads,
-                                int32_t* status, cudaStream_t st) {
+                                const CacheDev& small_cache, int64_t small_rows, const int32_t* active, int n_seq,
+                                int n_kv_heads, int32_t* status, cudaStream_t st) {
   dim3 grid((k_max + kGatherRows - 1) / kGatherRows, n_kv_heads, n_seq);
   return launch_ex(quant_gather_kernel, grid, dim3(kGatherThreads), 0, st, 1, topk_idx, k_small, k_max, full, small_cache,
-                   active, n_kv_heads, status);
+                   small_rows, active, n_kv_heads, status);
 }
 
 }  // namespace rkv

@@ -184,6 +184,24 @@ static int quant_cache(PyObject* o, const Key* k, rkv_quant_cache* c) {
   }
   return 0;
 }
+/* The small cache's tensors are on the context's device and describe its sequences (the kernel writes where they say). */
+static int small_cache_fits(PyObject* o, const Key* k) {
+  long long device, n_seq;
+  if (attr_ll(o, s_device, &device) != 0 || attr_ll(o, s_n_seq, &n_seq) != 0) {
+    if (PyErr_ExceptionMatches(PyExc_AttributeError))
+      PyErr_SetString(PyExc_ValueError, "the small cache is one that cache_struct describes");
+    return -1;
+  }
+  if (device != k->device) {
+    PyErr_SetString(PyExc_ValueError, "the small cache is on another device than the context");
+    return -1;
+  }
+  if (n_seq < k->n_seq) {
+    PyErr_SetString(PyExc_ValueError, "the small cache holds fewer sequences than the context");
+    return -1;
+  }
+  return 0;
+}
 
 static int stream_of(PyObject* o, long device, void** out) {
   PyObject* r;
@@ -330,7 +348,7 @@ static PyObject* quant_gather_small(PyObject* self, PyObject* const* a, Py_ssize
   void *idx, *k_small, *active, *st;
   int32_t k_max;
   if (count_args(n, 8) || as_key(a[0], &k) || quant_cache(a[4], &k, &full) ||
-      structure(a[5], c_cache, "an RkvCache", &small, sizeof(small)) || as_i32(a[3], &k_max) ||
+      structure(a[5], c_cache, "an RkvCache", &small, sizeof(small)) || as_i32(a[3], &k_max) || small_cache_fits(a[5], &k) ||
       indices(a[1], &k, k_max, &idx) || per_seq(a[2], &k, kRequired, &k_small) || per_seq(a[6], &k, kOptional, &active) ||
       stream_of(a[7], k.device, &st))
     return NULL;

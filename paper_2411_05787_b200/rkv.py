@@ -168,7 +168,11 @@ def cache_struct(k, v, row_offset, cap, length) -> RkvCache:
     """Describe a packed K/V cache (see include/rkv.h).  The caller keeps the tensors alive."""
     assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.shape == v.shape and k.shape[-1] == 128
     assert row_offset.dtype == torch.int64 and cap.dtype == torch.int32 and length.dtype == torch.int32
-    return RkvCache(_ptr(k), _ptr(v), k.numel() // 128, _ptr(row_offset), _ptr(cap), _ptr(length))
+    c = RkvCache(_ptr(k), _ptr(v), k.numel() // 128, _ptr(row_offset), _ptr(cap), _ptr(length))
+    # what the 8-bit cache's rebuild checks: the GPU of all of these tensors (-1: more than one), the sequences they describe
+    c.device = k.device.index if all(t.device == k.device for t in (v, row_offset, cap, length)) else -1
+    c.n_seq = min(row_offset.numel(), cap.numel(), length.numel())
+    return c
 
 
 def quant_cache_struct(k8, v8, k_scale, v_scale, row_offset, cap, length) -> RkvQuantCache:

@@ -169,3 +169,31 @@ def test_second_half_of_a_bad_layout(mods, form, bad):
             for h in range(n_kv):
                 why = O.check_topk_set(want[h], keep, idx[i, h].cpu().numpy())
                 assert why is None, why
+
+
+# -------------------------------------------------------------------------------------------------------------- rebuild
+@pytest.mark.parametrize("bad", ["before", "behind", "last head", "capacity"])
+def test_rebuild_leaves_rows_outside_the_small_cache_alone(mods, bad):
+    """A small cache whose sequence does not lie inside its buffers: flagged, nothing of that sequence is written."""
+    rkv, runner, synth = mods
+    n_kv, keep, b = 2, 20, 1
+    c = filled(synth, [200, 300], n_kv, 5)
+    small = synth.alloc_cache([32, 32], [7, 7], n_kv, torch.device("cuda"), fill=5.0)
+    whole = small.k                                        # 128 rows, of which the struct says fewer where rows are cut
+    ctx = context(rkv, 2, n_kv, n_kv, 512, keep)
+    rows = 128 if bad in ("before", "capacity") else 127
+    if bad == "before":
+        small.row_offset[b] = -32
+    elif bad == "behind":
+        small.row_offset[b] = 65
+    elif bad == "capacity":
+        small.cap[b] = 33
+    sc = rkv.cache_struct(small.k[:rows], small.v[:rows], small.row_offset, small.cap, small.len)
+    idx = torch.arange(keep, dtype=torch.int32, device="cuda").repeat(2, n_kv, 1).contiguous()
+    ctx.quant_gather_small(idx, i32([keep, keep]), keep, struct(rkv, c), sc)
+    assert ctx.device_status() == rkv.DEV_BAD_LAYOUT
+    assert small.len.tolist() == [keep, 7] and (whole[64:] == 5).all() and (small.v[64:] == 5).all()
+    host = Host(c, n_kv)
+    for h in range(n_kv):
+        want = torch.from_numpy(host.values("k", 0, h, 200)[:keep]).float().to(torch.bfloat16)
+        assert torch.equal(whole[32 * h: 32 * h + keep].cpu(), want)
