@@ -131,11 +131,6 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
-try:
-    from . import _rkv_calls as _calls     # links the librkv.so loaded above
-except ImportError as e:
-    raise ImportError(f"the binding's extension cannot be loaded ({e}): build it first "
-                      "(python -m paper_2411_05787_b200.build)") from e
 
 
 class RkvError(RuntimeError):
@@ -155,7 +150,8 @@ def _ptr(t):
     return t.data_ptr()
 
 
-_current_device = torch._C._cuda_getDevice
+def _current_device() -> int:
+    return torch.cuda.current_device()
 
 
 def _stream(stream):
@@ -224,9 +220,26 @@ class RopeTable:
         self.freqs = torch.tensor(signed, dtype=torch.int64).to(device)
 
 
-# what the extension's checks compare with; the last: cudaStream_t of a device's current stream
-_calls.setup(torch.bfloat16, torch.float32, torch.int32, RkvQuantCache, RkvCache, RopeTable,
-             torch._C._cuda_getCurrentRawStream)
+class _LazyCalls:
+    """Stands for the extension until its first call: the bf16 calls need neither it nor a host compiler to build it."""
+
+    def __getattr__(self, name):
+        global _calls
+        try:
+            from . import _rkv_calls     # links the librkv.so loaded above
+        except ImportError as e:
+            raise ImportError(f"the binding's extension cannot be loaded ({e}): build it first "
+                              "(python -m paper_2411_05787_b200.build)") from e
+        # what its checks compare with; the last: cudaStream_t of a device's current stream
+        raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw_stream is None:
+            raw_stream = lambda device: torch.cuda.current_stream(device).cuda_stream
+        _rkv_calls.setup(torch.bfloat16, torch.float32, torch.int32, RkvQuantCache, RkvCache, RopeTable, raw_stream)
+        _calls = _rkv_calls
+        return getattr(_rkv_calls, name)
+
+
+_calls = _LazyCalls()
 
 
 def small_step_noalloc(cfg: RkvConfig, q, small: RkvCache, out, active=None, max_len_hint=0, device_status=None,
