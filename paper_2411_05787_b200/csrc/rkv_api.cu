@@ -406,6 +406,13 @@ void note_quant_store(cudaStream_t st, const rkv_quant_cache* c) {
   add_ranges(&new_launch(st, false).writes, c);
 }
 
+void note_rows(cudaStream_t st, std::initializer_list<std::pair<const void*, size_t>> writes) {
+  std::lock_guard<std::mutex> lock(g_writes_mu);
+  LastLaunch& v = new_launch(st, false);
+  for (const auto& w : writes)
+    if (w.first != nullptr) v.writes.push_back({reinterpret_cast<uintptr_t>(w.first), reinterpret_cast<uintptr_t>(w.first) + w.second});
+}
+
 bool last_launch_was_fold(cudaStream_t st) {
   std::lock_guard<std::mutex> lock(g_writes_mu);
   auto it = g_writes.find(st);
@@ -829,7 +836,9 @@ rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "rotary launch");
   ctx->launches += 1;
-  rkv::note_launch(st, nullptr, nullptr);
+  // with one KV head the outputs can be a cache's own rows
+  const size_t q_bytes = (size_t)n_tok * n_q * rkv::kHeadDim * 2, kv_bytes = (size_t)n_tok * n_kv * rkv::kHeadDim * 2;
+  rkv::note_rows(st, {{q, q_bytes}, {k, kv_bytes}, {v, kv_bytes}});
   return RKV_OK;
 }
 

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
 #include <string>
 #include <map>
 #include <utility>
@@ -245,6 +246,7 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 // library starts).
 void note_launch(cudaStream_t st, const rkv_cache* a, const rkv_cache* b, bool fold = false);
 bool early_read_safe(cudaStream_t st, const rkv_cache* c);
+void note_rows(cudaStream_t st, std::initializer_list<std::pair<const void*, size_t>> writes);   // ... these bytes (NULL: none)
 void note_quant_store(cudaStream_t st, const rkv_quant_cache* c);   // the last launch writes rows of an 8-bit cache
 bool early_read_safe(cudaStream_t st, const rkv_quant_cache* c);
 bool last_launch_was_fold(cudaStream_t st);   // the library's last launch on the stream was the full step's merge kernel

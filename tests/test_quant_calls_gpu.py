@@ -197,3 +197,31 @@ def test_rebuild_leaves_rows_outside_the_small_cache_alone(mods, bad):
     for h in range(n_kv):
         want = torch.from_numpy(host.values("k", 0, h, 200)[:keep]).float().to(torch.bfloat16)
         assert torch.equal(whole[32 * h: 32 * h + keep].cpu(), want)
+
+
+# ------------------------------------------------------------------------------------------------------------- rotation
+def test_attention_right_behind_a_rotation_into_the_cache(mods):
+    """With one KV head, rkv_rope's keys and values can be the rows of a bf16 cache themselves.  The attention behind it
+    may request its first tiles ahead only of launches that leave the cache alone, which this one does not."""
+    rkv, runner, synth = mods
+    n, group = 4096, 4
+    c = synth.alloc_cache([n], [n], 1, torch.device("cuda"), fill=0.0)
+    cs = rkv.cache_struct(c.k, c.v, c.row_offset, c.cap, c.len)
+    ctx = context(rkv, 1, group, 1, n)
+    g, pos, table = gen(3), torch.arange(n, dtype=torch.int32, device="cuda"), rkv.RopeTable(device="cuda")
+    q = torch.empty((n, group, 128), dtype=torch.bfloat16, device="cuda")
+    qkv = [(normal(g, n, (group + 2) * 128) * s).to(torch.bfloat16) for s in (1.0, 2.0, 0.5)]
+
+    def run(x, wait):
+        ctx.rope(x, pos, table, q, c.k.view(n, 1, 128), c.v.view(n, 1, 128))
+        if wait:
+            torch.cuda.synchronize()
+        out = torch.empty((1, group, 128), dtype=torch.bfloat16, device="cuda")
+        ctx.full_attention(q[-1:], cs, out)
+        return out
+
+    want = [run(x, True) for x in qkv]
+    got = [run(x, False) for _ in range(20) for x in qkv]
+    for i, out in enumerate(got):
+        assert torch.equal(out, want[i % 3])
+    assert ctx.device_status() == 0
