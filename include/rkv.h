@@ -301,7 +301,12 @@ rkv_status rkv_append_small_step_evict(rkv_ctx* ctx, const void* q, const void* 
  *   code   = rne(x / scale'), rne = round to nearest even on the e4m3 grid.
  * NaN and infinities are stored as NaN and set RKV_DEV_NONFINITE.  Rows beyond cap[b] are dropped and set
  * RKV_DEV_APPEND_OVERFLOW; start[b] outside 0 .. min(len[b], cap[b]) sets RKV_DEV_LEN_CLAMPED and leaves the
- * sequence as it is.  Rows of the buffer outside start .. start + count - 1 keep their values.
+ * sequence as it is.  Rows of blocks that receive none keep their values.  In a block that does:
+ *   rows below start[b]  are encoded again where its scale rises, as above: a code that becomes subnormal (below 2^-6
+ *                        scale') loses bits, and values up to 2^-10 scale' become zero.  The scale does not fall again
+ *                        when rows are given up, so an outlier in a rejected draft leaves its block's kept rows coarser;
+ *   rows behind the new end  are undefined (their codes stay, their scale may not).
+ * A kept scale that is no power of two (not one of this call's) divides by a product with its reciprocal.
  *   k_new, v_new   bf16; head g of row t of sequence b starts at  b * seq_stride + t * tok_stride + g * 128  (elements;
  *                  strides are multiples of 8, so that rows can lie inside a projection's output)
  *   n_tok          host value >= 1: rows per sequence in k_new and v_new (a padded batch's longest); count[b] above it

@@ -276,9 +276,21 @@ rkv_status run_attention(rkv_ctx* ctx, const void* q, const rkv_cache* cache, co
 //   cluster   1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves.  For one sequence
 //             up to 2048 positions (8 KV heads, cluster against splits: 4.1 / 5.0 us at 1000, 4.85 / 5.1 at 2048, 6.6 / 6.05 at
 //             4096, 9.9 / 7.1 at 8192), for a batch while no CTA can get more than 8 tiles
-//   balanced  longer batches: equal runs of tiles across heads and sequences, then its own fold.  Cluster against
-//             balanced, 8 KV heads, sequences of one length / ragged below it: 8 x 2048 (4 tiles a CTA) 9.0 / 8.1 and 13.1 /
-//             10.5 us; 8 x 4096 (8 tiles) 14.2 / 12.1 and 18.1 / 13.1; 8 x 8192 (16 tiles) 24.6 / 21.4 and 27.4 / 16.9
+//   balanced  longer batches: equal runs of tiles across heads and sequences, then its own fold
+// Which of the two is faster for a batch depends on how its lengths differ, which only the device knows, and on how much
+// of the chip the clusters fill; the bound of 8 tiles a CTA goes by neither.  Cluster against balanced in us (attention
+// alone, 4 queries a head; ragged: spread evenly below the largest; * the form that is taken):
+//   tiles a CTA (few heads)          2              4              8             16
+//   positions                      2048           4096           8192          16384
+//   2 x 4 heads, one length    *5.1 /  6.8    *6.9 /  8.7   *10.2 /  9.4    17.0 / *13.4
+//                    ragged    *5.0 /  6.1    *6.8 /  7.4   *10.1 /  9.2    16.8 / *10.9
+//   2 x 1 head,  one length    *4.9 /  6.7    *6.7 /  7.8   *10.0 /  8.4    16.6 / *10.3
+//                    ragged    *4.8 /  6.1    *6.6 /  6.9    *9.9 /  7.3    16.5 /  *9.2
+//   8 x 8 heads, one length    *8.8 / 13.0   *14.0 / 17.8    23.7 / *27.3   42.6 / *46.1
+//                    ragged    *7.9 / 10.7   *12.8 / 14.4    21.2 / *20.1   38.3 / *32.2
+//   tiles a CTA (8 x 8)              4              8             16             32
+// So at 8 tiles a CTA clusters that leave most of the chip empty lose 8 to 36 % to the balanced form, and from 16 on it
+// loses 8 to 15 % to them on a full batch of one length, for not waiting for the longest sequence of a ragged one.
 constexpr int kQuantClusterMaxLen = 2048, kQuantClusterMaxTiles = 8;
 struct QuantPass { int gx; bool finished; const int32_t* counts; };   // what the second half has to know
 
