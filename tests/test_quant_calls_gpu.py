@@ -225,3 +225,75 @@ def test_attention_right_behind_a_rotation_into_the_cache(mods):
     for i, out in enumerate(got):
         assert torch.equal(out, want[i % 3])
     assert ctx.device_status() == 0
+
+
+# -------------------------------------------------------------------------------------------------------- other calls
+@pytest.mark.parametrize("order", ["tokens first", "one row for all", "batch of one"])
+def test_store_rows_in_other_orders(mods, order):
+    """Sequences that lie closer than tokens do, a batch that repeats one sequence's rows, strides that are never taken."""
+    rkv, runner, synth = mods
+    n_kv, T, g = 3, 100, gen(17)
+    B = 1 if order == "batch of one" else 3
+    if order == "tokens first":
+        k, v = (normal(g, T, B, n_kv, 128).to(torch.bfloat16).transpose(0, 1) for _ in range(2))
+        assert k.stride(0) < k.stride(1)
+    elif order == "one row for all":
+        k, v = (normal(g, 1, T, n_kv, 128).to(torch.bfloat16).expand(B, T, n_kv, 128) for _ in range(2))
+    else:
+        wide = normal(g, T, 2, n_kv, 128).to(torch.bfloat16)
+        k, v = (wide[None, :, i].as_strided((1, T, n_kv, 128), (7, 2 * n_kv * 128, 128, 1), i * n_kv * 128) for i in range(2))
+    c = synth.alloc_quant_cache([200] * B, n_kv, torch.device("cuda"))
+    ctx, host = context(rkv, B, n_kv, n_kv, 256), Host(c, n_kv)
+    for count in ([T, 63, 1][:B], [5, 37, T][:B]):
+        ctx.quant_store(k, v, struct(rkv, c), count=i32(count))
+        host.store(k, v, count=count)
+        host.check()
+    assert ctx.device_status() == 0
+
+
+def test_balanced_pass_captured_and_replayed(mods):
+    """Two graphs of a full step over a batch in the balanced form, on one workspace, replayed in turn while the lengths
+    grow and shrink on the device: each replay as the eager call on a context of its own."""
+    rkv, runner, synth = mods
+    n_kv, group, keep, most = 2, 4, 100, 9000
+    lens = [[9000, 1, 3000], [128, 0, 8999], [6000, 6000, 6000], [1, 1, 129]]
+    side = torch.cuda.Stream()
+    shared, own = (context(rkv, 3, n_kv * group, n_kv, most, 128) for _ in range(2))
+    k_small, steps = i32([keep] * 3), []
+    for seed in (1, 2):
+        c = filled(synth, [most] * 3, n_kv, seed)
+        q = normal(gen(seed), 3, n_kv * group, 128).to(torch.bfloat16)
+
+        def buffers():
+            return (torch.zeros_like(q), torch.zeros((3, n_kv, 128), dtype=torch.int32, device="cuda"),
+                    torch.zeros((3, n_kv, most), device="cuda"))
+
+        def step(ctx, t, q=q, cs=struct(rkv, c)):
+            ctx.quant_full_attention(q, cs, t[0])
+            ctx.score_keys(q, cs, k_small, 128, scores=t[2])
+            ctx.select_topk(None, cs, k_small, 128, t[1])
+
+        kept, eager = buffers(), buffers()
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.current_stream())
+            step(shared, kept)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                step(shared, kept)
+        step(own, eager)               # (the same calls on both sides: scores past a length stay what an earlier call wrote)
+        torch.cuda.synchronize()
+        steps.append((c, step, graph, kept, eager))
+    for ns in lens + lens[::-1]:
+        for c, step, graph, kept, eager in steps:
+            c.len.copy_(i32(ns))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _, _, graph, _, _ in steps:
+                graph.replay()
+        for _, step, _, _, eager in steps:
+            step(own, eager)
+        torch.cuda.synchronize()
+        for _, _, _, kept, eager in steps:
+            for a, b in zip(kept, eager):
+                assert torch.equal(a, b)
+    assert shared.device_status() == 0 and own.device_status() == 0
