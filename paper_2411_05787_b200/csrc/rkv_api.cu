@@ -216,6 +216,8 @@ rkv_status run_attention(rkv_ctx* ctx, const void* q, const rkv_cache* cache, co
   p.tickets = ctx->tickets;
   p.ml_t = ctx->ml_t;
   p.logits = logits ? ctx->logits : nullptr;
+  p.hist = ctx->hist;
+  p.anchor = ctx->anchor;
   p.status = ctx->status;
   p.logit_stride = ctx->logit_stride;
   p.n_q_heads = ctx->cfg.n_q_heads;
@@ -506,7 +508,6 @@ rkv_status rkv_create(const rkv_config* cfg, rkv_ctx** out) {
   ctx->hist = reinterpret_cast<uint32_t*>(ctx->workspace + w.hist);   // zeroed with the rest of the workspace above
   ctx->anchor = reinterpret_cast<int32_t*>(ctx->workspace + w.anchor);
   ctx->split_counts = reinterpret_cast<int32_t*>(ctx->workspace + w.counts);
-  ctx->hist_dirty = false;
   ctx->pending_keys.valid = false;
   ctx->pending_full.valid = false;
   ctx->logits = reinterpret_cast<float*>(ctx->workspace + w.logits);
@@ -567,10 +568,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   if (k_max < 1 || k_max > ctx->cfg.max_small) return RKV_ERR_INVALID_ARG;
   int n_max, chunk, gx;
   const int32_t* counts = nullptr;
-  // clears: the pass was one over an 8-bit cache, which clears the histogram itself.  What the host knew of it before
-  // stays what it knows after the selection has cleared it again: under stream capture nothing of this has run yet.
-  const bool clears = stage == kStageSelect ? ctx->pending_keys.clears : ctx->pending_full.clears;
-  const bool dirty_before = stage == kStageSelect ? ctx->pending_keys.dirty_before : ctx->hist_dirty;
+  const bool quant = stage == kStageSelect ? ctx->pending_keys.quant : ctx->pending_full.quant;   // an 8-bit cache's pass
   if (stage == kStageSelect) {
     if (!ctx->pending_keys.valid || ctx->pending_keys.k_max != k_max) return RKV_ERR_INVALID_ARG;
     n_max = ctx->pending_keys.n_max;
@@ -587,11 +585,6 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   // two launches: the score pass over all positions (keys, scores, histogram; folds out[] when asked to), then
   // the selection proper, one small cluster per (sequence, KV head)
   const int bg = ctx->cfg.n_seq * ctx->cfg.n_kv_heads;
-  if (ctx->hist_dirty && !clears && stage != kStageSelect) {   // an earlier score pass was never followed by its selection, which clears the histogram
-    cudaError_t e0 = cudaMemsetAsync(ctx->hist, 0, (size_t)bg * rkv::kSelectBins * sizeof(uint32_t), st);
-    if (e0 != cudaSuccess) return cuda_fail(ctx, e0, "histogram reset");
-    ctx->hist_dirty = false;
-  }
   ScoreParams cp;
   memset(&cp, 0, sizeof(cp));
   cp.logits = ctx->logits;
@@ -626,7 +619,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   cp.split_counts = counts;
   cp.pool_half = (ctx->cfg.pool_kernel - 1) / 2;
   cp.row_offset = full->row_offset;
-  cp.quant_rows = clears ? full->n_rows : 0;
+  cp.quant_rows = quant ? full->n_rows : 0;
   SelectParams sp;
   memset(&sp, 0, sizeof(sp));
   sp.keys = ctx->keys;
@@ -647,10 +640,9 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
   sp.keys_per_thread = rkv::select_keys_per_thread(n_max, cluster);
   sp.per_fixed = ctx->cfg.n_seq == 1 ? 1 : 0;
   sp.row_offset = full->row_offset;
-  sp.quant_rows = clears ? full->n_rows : 0;
+  sp.quant_rows = quant ? full->n_rows : 0;
   cudaError_t e;
   if (stage != kStageSelect) {
-    ctx->hist_dirty = true;
     {
       LaunchScope scope(ctx, st, RKV_KERNEL_SCORE);
       e = rkv::launch_score(cp, ctx->cfg.n_seq, st);
@@ -658,7 +650,7 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
     if (e != cudaSuccess) return cuda_fail(ctx, e, "score launch");
     ctx->launches += 1;
     if (stage == kStageScore) {
-      ctx->pending_keys = {true, n_max, k_max, full->k, active, clears, dirty_before};
+      ctx->pending_keys = {true, n_max, k_max, full->k, active, quant};
       rkv::note_launch(st, nullptr, nullptr);
       return RKV_OK;
     }
@@ -668,7 +660,6 @@ static rkv_status select_part(rkv_ctx* ctx, const void* q, const rkv_cache* full
     e = rkv::launch_select(sp, ctx->cfg.n_seq, cluster, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "select launch");
-  ctx->hist_dirty = clears && dirty_before;
   ctx->launches += 1;
   rkv::note_launch(st, nullptr, nullptr);
   return RKV_OK;

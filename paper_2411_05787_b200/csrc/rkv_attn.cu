@@ -198,6 +198,8 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   // per-sequence sizes and (MMA warps) the query fragments: independent loads, one round trip
   const int act = (p.active != nullptr) ? __ldcg(p.active + b) : 1;
   int n = __ldcg(p.len + b);
+  int filled = -1;
+  if (kLogits && warp == kMW) filled = __ldcg(p.anchor + (int64_t)b * p.n_kv_heads + g);
   const int zero = (int)blockDim.y - 1;   // (blocks are one row of threads, which the compiler does not know)
   // The G query rows go through shared memory: G * 16 coalesced 16-byte loads for the whole CTA instead of
   // sixteen 4-byte loads per lane (the memory pipe's request rate, not its latency, is what those cost).
@@ -371,6 +373,15 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
         }
         issue_tile(t, row0, policy);
       }
+    }
+    // The score pass that follows adds to the keys' histogram, which is to start from zero.  The selection leaves it so;
+    // one that was never made has not (anchor >= 0, and only the device knows when calls come from graphs): then each
+    // CTA that has work clears its share, while the MMA warps are at the last tiles.  (Cleared in any case: 0.1 us.)
+    if (kLogits && filled >= 0) {
+      __syncwarp();
+      const int live = min(il ? total_tiles : n_splits, (int)gridDim.x);
+      uint4* hist = reinterpret_cast<uint4*>(p.hist + ((int64_t)b * p.n_kv_heads + g) * kSelectBins);
+      for (int i = split * 32 + lane; i < kSelectBins / 4; i += live * 32) hist[i] = make_uint4(0u, 0u, 0u, 0u);
     }
     return;
   }

@@ -47,6 +47,8 @@ struct AttnParams {
   float* ml_t;                // [B*Hkv][16][max_splits]: the (m, l) of the partials again, split-contiguous, or null
   int32_t* tickets;           // [B*Hkv]
   float* logits;              // [B*Hkv][logit_stride][gp] (position-major) or null
+  uint32_t* hist;             // [B*Hkv][kSelectBins]: cleared, where logits are written, for heads with
+  const int32_t* anchor;      // [B*Hkv] >= 0
   int32_t* status;
   int64_t logit_stride;
   int32_t n_q_heads, n_kv_heads, group;
@@ -90,7 +92,7 @@ struct ScoreParams {
   float* scores;              // [B][Hkv][score_stride] or null
   uint32_t* keys;             // [B*Hkv][logit_stride]: key of every position
   uint32_t* hist;             // [B*Hkv][kSelectBins]: all zero on entry
-  int32_t* anchor;            // [B*Hkv]: where each histogram's window starts (whole nats of -log p)
+  int32_t* anchor;            // [B*Hkv]: where each histogram's window starts (whole nats of -log p); -1 once it is cleared again
   int32_t* status;
   int64_t logit_stride, score_stride;
   int32_t n_q_heads, n_kv_heads, group, agg;
@@ -107,7 +109,7 @@ struct ScoreParams {
 struct SelectParams {
   const uint32_t* keys;       // [B*Hkv][logit_stride]
   uint32_t* hist;             // [B*Hkv][kSelectBins]: read, then cleared
-  const int32_t* anchor;      // [B*Hkv]: written by the score pass
+  int32_t* anchor;            // [B*Hkv]: written by the score pass, -1 when its histogram has been cleared
   const int32_t* cap;
   const int32_t* len;
   const int32_t* k_small;     // [B]
@@ -299,10 +301,9 @@ struct rkv_ctx {
   int32_t* len_tickets;
   uint32_t* win_keys;
   uint32_t* keys;      // key of every position of the last score pass
-  uint32_t* hist;      // per (sequence, KV head) histogram of those keys; all zero between selections
-  int32_t* anchor;     // per (sequence, KV head): start of the histogram's window
+  uint32_t* hist;      // per (sequence, KV head) histogram of those keys: cleared by the selection, or by the next attention pass
+  int32_t* anchor;     // per (sequence, KV head): start of the histogram's window, -1: all zero
   int32_t* split_counts;   // per (sequence, KV head): partials of the last balanced pass over an 8-bit cache
-  bool hist_dirty;     // a score pass was launched whose selection (which clears the histogram) was not
   float* logits;
   int32_t* status;
   int64_t launches;
@@ -315,9 +316,9 @@ struct rkv_ctx {
   int select_keys_per_cta;   // keys one CTA of a selection cluster takes (about): fewer = shorter chain, more = fewer CTAs
   int score_slice;           // positions per CTA of the score pass; 0: chosen per launch
   // geometry of the last rkv_full_attention, for the rkv_select_topk that completes it
-  struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; const int32_t* counts; bool clears; } pending_full;
+  struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; const int32_t* counts; bool quant; } pending_full;
   // ... and of the last rkv_score_keys, for the rkv_select_topk that launches the selection alone
-  struct { bool valid; int n_max, k_max; const void* full_k; const int32_t* active; bool clears, dirty_before; } pending_keys;
+  struct { bool valid; int n_max, k_max; const void* full_k; const int32_t* active; bool quant; } pending_keys;
   int gp;              // floats per position in the logit scratch
   std::string last_error;
   std::map<std::pair<uint64_t, int64_t>, CUtensorMap> tmaps;   // (base address, rows) -> tensor map

@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(NTS) score_kernel(const ScoreParams p) {
   }
   const int anchor_i = window_anchor(lse_min);
   const float anchor = (float)anchor_i;
-  if (blockIdx.x == 0 && tid == 0) p.anchor[bg] = anchor_i;   // the selection kernel turns bins back into key ranges
+  if (blockIdx.x == 0 && tid == 0) p.anchor[bg] = anchor_i;   // the selection turns bins back into key ranges; -1: histogram empty
   const float inv_g = 1.f / (float)G;
   bool bad = false;
   uint32_t* keys_out = p.keys + bg * p.logit_stride;
@@ -852,6 +852,7 @@ __global__ void __launch_bounds__(NT, 2) select_kernel(const SelectParams p) {
   {
     uint4* hz = reinterpret_cast<uint4*>(p.hist + bg * kBins);
     for (int i = rank * NT + tid; i < kBins / 4; i += C * NT) hz[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (rank == 0 && tid == 0) p.anchor[bg] = -1;   // (every CTA has read it as well)
   }
   uint32_t flat_base = 0, below_before = 0, total = 0;
   int src = 0;                                // (threads below the candidate count) the CTA whose segment holds candidate tid

@@ -297,3 +297,53 @@ def test_balanced_pass_captured_and_replayed(mods):
             for a, b in zip(kept, eager):
                 assert torch.equal(a, b)
     assert shared.device_status() == 0 and own.device_status() == 0
+
+
+@pytest.mark.parametrize("left_by", ["8 bits", "bf16"])
+@pytest.mark.parametrize("captured", ["the step", "the scores"])
+def test_selection_behind_scores_that_were_never_selected(mods, left_by, captured):
+    """A score pass without its selection leaves its keys' histogram in the workspace.  A full step of the bf16 cache
+    behind it selects as ever, also where one of the two is a graph, so that the host cannot know what runs before what."""
+    rkv, runner, synth = mods
+    n_kv, group, n, keep = 2, 4, 3000, 200
+    ctx = context(rkv, 1, n_kv * group, n_kv, n, keep)
+    b = bf16_cache(synth, [n], [n], n_kv, 5)
+    bs = rkv.cache_struct(b.k, b.v, b.row_offset, b.cap, b.len)
+    c = filled(synth, [n], n_kv, 6)
+    cs, k_small = struct(rkv, c), i32([keep])
+    q = normal(gen(7), 1, n_kv * group, 128).to(torch.bfloat16)
+    other = torch.empty_like(q)
+    out, idx = torch.empty_like(q), torch.empty((1, n_kv, keep), dtype=torch.int32, device="cuda")
+
+    def step():
+        ctx.full_step(q, bs, k_small, keep, out, idx)
+
+    def scores():
+        if left_by == "bf16":
+            ctx.full_attention(q, bs, other)
+            ctx.score_keys(q, bs, k_small, keep)
+        else:
+            ctx.quant_full_attention(q, cs, other)
+            ctx.score_keys(q, cs, k_small, keep)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.current_stream())
+        step()
+        want = (out.clone(), idx.clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step() if captured == "the step" else scores()
+        step()                                    # (behind a captured score pass, which has not run)
+        for _ in range(3):
+            idx.fill_(-2)
+            out.zero_()
+            if captured == "the step":
+                scores()
+                graph.replay()
+            else:
+                graph.replay()
+                step()
+            side.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(idx, want[1])
+    assert ctx.device_status() == 0
