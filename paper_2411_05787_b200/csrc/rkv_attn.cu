@@ -264,11 +264,12 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       if (!evicting) n = n + 1;
     }
   }
+  const int read = (n ^ new_len_s ^ new_len_f ^ pos_new) & zero;
   if (!kAppend && q_row) *reinterpret_cast<uint4*>(sm_q + (tid >> 4) * kQPad + (tid & 15) * 4) = qv;
   uint32_t qb[8][2];              // B fragments of Q^T: [k = channel][n = head]
   if (warp < kMW) {
-    if (kAppend && !kCluster) {   // (with the copy warp, see below)
-      asm volatile("bar.sync 1, %0;" ::"r"(32 * kMW + 32 + (n & zero)) : "memory");
+    if (kAppend) {                // (with the copy warp, see below)
+      asm volatile("bar.sync 1, %0;" ::"r"(32 * kMW + 32 + read) : "memory");
     } else {
       consumer_bar();             // the query rows are in shared memory
     }
@@ -284,16 +285,16 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
       qb[2 * i + 1][1] = r[3];
     }
   }
-  // Streaming form: the copy warp, too, has to have read the old length before this CTA's ticket is drawn behind the
-  // barrier above, where it arrives without waiting.  (The barrier's count depends on the length just loaded, so that no
-  // warp can arrive before its load has returned.)
-  if (kAppend && !kCluster && warp == kMW) {
+  // Everyone, the copy warp too, has to have read the sizes that the append changes before a ticket says so.  The copy
+  // warp arrives at the barrier above without waiting, and the barrier's count depends on what was loaded (`read` is
+  // zero), so that no warp can arrive before its loads have returned.
+  if (kAppend && warp == kMW) {
     __syncwarp();
-    asm volatile("bar.arrive 1, %0;" ::"r"(32 * kMW + 32 + (n & zero)) : "memory");
+    asm volatile("bar.arrive 1, %0;" ::"r"(32 * kMW + 32 + read) : "memory");
   }
   // Fused append: the lengths are bumped by the last ticket holder of the sequence.  A ticket is taken only
-  // after the old lengths have been read by everyone it stands for - one per cluster, taken behind the cluster
-  // barrier, or (streaming form, no barrier) one per CTA - so nobody can still see them change.
+  // after the old lengths have been read by everyone it stands for - one per cluster, taken when every peer's slice,
+  // sent behind that peer's barrier, has arrived, or (streaming form) one per CTA - so nobody can still see them change.
   // (In a cluster the ticket goes to the last MMA thread, not to thread 0: the atomic's round trip would otherwise
   // hold up warp 0, which finishes the CTA's share of the output right behind it.)
   bool ticket_due = kAppend && tid == (kCluster ? 32 * kMW - 1 : 0) && (!kCluster || split == 0);
@@ -304,7 +305,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CU
   if (!kCluster && ticket_due) {
     // (the increment is made to depend on the lengths just loaded, so that the atomic cannot be issued before
     // those loads have returned: a ticket says "this CTA HAS read the old lengths")
-    const int one = 1 + ((n ^ new_len_f ^ new_len_s) & zero);
+    const int one = 1 + read;
     ticket_old = atomicAdd(p.len_tickets + b, one);
   }
   auto take_len_ticket = [&] {
