@@ -481,7 +481,9 @@ int64_t rkv_launch_count(const rkv_ctx* ctx);
  *                             cache (the library keeps a host-side record per stream; the row a call appends
  *                             itself is patched in on chip; kernels of other origin complete before a kernel of
  *                             this library starts, unless they themselves release their dependents early while
- *                             still writing the cache - turn the option off in that case); 0: never.
+ *                             still writing the cache - turn the option off in that case; calls made under stream
+ *                             capture enter the record as if they ran, so let a stream finish before capturing on
+ *                             it); 0: never.
  *   RKV_OPT_INTERLEAVE_TILES  1 (default): the full-cache pass deals the 64-position tiles of a (sequence,
  *                             KV head) out to its CTAs in turn, so that every CTA walks the whole length and
  *                             all carry the same number of tiles up to one; 0: each CTA takes one contiguous
