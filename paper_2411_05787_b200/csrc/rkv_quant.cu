@@ -11,10 +11,10 @@ namespace {
 //   code = rne(x / scale'),  needed(a) = the smallest power of two >= a / 448 (not below 2^-126).
 // One CTA per (block, KV head, sequence): all of its new rows, K and V, sit in registers (32 KB per CTA in flight,
 // 128 bytes a thread), the two maxima meet once in shared memory, then the codes leave as whole 128-byte rows.
-// HBM-bound for prompts (256 bytes read and 128 written per row and cache): 32768 rows of eight heads in 33.4 us,
-// 6.02 TB/s (512 threads a CTA 45.8 us, 128: 36.2; without the bound of 64 registers, which costs the fourth CTA of an SM,
-// 36.1); 2000-row chunks of four ragged sequences 4.6 us.  For single tokens a chain of two round trips (sizes, then rows
-// and scales), three when a block has to be encoded again: 2.4 us.
+// HBM-bound for prompts (256 bytes read and 128 written per row and cache): 32768 rows of eight heads in 33.2 us,
+// 6.06 TB/s (512 threads a CTA 45.8 us, 128: 36.2; without the bound of 64 registers, which costs the fourth CTA of an SM,
+// 36.1); 2000-row chunks of four ragged sequences 4.6 us, of which the grid without rows takes 1.8.  For single tokens a
+// chain of two round trips (sizes, then rows and scales), three when a block has to be encoded again: 2.2 us.
 constexpr int kStoreThreads = 256;
 constexpr int kStorePer = kQuantBlock * 16 / kStoreThreads;   // 16-byte pieces of bf16 per thread and cache
 
@@ -221,10 +221,10 @@ __global__ void __launch_bounds__(kStoreThreads, 4) store_kernel(const StorePara
 // small.K[b][g][r] = code * scale of full.K[b][g][idx[b][g][r]] (and V), as bf16: exact for scales that are powers of
 // two (a code has four significant bits), rounded once otherwise.  One CTA of 128 threads per 32 output rows,
 // eight lanes to a row; a lane moves eight codes from either half of a row, so that what a warp stores are whole 128-byte
-// lines (16 neighbouring codes a lane, two half-covered lines per store: 4.2 against 3.2 us for 2048 rows of eight heads,
-// 10.0 against 6.5 us for four ragged sequences of up to 4096; 32 rows a CTA instead of 64 brings the latter to 5.1 us,
-// 4.1 TB/s, 16 rows to 6.8).  Indices come with the sizes, rows and scales in the round trip behind them: two in all,
-// and what is left is their latency.
+// lines (16 neighbouring codes a lane, two half-covered lines per store, took 4.2 us where this takes 3.1 for 2048 rows of
+// eight heads, and half as long again for four ragged sequences of up to 4096).  Rows a CTA: 32 take 3.1 and 5.9 us (3.6
+// TB/s), 64 take 3.1 and 6.6, 16 take 3.4 and 8.6.  Indices come with the sizes, rows and scales in the round trip behind
+// them: two in all, and what is left is their latency.
 constexpr int kGatherRows = 32;
 constexpr int kGatherThreads = 128;
 
