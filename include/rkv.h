@@ -398,6 +398,83 @@ rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_
                     void* k, void* v, void* stream);
 
 /*
+ * Paged cache (no counterpart in the paper, whose cache is one buffer a sequence: for batches whose sequences grow, end and
+ * share their beginnings).  The memory is a pool of pages of 16, 32, 64 or 128 positions, handed out by the caller:
+ * position p of sequence b and KV head g is row p % page of page table[b][p / page], and
+ *   k, v          [n_pages][Hkv][page][128]
+ * With every page and KV head go the bounds of its keys, per channel over the positions it holds,
+ *   k_min, k_max  [n_pages][Hkv][128]
+ * which rkv_paged_append keeps and rkv_paged_sparse_attention scores pages by; both NULL: no bounds are kept.
+ * A page may be in several tables (a common prefix) as long as no call writes it.  Entries of table below a sequence's
+ * length (or, in an append, its new length) are read; one outside 0 .. n_pages - 1 sets RKV_DEV_BAD_INDEX, and its
+ * positions are neither written nor attended.  Lengths above table_stride * page (or the call's bound) are clamped to it
+ * and set RKV_DEV_LEN_CLAMPED.
+ * The attention calls end what rkv_full_attention or rkv_quant_full_attention left in the context for a rkv_select_topk.
+ */
+typedef struct {
+  void* k;              /* bf16, 16-byte aligned                                       */
+  void* v;              /* bf16, 16-byte aligned                                       */
+  void* k_min;          /* bf16, 16-byte aligned, or NULL                              */
+  void* k_max;          /* bf16, 16-byte aligned; NULL exactly where k_min is          */
+  int64_t n_pages;      /* host value: n_pages * Hkv * page < 2^31                     */
+  int32_t page;         /* host value: positions of a page, 16, 32, 64 or 128          */
+  int32_t table_stride; /* host value: pages a row of the table has room for           */
+  const int32_t* table; /* [B][table_stride]                                           */
+  int32_t* len;         /* [B] current length; rkv_paged_append updates it             */
+} rkv_paged_cache;
+
+/*
+ * Append a prompt's, a chunk's or a token's rows to a paged cache straight from the fused projection, in one launch: queries,
+ * keys and values are split, queries and keys turned by their positions exactly as rkv_rope turns them (freqs, rot_dim,
+ * layout, amplitude as there; freqs == NULL: nothing is turned), and rounded to bf16.  For row t < count[b] of sequence b,
+ * p = start[b] + t:  q[b][t] = its queries, k and v at position p = its keys and values;  len[b] = start[b] + count[b].
+ * Bounds: the page that p lies in has, when the call is over,
+ *   k_min = min(the new keys in it, and unless its first position is among them, its k_min before);  k_max likewise
+ * (NaN does not count).  start == NULL: the current lengths.  start[b] < len[b] gives up what lay from start[b] on; a page kept
+ * in part then keeps its bounds, which still hold for its keys but may be wider.  count == NULL: n_tok rows for every
+ * sequence; count[b] <= 0: none.  Rows beyond the table are dropped (RKV_DEV_APPEND_OVERFLOW); start[b] outside
+ * 0 .. min(len[b], table_stride * page) sets RKV_DEV_LEN_CLAMPED and leaves the sequence as it is.  Rows of q that no
+ * row of qkv goes to are left as they are.
+ *   qkv    bf16 (is_bf16 != 0) or fp32: (Hq + 2 Hkv) heads of 128 side by side; row t of sequence b starts at
+ *          b * seq_stride + t * tok_stride (elements; multiples of 16 bytes, as the base is)
+ *   n_tok  host value >= 1: rows per sequence in qkv and q; count[b] above it is cut to it
+ *   q      bf16 [B][n_tok][Hq][128];  must not overlap qkv
+ */
+rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t seq_stride, int64_t tok_stride,
+                            int32_t n_tok, const int32_t* start, const int32_t* count, const uint64_t* freqs,
+                            int32_t rot_dim, int32_t layout, float amplitude, const rkv_paged_cache* cache /*host struct*/,
+                            void* q, void* stream);
+
+/*
+ * Attention of one query token per sequence over a paged cache: out as in rkv_full_step.  A sequence of length 0 has zeros.
+ *   shared    int32 [n_shared] or NULL: the pages that hold the first n_shared * page positions of every sequence (its table
+ *             names them too).  They are read once for the whole batch, all of its queries together.  A sequence
+ *             that is shorter than that is attended through its own table.
+ *   max_len_hint  host value: upper bound of len[b] (0 = cfg.max_len)
+ */
+rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cache* cache /*host struct*/,
+                               const int32_t* active, const int32_t* shared, int32_t n_shared, void* out,
+                               int32_t max_len_hint, void* stream);
+
+/*
+ * Attention over the pages that a cheap score selects, per sequence and KV head (an alternative to the partial step: no
+ * full step is needed, the selection is fresh for every token, and costs page / 2 times less to read than the keys).
+ * With n = len[b] and P = ceil(n / page) pages, for page i
+ *   score[i] = max_{h in group g} sum_c max(q[h][c] k_min[i][c], q[h][c] k_max[i][c]),
+ * which no <q[h], k> of the page exceeds; evaluated in 64 bits, so that only equal sums tie.  The first `first_pages` and the
+ * last `last_pages` of the P pages come before all others; then the larger score, then the lower page.  The m = min(top_pages, P)
+ * foremost pages are attended as in rkv_full_step (positions >= n are not), and
+ *   page_idx[b][g][0..m) = those pages in ascending order, m..top_pages-1 = -1.
+ * In the scores an infinity, of a bound or a query, counts as 2^128 with its sign, and NaN as some number of that size.
+ * Inactive sequences: nothing is read or written.
+ *   page_idx   int32 [B][Hkv][top_pages]
+ *   top_pages, first_pages, last_pages   host values, >= 1, >= 0, >= 0
+ */
+rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cache* cache /*host struct*/,
+                                      const int32_t* active, int32_t top_pages, int32_t first_pages, int32_t last_pages,
+                                      int32_t* page_idx, void* out, int32_t max_len_hint, void* stream);
+
+/*
  * Refresh trigger (Sec. 2.2 "Deciding when to decode with full cache").
  *   qbar  = mean over the Hq heads of q_now[b];  qbar' likewise from q_last_full[b]
  *   sim   = <qbar, qbar'> / (|qbar| |qbar'|)          (fp32)
@@ -518,11 +595,13 @@ rkv_status rkv_get_option(const rkv_ctx* ctx, int32_t option, int32_t* value);
  * the sums and the launch counts and forgets the samples.  Do not enable it during stream capture.
  *   total_us, launches   host arrays of RKV_KERNEL_KINDS entries
  */
-#define RKV_KERNEL_ATTN_FULL 0  /* full-cache attention + logit emission (rkv_[quant_]full_step, 1st kernel) */
-#define RKV_KERNEL_SELECT 1     /* top-K from the keys' histogram        (rkv_full_step, 3rd kernel) */
-#define RKV_KERNEL_ATTN_SMALL 2 /* small-cache attention                 (rkv_small_step)            */
+#define RKV_KERNEL_ATTN_FULL 0  /* full-cache attention + logit emission (rkv_[quant_]full_step, 1st kernel;
+                                   rkv_paged_attention)                                              */
+#define RKV_KERNEL_SELECT 1     /* top-K from the keys' histogram        (rkv_full_step, 3rd kernel);
+                                   pages' scores and selection           (rkv_paged_sparse_attention) */
+#define RKV_KERNEL_ATTN_SMALL 2 /* small-cache attention                 (rkv_small_step), selected pages */
 #define RKV_KERNEL_GATHER 3     /* rkv_gather_small, rkv_quant_gather_small                          */
-#define RKV_KERNEL_APPEND 4     /* rkv_append, rkv_quant_store                                       */
+#define RKV_KERNEL_APPEND 4     /* rkv_append, rkv_quant_store, rkv_paged_append                     */
 #define RKV_KERNEL_TRIGGER 5    /* rkv_should_refresh                                                */
 #define RKV_KERNEL_FOLD 6       /* output from the split partials        (rkv_[append_]full_attention, 2nd kernel) */
 #define RKV_KERNEL_SCORE 7      /* logits -> scores, keys, histogram     (rkv_full_step, 2nd kernel) */

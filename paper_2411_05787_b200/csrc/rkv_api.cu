@@ -107,6 +107,17 @@ bool quant_ok(const rkv_quant_cache* c) {
          c->n_rows < (int64_t(1) << 31) && c->n_rows % rkv::kQuantBlock == 0 && aligned16(c->k) && aligned16(c->v) &&
          (reinterpret_cast<uintptr_t>(c->k_scale) & 3) == 0 && (reinterpret_cast<uintptr_t>(c->v_scale) & 3) == 0;
 }
+bool paged_ok(const rkv_ctx* ctx, const rkv_paged_cache* c) {
+  return c && c->k && c->v && c->table && c->len && (c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128) &&
+         c->n_pages > 0 && c->n_pages < (int64_t(1) << 31) &&
+         c->n_pages * c->page < ((int64_t(1) << 31) + ctx->cfg.n_kv_heads - 1) / ctx->cfg.n_kv_heads && c->table_stride > 0 &&
+         aligned16(c->k) && aligned16(c->v) && aligned16(c->k_min) && aligned16(c->k_max) &&
+         (c->k_min == nullptr) == (c->k_max == nullptr);
+}
+rkv::PagedDev dev_of(const rkv_ctx* ctx, const rkv_paged_cache* c) {
+  return rkv::PagedDev{c->k, c->v, c->k_min, c->k_max, c->table, c->len, c->n_pages,
+                       c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7, c->table_stride, ctx->cfg.n_kv_heads};
+}
 // What the score pass and the selection read of a cache: its sizes (the rows' pointer is its identity there).
 rkv_cache sizes_of(const rkv_quant_cache* c) { return rkv_cache{c->k, c->v, c->n_rows, c->row_offset, c->cap, c->len}; }
 // The 8-bit calls launch on the context's device only.
@@ -116,10 +127,11 @@ bool on_device(const rkv_ctx* ctx) {
 }
 
 // [n_rows][128] bf16 as {64 channels, row, half}: one box = 64 rows x both halves, 128-byte swizzle.
-// quant: [n_rows][128] codes, one box = 128 rows.
-rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out, bool quant = false) {
+// quant: [n_rows][128] codes, one box = 128 rows.  paged_box: the rows of a pool of pages, one box = this many of them.
+rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out, bool quant = false, int paged_box = 0) {
   // the map depends on nothing else
-  const std::pair<uint64_t, int64_t> key(reinterpret_cast<uint64_t>(base), quant ? -n_rows : n_rows);
+  const std::pair<uint64_t, int64_t> key(reinterpret_cast<uint64_t>(base),
+                                         quant ? -n_rows : n_rows + ((int64_t)paged_box << 32));
   auto it = ctx->tmaps.find(key);
   if (it != ctx->tmaps.end()) { *out = it->second; return RKV_OK; }
   if (g_encode == nullptr) {
@@ -131,7 +143,9 @@ rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out
     g_encode = reinterpret_cast<rkv::EncodeTiledFn>(fn);
   }
   CUtensorMap tm;
-  CUresult r = quant ? rkv::encode_quant_map(g_encode, base, n_rows, &tm) : rkv::encode_cache_map(g_encode, base, n_rows, &tm);
+  CUresult r = quant           ? rkv::encode_quant_map(g_encode, base, n_rows, &tm)
+               : paged_box > 0 ? rkv::encode_paged_map(g_encode, base, n_rows, paged_box, &tm)
+                               : rkv::encode_cache_map(g_encode, base, n_rows, &tm);
   if (r != CUDA_SUCCESS) {
     ctx->last_error = "cuTensorMapEncodeTiled failed with CUresult " + std::to_string((int)r);
     return RKV_ERR_CUDA;
@@ -489,6 +503,8 @@ rkv_status rkv_create(const rkv_config* cfg, rkv_ctx** out) {
       e = rkv::prepare_attention();
       if (e == cudaSuccess) e = rkv::prepare_select();
       if (e == cudaSuccess) e = rkv::prepare_quant_attention();
+      if (e == cudaSuccess) e = rkv::prepare_page_select();
+      if (e == cudaSuccess) e = rkv::prepare_paged_attention();
       if (e != cudaSuccess) { delete ctx; return RKV_ERR_CUDA; }
       g_prepared[ctx->device] = true;
     }
@@ -843,6 +859,169 @@ rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_
   const size_t q_bytes = (size_t)n_tok * n_q * rkv::kHeadDim * 2, kv_bytes = (size_t)n_tok * n_kv * rkv::kHeadDim * 2;
   rkv::note_rows(st, {{q, q_bytes}, {k, kv_bytes}, {v, kv_bytes}});
   return RKV_OK;
+}
+
+// ------------------------------------------------------------------------------------------------------ the paged cache
+rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t seq_stride, int64_t tok_stride,
+                            int32_t n_tok, const int32_t* start, const int32_t* count, const uint64_t* freqs,
+                            int32_t rot_dim, int32_t layout, float amplitude, const rkv_paged_cache* cache, void* q,
+                            void* stream) {
+  if (!ctx || !qkv || !q || n_tok < 1 || !paged_ok(ctx, cache) || !on_device(ctx)) return RKV_ERR_INVALID_ARG;
+  if (freqs != nullptr && (rot_dim < 16 || rot_dim > rkv::kHeadDim || rot_dim % 16 != 0 ||
+                           (layout != RKV_ROPE_HALF && layout != RKV_ROPE_INTERLEAVED)))
+    return RKV_ERR_UNSUPPORTED;
+  const int64_t size = is_bf16 ? 2 : 4;
+  if (!aligned16(qkv) || !aligned16(q) || (seq_stride * size) % 16 != 0 || (tok_stride * size) % 16 != 0 ||
+      (reinterpret_cast<uintptr_t>(freqs) & 7) != 0)
+    return RKV_ERR_INVALID_ARG;   // the kernel reads and writes 16 bytes at a time
+  rkv::PagedAppendParams p;
+  memset(&p, 0, sizeof(p));
+  p.c = dev_of(ctx, cache);
+  p.qkv = qkv;
+  p.seq_stride = seq_stride;
+  p.tok_stride = tok_stride;
+  p.start = start;
+  p.count = count;
+  p.freqs = reinterpret_cast<const unsigned long long*>(freqs);
+  p.q = q;
+  p.tickets = ctx->len_tickets;
+  p.status = ctx->status;
+  p.n_tok = n_tok;
+  p.n_q_heads = ctx->cfg.n_q_heads;
+  p.rot = freqs != nullptr ? rot_dim : 0;
+  p.amp = amplitude;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_APPEND);
+    e = rkv::launch_paged_append(p, is_bf16 != 0, freqs != nullptr && layout == RKV_ROPE_INTERLEAVED, ctx->cfg.n_seq,
+                                 ctx->sm_count, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "paged append launch");
+  ctx->launches += 1;
+  // (a pool, or the queries, may lie in memory that another cache's calls read early)
+  const size_t pool = (size_t)cache->n_pages * ctx->cfg.n_kv_heads * cache->page * rkv::kHeadDim * 2;
+  const size_t bounds = pool / cache->page, q_bytes = (size_t)ctx->cfg.n_seq * n_tok * ctx->cfg.n_q_heads * rkv::kHeadDim * 2;
+  rkv::note_rows(st, {{cache->k, pool}, {cache->v, pool}, {cache->k_min, bounds}, {cache->k_max, bounds}, {q, q_bytes}});
+  return RKV_OK;
+}
+
+// The pass over pages, in one of two forms (the rule and its measurements stand at the top of this function).
+static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, const rkv_paged_cache* cache, int most,
+                                      int kind, cudaStream_t st) {
+  CUtensorMap tm_k, tm_v;
+  const int64_t rows = cache->n_pages * ctx->cfg.n_kv_heads * cache->page;
+  const int box = cache->page < rkv::kTile ? cache->page : rkv::kTile;
+  rkv_status s = tensor_map(ctx, cache->k, rows, &tm_k, false, box);
+  if (s != RKV_OK) return s;
+  s = tensor_map(ctx, cache->v, rows, &tm_v, false, box);
+  if (s != RKV_OK) return s;
+  const int64_t bg = (int64_t)ctx->cfg.n_seq * ctx->cfg.n_kv_heads, slots = 2 * ctx->sm_count;
+  const int tiles = (most + rkv::kTile - 1) / rkv::kTile, room = ctx->max_splits - p.first_slot;
+  int gx = (int)(slots / bg);
+  if (gx > room) gx = room;
+  if (gx > tiles) gx = tiles;
+  if (gx < 1) gx = 1;
+  const int cluster_gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
+  const bool cluster = p.first_slot == 0 && tiles <= 8 * cluster_gx;
+  if (cluster) gx = cluster_gx;
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, kind);
+    e = rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "paged attention launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  if (cluster) return RKV_OK;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_FOLD);
+    e = rkv::launch_paged_fold(p, ctx->cfg.n_seq, gx, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "fold launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr, true);
+  return RKV_OK;
+}
+
+static rkv::PagedAttnParams paged_params(const rkv_ctx* ctx, const rkv_paged_cache* cache, const void* q,
+                                         const int32_t* active, void* out, int n_max) {
+  rkv::PagedAttnParams p;
+  memset(&p, 0, sizeof(p));
+  p.c = dev_of(ctx, cache);
+  p.q = q;
+  p.active = active;
+  p.out = out;
+  p.partials = ctx->partials;
+  p.ml_t = ctx->ml_t;
+  p.status = ctx->status;
+  p.n_q_heads = ctx->cfg.n_q_heads;
+  p.group = ctx->group;
+  p.max_splits = ctx->max_splits;
+  p.max_len = n_max;
+  p.scale = ctx->cfg.softmax_scale;
+  return p;
+}
+
+rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cache* cache, const int32_t* active,
+                               const int32_t* shared, int32_t n_shared, void* out, int32_t max_len_hint, void* stream) {
+  if (!ctx || !q || !out || !paged_ok(ctx, cache) || !on_device(ctx) || !aligned16(q) || !aligned16(out))
+    return RKV_ERR_INVALID_ARG;
+  const int n_max = max_len_hint == 0 ? ctx->cfg.max_len : max_len_hint;
+  if (n_max < 1 || n_max > ctx->cfg.max_len || n_shared < 0 || (shared == nullptr) != (n_shared == 0))
+    return RKV_ERR_INVALID_ARG;
+  ctx->pending_full.valid = false;   // its partials and logits are about to be overwritten
+  rkv::PagedAttnParams p = paged_params(ctx, cache, q, active, out, n_max);
+  return run_paged_attention(ctx, p, cache, n_max, RKV_KERNEL_ATTN_FULL, static_cast<cudaStream_t>(stream));
+}
+
+rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cache* cache, const int32_t* active,
+                                      int32_t top_pages, int32_t first_pages, int32_t last_pages, int32_t* page_idx,
+                                      void* out, int32_t max_len_hint, void* stream) {
+  if (!ctx || !q || !out || !page_idx || !paged_ok(ctx, cache) || !cache->k_min || !on_device(ctx) || !aligned16(q) ||
+      !aligned16(out) || top_pages < 1 || first_pages < 0 || last_pages < 0)
+    return RKV_ERR_INVALID_ARG;
+  const int n_max = max_len_hint == 0 ? ctx->cfg.max_len : max_len_hint;
+  if (n_max < 1 || n_max > ctx->cfg.max_len) return RKV_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  ctx->pending_full.valid = false;
+  int most = (n_max - 1) / cache->page + 1;
+  if (most > cache->table_stride) most = cache->table_stride;
+  rkv::PageSelectParams sp;
+  memset(&sp, 0, sizeof(sp));
+  sp.c = dev_of(ctx, cache);
+  sp.q = q;
+  sp.active = active;
+  sp.scores = reinterpret_cast<double*>(ctx->logits);     // (8 bytes a page of 16 positions or more, of 16 or more a position)
+  sp.score_stride = ctx->logit_stride * ctx->gp / 2;
+  sp.page_idx = page_idx;
+  sp.status = ctx->status;
+  sp.n_q_heads = ctx->cfg.n_q_heads;
+  sp.group = ctx->group;
+  sp.top = top_pages;
+  sp.first = first_pages;
+  sp.last = last_pages;
+  sp.max_len = n_max;
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_SELECT);
+    e = rkv::launch_page_scores(sp, ctx->cfg.n_seq, most, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "page score launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_SELECT);
+    e = rkv::launch_page_select(sp, ctx->cfg.n_seq, most, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "page selection launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  rkv::PagedAttnParams p = paged_params(ctx, cache, q, active, out, n_max);
+  p.page_idx = page_idx;
+  p.top = top_pages;
+  const int taken = top_pages < most ? top_pages : most;
+  return run_paged_attention(ctx, p, cache, taken * cache->page, RKV_KERNEL_ATTN_SMALL, st);
 }
 
 rkv_status rkv_full_step(rkv_ctx* ctx, const void* q, const rkv_cache* full, const int32_t* k_small, int32_t k_max,

@@ -174,6 +174,58 @@ cudaError_t launch_rope(const void* qkv, bool is_bf16, int64_t tok_stride, const
                         int n_kv, const uint64_t* freqs, int rot, bool interleaved, float amp, void* q, void* k, void* v,
                         cudaStream_t st);
 
+// The paged cache as the kernels see it.
+struct PagedDev {
+  void* k; void* v; void* k_min; void* k_max;
+  const int32_t* table; int32_t* len;
+  int64_t n_pages;
+  int32_t page_shift, table_stride, n_kv_heads;
+};
+
+struct PagedAppendParams {
+  PagedDev c;
+  const void* qkv; int64_t seq_stride, tok_stride;     // elements
+  const int32_t* start; const int32_t* count;          // [B] or null
+  const unsigned long long* freqs;                     // null: nothing is turned
+  void* q;
+  int32_t* tickets; int32_t* status;
+  int32_t n_tok, n_q_heads, rot;
+  float amp;
+  int32_t rounds;                                      // heads a warp takes, one after the other
+};
+cudaError_t launch_paged_append(const PagedAppendParams& p, bool is_bf16, bool interleaved, int n_seq, int sm_count,
+                                cudaStream_t st);
+
+// Scores and selection of a sequence's pages.
+struct PageSelectParams {
+  PagedDev c;
+  const void* q; const int32_t* active;
+  double* scores;             // [B*Hkv][score_stride]
+  int32_t* page_idx;          // [B][Hkv][top]
+  int32_t* status;
+  int64_t score_stride;
+  int32_t n_q_heads, group, top, first, last, max_len;
+};
+cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
+cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
+cudaError_t prepare_page_select();
+
+struct PagedAttnParams {
+  PagedDev c;
+  const void* q; const int32_t* active; void* out;
+  const int32_t* page_idx;    // [B][Hkv][top]: the pages attended, or null: all positions from `from` on
+  float* partials; float* ml_t;     // as in AttnParams
+  int32_t* status;
+  int32_t n_q_heads, group, top, max_splits, max_len;
+  int32_t from;               // positions that the batch shares: sequences that reach so far begin behind them
+  int32_t first_slot;         // split partials of the shared positions
+  float scale;
+};
+cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_seq,
+                                   int grid_x, bool cluster, cudaStream_t st);
+cudaError_t launch_paged_fold(const PagedAttnParams& p, int n_seq, int grid_x, cudaStream_t st);
+cudaError_t prepare_paged_attention();
+
 cudaError_t launch_attention(const AttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                              int n_seq, int grid_x, bool write_logits, cudaStream_t st, bool append = false);
 cudaError_t launch_attention_cluster(const AttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
@@ -270,6 +322,17 @@ inline CUresult encode_cache_map(EncodeTiledFn encode, void* base, int64_t n_row
   const cuuint64_t dims[3] = {64, (cuuint64_t)n_rows, 2};
   const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim * 2, 128};   // bytes: next row, next half
   const cuuint32_t box[3] = {64, (cuuint32_t)kTile, 2};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+// A pool of pages ([n_pages][Hkv][page][128] bf16): the same with a box of one page, or of 64 rows where a page is larger.
+inline CUresult encode_paged_map(EncodeTiledFn encode, void* base, int64_t n_rows, int box_rows, CUtensorMap* out) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)n_rows, 2};
+  const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim * 2, 128};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 2};
   const cuuint32_t estr[3] = {1, 1, 1};
   return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

@@ -1,0 +1,518 @@
+// The paged cache: rows appended with the rotation on the way, and the scores that select pages.
+#include <cuda_bf16.h>
+
+#include "rkv_internal.h"
+#include "rkv_ptx.cuh"
+#include "rkv_rows.cuh"
+
+namespace rkv {
+namespace {
+
+// ----------------------------------------------------------------------------------------------------------- append
+// Rows of the fused projection become queries [token][head] and keys and values in their pages, queries and keys turned by
+// their positions (the angle as in rkv_rope.cu: turns as 64-bit fixed point), and the keys' bounds follow.
+//
+// HBM-bound for prompts: every channel is read once and written once.  A CTA takes the new rows of kUnit positions (or of
+// one page, where that is more) for 8 or more heads, a warp one head at a time over all of those rows, so that a page's
+// bounds stay in the warp's registers until the page ends, and no two CTAs meet at a page and head.  Eight threads share
+// a row, each with two pieces of eight channels (eight pairs, or channels that are only copied); a warp has four rows of
+// four groups of its rows in flight.  Sines and cosines of the unit's (row, pair)s are worked out once per CTA, in shared memory.
+constexpr int kAppendThreads = 256, kAppendWarps = kAppendThreads / 32;
+constexpr int kUnit = 64;                    // positions of a CTA
+constexpr int kAppendAhead = 4;              // rows of a thread in flight
+constexpr int kCsRow = kHeadDim / 2 + 8;     // (and the four rows of a warp beside each other)
+
+template <typename T, bool kInterleaved>
+__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedAppendParams p) {
+  __shared__ float2 sm_cs[kUnit][kCsRow];       // pair 8 i + j of a row at 8 j + i: the eight threads of a row read side by side
+  __shared__ int sm_sizes[3];
+  __shared__ int sm_page[kUnit / 16];
+  const int b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int part = tid & 7, octet = lane >> 3;
+  const int n_kv = p.c.n_kv_heads, heads = p.n_q_heads + 2 * n_kv;
+  const int page = 1 << p.c.page_shift, unit = page > kUnit ? page : kUnit;
+  const int half = p.rot >> 1;
+  const bool turns = part < (p.rot >> 4);
+  const int ca = (kInterleaved || !turns) ? 16 * part : 8 * part;          // this thread's pieces of a row
+  const int cb = (kInterleaved || !turns) ? 16 * part + 8 : half + 8 * part;
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  // One thread reads the sizes for its CTA; behind the barrier it draws a ticket, the last of which writes the new length:
+  // a ticket says that nobody in its CTA will read the sizes again.
+  if (tid == 0) {
+    const int l = __ldcg(p.c.len + b);
+    sm_sizes[0] = l;
+    sm_sizes[1] = p.start != nullptr ? __ldcg(p.start + b) : l;
+    sm_sizes[2] = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
+  }
+  __syncthreads();
+  int ticket = -1;
+  if (tid == 0) ticket = atomicAdd(p.tickets + b, 1);
+  const int len = sm_sizes[0], start = sm_sizes[1];
+  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  int count = min(max(sm_sizes[2], 0), p.n_tok);
+  const bool sound = start >= 0 && start <= len && start <= room;
+  int flags = 0;
+  if (!sound) {
+    flags = RKV_DEV_LEN_CLAMPED;
+    count = 0;
+  } else if (count > room - start) {
+    flags = RKV_DEV_APPEND_OVERFLOW;
+    count = (int)(room - start);
+  }
+  const int64_t end = (int64_t)start + count;
+  const int64_t u0 = ((int64_t)start / unit + blockIdx.x) * unit;          // the CTA's positions
+  const int64_t first = u0 > start ? u0 : start, last = u0 + unit < end ? u0 + unit : end;
+  if (tid == 0) {
+    if (ticket == (int)(gridDim.x * gridDim.y) - 1) {
+      if (sound) p.c.len[b] = (int)end;
+      p.tickets[b] = 0;   // ready for the next call on this stream
+    }
+    if (flags != 0 && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, flags);
+  }
+  if (count <= 0 || first >= last) return;
+
+  const T* rows = static_cast<const T*>(p.qkv) + (int64_t)b * p.seq_stride;
+  for (int64_t s0 = u0; s0 < last; s0 += kUnit) {       // (once, but for pages of 128)
+    const int64_t lo = s0 > first ? s0 : first, hi = s0 + kUnit < last ? s0 + kUnit : last;
+    if (lo >= hi) continue;
+    const int n = (int)(hi - lo), off = (int)(lo - s0);   // rows, and the first one's place in the unit
+    if (s0 != u0) __syncthreads();                       // (the sines of the half before are still in use)
+    const int most = page < kUnit ? page : kUnit;         // positions of a page in this part of the unit
+    if (tid < kUnit / most) {
+      const int64_t at = s0 + tid * most;
+      int pg = -1;
+      if (at < hi && at + most > lo) {
+        pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + (at >> p.c.page_shift));
+        if ((unsigned)pg >= (unsigned)p.c.n_pages) {
+          pg = -1;
+          if (blockIdx.y == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+        }
+      }
+      sm_page[tid] = pg;
+    }
+    for (int i = tid; i < n * half; i += kAppendThreads) {
+      const int r = i / half, j = i - r * half;
+      const unsigned long long t = (unsigned long long)(lo + r) * __ldg(p.freqs + j);
+      float s, c;
+      sincospif((float)(int)(t >> 32) * 4.656612873e-10f, &s, &c);   // 2^-31: half turns
+      sm_cs[r][8 * (j & 7) + (j >> 3)] = make_float2(c * p.amp, s * p.amp);
+    }
+    __syncthreads();
+    for (int round = 0; round < p.rounds; ++round) {
+      const int h = ((int)blockIdx.y * p.rounds + round) * kAppendWarps + warp;
+      if (h >= heads) break;
+      const bool is_q = h < p.n_q_heads, is_k = !is_q && h < p.n_q_heads + n_kv;
+      const int g = is_q ? 0 : is_k ? h - p.n_q_heads : h - p.n_q_heads - n_kv;
+      const bool turn = turns && (is_q || is_k);
+      const bool bounds = is_k && p.c.k_min != nullptr;
+      __nv_bfloat16* pool = static_cast<__nv_bfloat16*>(is_k ? p.c.k : p.c.v);
+      Bounds8 ba, bb;
+      ba.reset();
+      bb.reset();
+      // positions page by page: rows off .. off + n - 1 of this part
+      for (int pi = off / most; pi * most < off + n; ++pi) {
+        const int r0 = max(pi * most, off), r1 = min((pi + 1) * most, off + n);
+        const int pg = sm_page[pi];
+        const int64_t pos0 = s0 + r0;
+        if (bounds && (r0 & (most - 1)) == 0 && (pos0 & (page - 1)) == 0) {
+          ba.reset();
+          bb.reset();
+        }
+        for (int r = r0 + octet; r < r1; r += 4 * kAppendAhead) {
+          Raw8<T> xa[kAppendAhead], xb[kAppendAhead];
+#pragma unroll
+          for (int i = 0; i < kAppendAhead; ++i) {
+            if (r + 4 * i < r1) {
+              const T* x = rows + (s0 + r + 4 * i - start) * p.tok_stride + h * kHeadDim;
+              xa[i].load(x + ca);
+              xb[i].load(x + cb);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kAppendAhead; ++i) {
+            const int rr = r + 4 * i;
+            if (rr >= r1) break;
+            float a[8], w[8];
+            xa[i].get(a);
+            xb[i].get(w);
+            if (turn) {
+              const float2* cs = &sm_cs[rr - off][part];
+              if (kInterleaved) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const float2 e = cs[8 * j], f = cs[8 * (4 + j)];
+                  const float x = a[2 * j], y = a[2 * j + 1], z = w[2 * j], u = w[2 * j + 1];
+                  a[2 * j] = x * e.x - y * e.y;
+                  a[2 * j + 1] = x * e.y + y * e.x;
+                  w[2 * j] = z * f.x - u * f.y;
+                  w[2 * j + 1] = z * f.y + u * f.x;
+                }
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const float2 e = cs[8 * j];
+                  const float x = a[j], y = w[j];
+                  a[j] = x * e.x - y * e.y;
+                  w[j] = x * e.y + y * e.x;
+                }
+              }
+            }
+            const uint4 pa = pack8(a), pb = pack8(w);
+            if (bounds) {
+              ba.take(pa);
+              bb.take(pb);
+            }
+            __nv_bfloat16* to;
+            if (is_q) {
+              to = static_cast<__nv_bfloat16*>(p.q) + (((int64_t)b * p.n_tok + (s0 + rr - start)) * p.n_q_heads + h) * kHeadDim;
+            } else {
+              if (pg < 0) continue;
+              to = pool + ((((int64_t)pg * n_kv + g) << p.c.page_shift) + ((s0 + rr) & (page - 1))) * kHeadDim;
+            }
+            *reinterpret_cast<uint4*>(to + ca) = pa;
+            *reinterpret_cast<uint4*>(to + cb) = pb;
+          }
+        }
+        // The page's last new row: its bounds leave.  A page whose first position is not among the new ones takes in the
+        // bounds that it had; one of 128 positions whose first half this CTA has just done, those.
+        if (bounds) {
+          __syncwarp();
+          ba.over_octets();
+          bb.over_octets();
+          if (octet == 0 && pg >= 0) {
+            const int64_t at = ((int64_t)pg * n_kv + g) * kHeadDim;
+            const bool joins = (pos0 & (page - 1)) != 0;
+            uint4* lo4 = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.c.k_min) + at);
+            uint4* hi4 = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.c.k_max) + at);
+            if (joins) {
+              ba.join(__ldcg(lo4 + ca / 8), __ldcg(hi4 + ca / 8));
+              bb.join(__ldcg(lo4 + cb / 8), __ldcg(hi4 + cb / 8));
+            }
+            lo4[ca / 8] = ba.lo4();
+            lo4[cb / 8] = bb.lo4();
+            hi4[ca / 8] = ba.hi4();
+            hi4[cb / 8] = bb.hi4();
+          }
+          ba.reset();
+          bb.reset();
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------ pages' scores
+// score[i] = max_h sum_c max(q[h][c] k_min[i][c], q[h][c] k_max[i][c]): the bound that is taken depends on the sign of
+// q[h][c] alone, so a page and head cost 128 products.  They are formed and added in 64 bits: the products of two bf16 are
+// then exact and their sums all but exact, and the selection does not depend on the order of the sum.  A bf16 becomes a
+// double of 2^-896 its value by moving its bits (subnormals and zeros too), without a conversion; the queries carry 2^512.
+//
+// Bound by the bounds' bytes (512 per page and head) or by the 64-bit pipe (64 products a clock and SM), whichever takes
+// longer: seven heads a group 1.5 times the bytes' time.  Sixteen threads share a page, eight channels each, and have four
+// pages in flight; four heads at a time.  The sixteen sums (page, head) of a thread meet in fifteen exchanges that leave
+// each thread one of them.
+constexpr int kScorePages = 32;              // of a CTA: four warps of two halves with four pages each
+constexpr int kScoreCtaThreads = 128;
+
+__device__ __forceinline__ double wide_hi(uint32_t top) {   // bf16 in the upper half of `top`, as a double times 2^-896
+  return __hiloint2double((int)((top & 0x80000000u) | ((top & 0x7fff0000u) >> 3)), 0);
+}
+
+__global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const PageSelectParams p) {
+  __shared__ double2 sm_q[kMaxGroup][4][16];   // channels 8 l + 2 i, 8 l + 2 i + 1 of head h at [h][i][l]
+  const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 31, l = lane & 15;
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  const int n_kv = p.c.n_kv_heads, G = p.group;
+  const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
+  const int n = __ldcg(p.c.len + b);
+  const int i0 = blockIdx.x * kScorePages + (tid >> 4) * 4;   // this thread's four pages
+  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  const int lim = room < p.max_len ? (int)room : p.max_len;
+  const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
+  if (act == 0 || (int)(blockIdx.x * kScorePages) >= pages) return;
+  if (tid < G * 16) {
+    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
+                                                          ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim) + tid);
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      sm_q[tid >> 4][i][tid & 15] = make_double2(wide_hi(x[i] << 16) * 0x1p1000 * 0x1p408, wide_hi(x[i]) * 0x1p1000 * 0x1p408);
+  } else if (tid < kMaxGroup * 16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sm_q[tid >> 4][i][tid & 15] = make_double2(0.0, 0.0);
+  }
+  uint4 least[4], most[4];
+  int bad = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    least[u] = most[u] = make_uint4(0u, 0u, 0u, 0u);
+    if (i0 + u < pages) {
+      const int pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + i0 + u);
+      if ((unsigned)pg >= (unsigned)p.c.n_pages) {
+        bad |= 1 << u;
+      } else {
+        const int64_t at = ((int64_t)pg * n_kv + g) * (kHeadDim / 8) + l;
+        least[u] = __ldcg(static_cast<const uint4*>(p.c.k_min) + at);
+        most[u] = __ldcg(static_cast<const uint4*>(p.c.k_max) + at);
+      }
+    }
+  }
+  __syncthreads();
+  double best = -INFINITY;
+  for (int h0 = 0; h0 < G; h0 += 4) {
+    double v[16];   // [page][head]
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      double2 q[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) q[h] = sm_q[h0 + h][i][l];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t a = i == 0 ? least[u].x : i == 1 ? least[u].y : i == 2 ? least[u].z : least[u].w;
+        const uint32_t z = i == 0 ? most[u].x : i == 1 ? most[u].y : i == 2 ? most[u].z : most[u].w;
+        const double a0 = wide_hi(a << 16), a1 = wide_hi(a), z0 = wide_hi(z << 16), z1 = wide_hi(z);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          v[4 * u + h] = fma(q[h].x, __double2hiint(q[h].x) < 0 ? a0 : z0, v[4 * u + h]);
+          v[4 * u + h] = fma(q[h].y, __double2hiint(q[h].y) < 0 ? a1 : z1, v[4 * u + h]);
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+      const bool up = (lane & o) != 0;
+#pragma unroll
+      for (int j = 0; j < o; ++j) {
+        const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
+        v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      }
+    }
+    double s = h0 + (l & 3) < G ? v[0] : -INFINITY;   // page l >> 2, head h0 + (l & 3)
+    s = fmax(s, __shfl_xor_sync(0xffffffffu, s, 1));
+    s = fmax(s, __shfl_xor_sync(0xffffffffu, s, 2));
+    best = fmax(best, s);
+  }
+  const int u = l >> 2;
+  if ((l & 3) == 0 && i0 + u < pages) {
+    if ((bad >> u) & 1) {   // a page that is not there comes after all others
+      best = -1.7e308;
+      if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+    }
+    p.scores[((int64_t)b * n_kv + g) * p.score_stride + i0 + u] = best;
+  }
+  if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
+}
+
+// -------------------------------------------------------------------------------------------------------- selection
+// The m foremost pages of one (sequence, KV head), one CTA: forced pages first, then by score, then the lower page.  The
+// candidates for the last places are narrowed down: the range of their scores is cut into kBins equal parts (the part is a
+// monotone function of the score), those in parts above the one that holds the last place are in, those below are out, and what
+// is left goes round again until it is no more than one thread can be had for each; these are ranked by comparing all with all.
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
+constexpr int kBins = 1024, kRanked = 256;
+constexpr int kMostPages = kSelectCluster * kSelectMaxKeysPerCta / 16;   // longest context in pages of 16
+constexpr int kPickWords = (kMostPages + 31) / 32;
+
+__device__ __forceinline__ void block_range(double& lo, double& hi, double (*sm)[2], int tid) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = fmin(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmax(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  if ((tid & 31) == 0) {
+    sm[tid >> 5][0] = lo;
+    sm[tid >> 5][1] = hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kPickWarps; ++w) {
+    lo = fmin(lo, sm[w][0]);
+    hi = fmax(hi, sm[w][1]);
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int block_scan(int x, int* sm, int tid, int* total) {   // exclusive
+  int inc = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, inc, o);
+    if ((tid & 31) >= o) inc += y;
+  }
+  if ((tid & 31) == 31) sm[tid >> 5] = inc;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPickWarps; ++w) {
+    const int y = sm[w];
+    if (w < (tid >> 5)) before += y;
+    all += y;
+  }
+  __syncthreads();
+  *total = all;
+  return before + inc - x;
+}
+
+__global__ void __launch_bounds__(kPickThreads) page_select_kernel(const PageSelectParams p) {
+  extern __shared__ double sm_s[];
+  __shared__ double sm_range[kPickWarps][2], sm_cand[kRanked];
+  __shared__ int sm_at[kRanked], sm_scan[kPickWarps], sm_bins[kBins], sm_pick[3];
+  __shared__ uint32_t sm_in[kPickWords];
+  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
+  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  const int lim = room < p.max_len ? (int)room : p.max_len;
+  const int n = min(max(__ldcg(p.c.len + b), 0), lim);
+  if (act == 0) return;
+  const int pages = (n + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
+  const int m = min(p.top, pages);
+  int32_t* out = p.page_idx + ((int64_t)b * gridDim.x + g) * p.top;
+  for (int i = m + tid; i < p.top; i += kPickThreads) out[i] = -1;
+  if (m == pages) {
+    for (int i = tid; i < m; i += kPickThreads) out[i] = i;
+    return;
+  }
+  const int first = min(p.first, pages), last = min(p.last, pages - first);
+  if (first + last >= m) {   // no room beside the forced pages: the lower ones
+    for (int i = tid; i < m; i += kPickThreads) out[i] = i < first ? i : pages - last + (i - first);
+    return;
+  }
+  const int lo_i = first, hi_i = pages - last;   // the pages that compete
+  int want = m - first - last;
+  const double* score = p.scores + ((int64_t)b * gridDim.x + g) * p.score_stride;
+  double c_lo = INFINITY, c_hi = -INFINITY;      // the candidates: those with a score of c_lo .. c_hi
+  for (int i = lo_i + tid; i < hi_i; i += kPickThreads) {
+    const double s = __ldcg(score + i);
+    sm_s[i] = s;
+    c_lo = fmin(c_lo, s);
+    c_hi = fmax(c_hi, s);
+  }
+  block_range(c_lo, c_hi, sm_range, tid);
+  int count = hi_i - lo_i;
+  while (count > kRanked && count != want && c_lo < c_hi) {
+    for (int i = tid; i < kBins; i += kPickThreads) sm_bins[i] = 0;
+    __syncthreads();
+    const double f = kBins / (c_hi - c_lo);
+    auto bin = [&](double s) { return min(kBins - 1, (int)((c_hi - s) * f)); };
+    for (int i = lo_i + tid; i < hi_i; i += kPickThreads) {
+      const double s = sm_s[i];
+      if (s >= c_lo && s <= c_hi) atomicAdd(&sm_bins[bin(s)], 1);
+    }
+    __syncthreads();
+    const int a0 = sm_bins[2 * tid], a1 = sm_bins[2 * tid + 1];
+    int all;
+    const int at = block_scan(a0 + a1, sm_scan, tid, &all);
+    if (at < want && want <= at + a0 + a1) {       // one thread's
+      const bool second = want > at + a0;
+      sm_pick[0] = 2 * tid + second;
+      sm_pick[1] = second ? at + a0 : at;
+      sm_pick[2] = second ? a1 : a0;
+    }
+    __syncthreads();
+    const int pick = sm_pick[0];
+    want -= sm_pick[1];
+    count = sm_pick[2];
+    double n_lo = INFINITY, n_hi = -INFINITY;
+    for (int i = lo_i + tid; i < hi_i; i += kPickThreads) {
+      const double s = sm_s[i];
+      if (s >= c_lo && s <= c_hi && bin(s) == pick) {
+        n_lo = fmin(n_lo, s);
+        n_hi = fmax(n_hi, s);
+      }
+    }
+    block_range(n_lo, n_hi, sm_range, tid);
+    c_lo = n_lo;
+    c_hi = n_hi;
+  }
+  // in: the forced ones and those above the candidates
+  const int words = (pages + 31) >> 5;
+  if (tid == 0) sm_pick[0] = 0;
+  __syncthreads();
+  const bool ties = count > kRanked && count != want;      // more candidates of one score than can be ranked
+  for (int i0 = (tid >> 5) * 32; i0 < words * 32; i0 += kPickThreads) {
+    const int i = i0 + lane;
+    const bool competes = i >= lo_i && i < hi_i;
+    const double s = competes ? sm_s[i] : 0.0;
+    const bool in = i < pages && (!competes || s > c_hi || (count == want && s >= c_lo));
+    const uint32_t mask = __ballot_sync(0xffffffffu, in);
+    if (lane == 0) sm_in[i0 >> 5] = mask;
+    if (competes && count != want && !ties && s >= c_lo && s <= c_hi) {
+      const int k = atomicAdd(&sm_pick[0], 1);             // (any order: they are ranked)
+      sm_cand[k] = s;
+      sm_at[k] = i;
+    }
+  }
+  __syncthreads();
+  if (count != want && !ties) {
+    if (tid < count) {
+      const double s = sm_cand[tid];
+      const int i = sm_at[tid];
+      int rank = 0;
+      for (int k = 0; k < count; ++k) rank += sm_cand[k] > s || (sm_cand[k] == s && sm_at[k] < i);
+      if (rank < want) atomicOr(&sm_in[i >> 5], 1u << (i & 31));
+    }
+    __syncthreads();
+  }
+  if (ties) {   // the first `want` of them
+    int before = 0;
+    for (int i0 = 0; i0 < pages; i0 += kPickThreads) {
+      const int i = i0 + tid;
+      const bool c = i >= lo_i && i < hi_i && sm_s[i] >= c_lo && sm_s[i] <= c_hi;
+      int all;
+      const int at = before + block_scan(c ? 1 : 0, sm_scan, tid, &all);
+      if (c && at < want) atomicOr(&sm_in[i >> 5], 1u << (i & 31));
+      before += all;
+    }
+    __syncthreads();
+  }
+  int before = 0;
+  for (int w0 = 0; w0 < words; w0 += kPickThreads) {
+    uint32_t mask = w0 + tid < words ? sm_in[w0 + tid] : 0u;
+    int all;
+    int at = before + block_scan(__popc(mask), sm_scan, tid, &all);
+    for (; mask != 0u; mask &= mask - 1u) out[at++] = (w0 + tid) * 32 + __ffs(mask) - 1;
+    before += all;
+  }
+}
+
+}  // namespace
+
+cudaError_t prepare_page_select() {
+  return cudaFuncSetAttribute(page_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostPages * 8);
+}
+
+cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
+  return launch_ex(page_score_kernel, dim3((most_pages + kScorePages - 1) / kScorePages, p.c.n_kv_heads, n_seq),
+                   dim3(kScoreCtaThreads), 0, st, 1, p);
+}
+
+cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
+  return launch_ex(page_select_kernel, dim3(p.c.n_kv_heads, n_seq), dim3(kPickThreads), (size_t)most_pages * 8, st, 1, p);
+}
+
+cudaError_t launch_paged_append(const PagedAppendParams& p0, bool is_bf16, bool interleaved, int n_seq, int sm_count,
+                                cudaStream_t st) {
+  PagedAppendParams p = p0;
+  const int unit = (1 << p.c.page_shift) > kUnit ? (1 << p.c.page_shift) : kUnit;
+  const int units = (p.n_tok - 1) / unit + 2;        // new rows that begin inside a unit may end inside one more
+  const int heads = p.n_q_heads + 2 * p.c.n_kv_heads, all = (heads + kAppendWarps - 1) / kAppendWarps;
+  // Sines and cosines are worked out once per CTA: as many heads to a CTA as leave four CTAs to an SM.
+  const int64_t ctas = (int64_t)units * n_seq * all;
+  p.rounds = (int)(ctas / (4 * (int64_t)sm_count));
+  if (p.rounds > all) p.rounds = all;
+  if (p.rounds < 1) p.rounds = 1;
+  const dim3 grid(p.n_tok == 1 ? 1 : units, (all + p.rounds - 1) / p.rounds, n_seq), block(kAppendThreads);
+  if (is_bf16)
+    return interleaved ? launch_ex(paged_append_kernel<__nv_bfloat16, true>, grid, block, 0, st, 1, p)
+                       : launch_ex(paged_append_kernel<__nv_bfloat16, false>, grid, block, 0, st, 1, p);
+  return interleaved ? launch_ex(paged_append_kernel<float, true>, grid, block, 0, st, 1, p)
+                     : launch_ex(paged_append_kernel<float, false>, grid, block, 0, st, 1, p);
+}
+
+}  // namespace rkv

@@ -17,6 +17,7 @@
 #include <cuda_bf16.h>
 
 #include "rkv_internal.h"
+#include "rkv_rows.cuh"
 
 namespace rkv {
 namespace {
@@ -31,39 +32,8 @@ struct RopeParams {
   float amp;
 };
 
-// Eight channels as they come (converted where they are used, so that as many heads as possible are in flight).
-template <typename T> struct Raw8;
-template <> struct Raw8<__nv_bfloat16> {
-  uint4 w;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcg(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  }
-};
-template <> struct Raw8<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = __ldcg(reinterpret_cast<const float4*>(p));
-    b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
-  }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
-  uint32_t u[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 r = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    u[i] = *reinterpret_cast<const uint32_t*>(&r);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+  *reinterpret_cast<uint4*>(p) = pack8(x);
 }
 
 constexpr int kBatch = 6;   // heads of a thread whose loads are in flight together

@@ -1,4 +1,4 @@
-/* The 8-bit cache's calls and rkv_rope as a CPython extension: argument checks and marshalling for rkv.Context.
+/* The 8-bit and the paged cache's calls and rkv_rope as a CPython extension: argument checks and marshalling for rkv.Context.
  *
  * A decode loop issues these calls once per layer and token, and one of them runs for 2 to 5 us on the GPU: checked in
  * Python and marshalled by ctypes, a call costs the host 7 to 11 us, of which the library (the launch) needs 2.5.
@@ -13,9 +13,9 @@
 #include "rkv.h"
 
 static PyObject *s_dtype, *s_shape, *s_stride, *s_numel, *s_get_device, *s_is_contiguous, *s_data_ptr, *s_cuda_stream,
-    *s_device, *s_n_seq, *s_freqs, *s_rot_dim, *s_layout, *s_amplitude;
+    *s_device, *s_n_seq, *s_n_kv, *s_freqs, *s_rot_dim, *s_layout, *s_amplitude;
 /* set once by setup() */
-static PyObject *t_bf16, *t_f32, *t_i32, *c_quant_cache, *c_cache, *c_table, *f_stream;
+static PyObject *t_bf16, *t_f32, *t_i32, *c_quant_cache, *c_cache, *c_table, *c_paged_cache, *f_stream;
 
 typedef struct {
   rkv_ctx* ctx;
@@ -180,6 +180,20 @@ static int quant_cache(PyObject* o, const Key* k, rkv_quant_cache* c) {
   }
   if (n_seq != k->n_seq) {
     PyErr_SetString(PyExc_ValueError, "the cache holds another number of sequences than the context");
+    return -1;
+  }
+  return 0;
+}
+static int paged_cache(PyObject* o, const Key* k, rkv_paged_cache* c) {
+  if (structure(o, c_paged_cache, "an RkvPagedCache", c, sizeof(*c)) != 0) return -1;
+  long long device, n_seq, n_kv;
+  if (attr_ll(o, s_device, &device) != 0 || attr_ll(o, s_n_seq, &n_seq) != 0 || attr_ll(o, s_n_kv, &n_kv) != 0) return -1;
+  if (device != k->device) {
+    PyErr_SetString(PyExc_ValueError, "the cache is on another device than the context");
+    return -1;
+  }
+  if (n_seq != k->n_seq || n_kv != k->n_kv) {
+    PyErr_SetString(PyExc_ValueError, "the cache holds another number of sequences or heads than the context");
     return -1;
   }
   return 0;
@@ -355,11 +369,30 @@ static PyObject* quant_gather_small(PyObject* self, PyObject* const* a, Py_ssize
   CALL(rkv_quant_gather_small(k.ctx, idx, k_small, k_max, &full, &small, active, st));
 }
 
+/* What the library needs of a RopeTable. */
+static int rope_table(PyObject* table, const Key* k, void** freqs, long long* rot, long long* layout, double* amplitude) {
+  if ((PyObject*)Py_TYPE(table) != c_table) {
+    PyErr_SetString(PyExc_TypeError, "a RopeTable expected");
+    return -1;
+  }
+  PyObject* fr = PyObject_GetAttr(table, s_freqs);
+  if (fr == NULL) return -1;
+  const int bad = on_device(fr, k->device, "the table") || pointer_of(fr, freqs);
+  Py_DECREF(fr); /* (the table keeps it) */
+  if (bad || attr_ll(table, s_rot_dim, rot) || attr_ll(table, s_layout, layout)) return -1;
+  PyObject* am = PyObject_GetAttr(table, s_amplitude);
+  if (am == NULL) return -1;
+  *amplitude = PyFloat_AsDouble(am);
+  Py_DECREF(am);
+  return (*amplitude == -1.0 && PyErr_Occurred()) ? -1 : 0;
+}
+
 /* rope(key, qkv, pos, table, q, k, v, stream) */
 static PyObject* rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Key k;
   void *at, *pos, *freqs, *q, *kk, *v, *st;
   long long shape[2], stride[2], qs[3], ks[3], rot, layout;
+  double amplitude;
   if (count_args(n, 8) || as_key(a[0], &k)) return NULL;
   PyObject *qkv = a[1], *table = a[3];
   const int bf16 = has_dtype(qkv, t_bf16), f32 = has_dtype(qkv, t_f32);
@@ -382,20 +415,7 @@ static PyObject* rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     PyErr_SetString(PyExc_ValueError, "the projection's rows are contiguous and start on 16-byte boundaries");
     return NULL;
   }
-  if ((PyObject*)Py_TYPE(table) != c_table) {
-    PyErr_SetString(PyExc_TypeError, "a RopeTable expected");
-    return NULL;
-  }
-  PyObject* fr = PyObject_GetAttr(table, s_freqs);
-  if (fr == NULL) return NULL;
-  const int bad = on_device(fr, k.device, "the table") || pointer_of(fr, &freqs);
-  Py_DECREF(fr); /* (the table keeps it) */
-  if (bad || attr_ll(table, s_rot_dim, &rot) || attr_ll(table, s_layout, &layout)) return NULL;
-  PyObject* am = PyObject_GetAttr(table, s_amplitude);
-  if (am == NULL) return NULL;
-  const double amplitude = PyFloat_AsDouble(am);
-  Py_DECREF(am);
-  if (amplitude == -1.0 && PyErr_Occurred()) return NULL;
+  if (rope_table(table, &k, &freqs, &rot, &layout, &amplitude)) return NULL;
   if (tensor(a[2], t_i32, n_tok, k.device, kRequired, "pos [T]", &pos) ||
       tensor(a[4], t_bf16, n_tok * n_q * RKV_HEAD_DIM, k.device, kRequired, "q [T, Hq, 128]", &q) ||
       tensor(a[5], t_bf16, n_tok * n_kv * RKV_HEAD_DIM, k.device, kRequired, "k [T, Hkv, 128]", &kk) ||
@@ -406,26 +426,99 @@ static PyObject* rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
                 (float)amplitude, q, kk, v, st));
 }
 
-/* setup(bfloat16, float32, int32, RkvQuantCache, RkvCache, RopeTable, raw_stream): what the checks compare with */
+/* paged_append(key, qkv, cache, table, q, start, count, stream) */
+static PyObject* paged_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Key k;
+  rkv_paged_cache cache;
+  void *at, *freqs = NULL, *q, *start, *count, *st;
+  long long shape[3], stride[3], rot = 0, layout = 0;
+  double amplitude = 1.0;
+  if (count_args(n, 8) || as_key(a[0], &k) || paged_cache(a[2], &k, &cache)) return NULL;
+  PyObject* qkv = a[1];
+  const int bf16 = has_dtype(qkv, t_bf16), f32 = has_dtype(qkv, t_f32), d = dims(qkv, s_shape, 0, 3, shape);
+  if (bf16 < 0 || f32 < 0 || d < 0) return NULL;
+  if (!(bf16 || f32) || d != 3 || shape[0] != k.n_seq || shape[1] < 1 || shape[1] > INT32_MAX ||
+      shape[2] != (k.n_q + 2 * k.n_kv) * RKV_HEAD_DIM) {
+    PyErr_SetString(PyExc_ValueError, "qkv is a bfloat16 or float32 tensor [B, T, (Hq + 2 Hkv) * 128]");
+    return NULL;
+  }
+  if (on_device(qkv, k.device, "qkv") || dims(qkv, s_stride, 1, 3, stride) != 3 || pointer_of(qkv, &at)) return NULL;
+  /* (a stride that is never taken may have any value) */
+  const long long seq = shape[0] > 1 ? stride[0] : 0, tok = shape[1] > 1 ? stride[1] : 0, unit = bf16 ? 8 : 4;
+  if (stride[2] != 1 || seq % unit != 0 || tok % unit != 0 || (uintptr_t)at % 16 != 0) {
+    PyErr_SetString(PyExc_ValueError, "the projection's rows are contiguous and start on 16-byte boundaries");
+    return NULL;
+  }
+  if (a[3] != Py_None && rope_table(a[3], &k, &freqs, &rot, &layout, &amplitude)) return NULL;
+  if (tensor(a[4], t_bf16, k.n_seq * shape[1] * k.n_q * RKV_HEAD_DIM, k.device, kRequired, "q [B, T, Hq, 128]", &q) ||
+      per_seq(a[5], &k, kOptional, &start) || per_seq(a[6], &k, kOptional, &count) || stream_of(a[7], k.device, &st))
+    return NULL;
+  CALL(rkv_paged_append(k.ctx, at, bf16, seq, tok, (int32_t)shape[1], start, count, freqs, (int32_t)rot, (int32_t)layout,
+                        (float)amplitude, &cache, q, st));
+}
+
+/* paged_attention(key, q, cache, out, active, shared, max_len_hint, stream) */
+static PyObject* paged_attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Key k;
+  rkv_paged_cache cache;
+  void *q, *out, *active, *shared = NULL, *st;
+  long long n_shared = 0;
+  int32_t hint;
+  if (count_args(n, 8) || as_key(a[0], &k) || paged_cache(a[2], &k, &cache) || queries(a[1], &k, kRequired, &q) ||
+      queries(a[3], &k, kRequired, &out) || per_seq(a[4], &k, kOptional, &active))
+    return NULL;
+  if (a[5] != Py_None) {
+    if (method_ll(a[5], s_numel, &n_shared)) return NULL;
+    if (n_shared > cache.table_stride) {
+      PyErr_SetString(PyExc_ValueError, "more shared pages than a sequence's table has room for");
+      return NULL;
+    }
+    if (n_shared > 0 && tensor(a[5], t_i32, n_shared, k.device, kRequired, "shared", &shared)) return NULL;
+  }
+  if (as_i32(a[6], &hint) || stream_of(a[7], k.device, &st)) return NULL;
+  CALL(rkv_paged_attention(k.ctx, q, &cache, active, shared, (int32_t)n_shared, out, hint, st));
+}
+
+/* paged_sparse_attention(key, q, cache, top_pages, page_idx, out, active, first_pages, last_pages, max_len_hint, stream) */
+static PyObject* paged_sparse_attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Key k;
+  rkv_paged_cache cache;
+  void *q, *idx, *out, *active, *st;
+  int32_t top, first, last, hint;
+  if (count_args(n, 11) || as_key(a[0], &k) || paged_cache(a[2], &k, &cache) || queries(a[1], &k, kRequired, &q) ||
+      as_i32(a[3], &top) ||
+      tensor(a[4], t_i32, k.n_seq * k.n_kv * (long long)top, k.device, kRequired, "page_idx [B, Hkv, top_pages]", &idx) ||
+      queries(a[5], &k, kRequired, &out) || per_seq(a[6], &k, kOptional, &active) || as_i32(a[7], &first) ||
+      as_i32(a[8], &last) || as_i32(a[9], &hint) || stream_of(a[10], k.device, &st))
+    return NULL;
+  if (cache.k_min == NULL) {
+    PyErr_SetString(PyExc_ValueError, "the cache keeps no bounds to select pages by");
+    return NULL;
+  }
+  CALL(rkv_paged_sparse_attention(k.ctx, q, &cache, active, top, first, last, idx, out, hint, st));
+}
+
+/* setup(bfloat16, float32, int32, RkvQuantCache, RkvCache, RopeTable, RkvPagedCache, raw_stream): what the checks compare with */
 static PyObject* setup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  if (count_args(n, 7)) return NULL;
-  PyObject** to[7] = {&t_bf16, &t_f32, &t_i32, &c_quant_cache, &c_cache, &c_table, &f_stream};
-  for (int i = 0; i < 7; ++i) Py_XSETREF(*to[i], Py_NewRef(a[i]));
+  if (count_args(n, 8)) return NULL;
+  PyObject** to[8] = {&t_bf16, &t_f32, &t_i32, &c_quant_cache, &c_cache, &c_table, &c_paged_cache, &f_stream};
+  for (int i = 0; i < 8; ++i) Py_XSETREF(*to[i], Py_NewRef(a[i]));
   Py_RETURN_NONE;
 }
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(setup), METHOD(quant_store), METHOD(quant_full_attention), METHOD(quant_score_keys),
                                 METHOD(quant_select_topk), METHOD(quant_full_step), METHOD(quant_gather_small),
-                                METHOD(rope), {NULL, NULL, 0, NULL}};
+                                METHOD(rope), METHOD(paged_append), METHOD(paged_attention), METHOD(paged_sparse_attention),
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rkv_calls", "Checked calls of librkv.", -1, methods,
                                     NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__rkv_calls(void) {
   PyObject** names[] = {&s_dtype, &s_shape, &s_stride, &s_numel, &s_get_device, &s_is_contiguous, &s_data_ptr,
-                        &s_cuda_stream, &s_device, &s_n_seq, &s_freqs, &s_rot_dim, &s_layout, &s_amplitude};
+                        &s_cuda_stream, &s_device, &s_n_seq, &s_n_kv, &s_freqs, &s_rot_dim, &s_layout, &s_amplitude};
   const char* text[] = {"dtype", "shape", "stride", "numel", "get_device", "is_contiguous", "data_ptr",
-                        "cuda_stream", "device", "n_seq", "freqs", "rot_dim", "layout", "amplitude"};
+                        "cuda_stream", "device", "n_seq", "n_kv", "freqs", "rot_dim", "layout", "amplitude"};
   for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
     if ((*names[i] = PyUnicode_InternFromString(text[i])) == NULL) return NULL;
   return PyModule_Create(&module);

@@ -26,8 +26,10 @@ EXPORTS = ["rkv_create", "rkv_destroy", "rkv_workspace_bytes", "rkv_full_step", 
            "rkv_gather_small_evict", "rkv_append_small_step_evict", "rkv_full_attention", "rkv_select_topk",
            "rkv_append_full_attention", "rkv_get_option", "rkv_score_keys", "rkv_quant_store",
            "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk", "rkv_quant_full_step",
-           "rkv_quant_gather_small", "rkv_rope_frequencies", "rkv_rope"]
+           "rkv_quant_gather_small", "rkv_rope_frequencies", "rkv_rope", "rkv_paged_append", "rkv_paged_attention",
+           "rkv_paged_sparse_attention"]
 QUANT_BLOCK = 64
+PAGE_SIZES = (16, 32, 64, 128)
 NOALLOC_MAX_PROBLEMS, NOALLOC_MAX_LEN = 32, 65536
 OPT_SMALL_MIN_CHUNK, OPT_DEPENDENT_LAUNCH, OPT_SMALL_CLUSTER, OPT_EARLY_CACHE_READ, OPT_INTERLEAVE_TILES = 1, 2, 3, 4, 5
 OPT_SELECT_KEYS_PER_CTA = 6
@@ -50,6 +52,12 @@ class RkvQuantCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_rows", ctypes.c_int64), ("row_offset", ctypes.c_void_p), ("cap", ctypes.c_void_p),
                 ("len", ctypes.c_void_p)]
+
+
+class RkvPagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_min", ctypes.c_void_p), ("k_max", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("len", ctypes.c_void_p)]
 
 
 class RkvRopeConfig(ctypes.Structure):
@@ -121,6 +129,12 @@ def _load() -> ctypes.CDLL:
     lib.rkv_rope_frequencies.argtypes = [ctypes.POINTER(RkvRopeConfig), ctypes.POINTER(ctypes.c_uint64),
                                          ctypes.POINTER(f32)]
     lib.rkv_rope.argtypes = [vp, vp, i32, i64, vp, i32, i32, i32, vp, i32, i32, f32, vp, vp, vp, vp]
+    pagedp = ctypes.POINTER(RkvPagedCache)
+    lib.rkv_paged_append.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, vp, i32, i32, f32, pagedp, vp, vp]
+    lib.rkv_paged_attention.argtypes = [vp, vp, pagedp, vp, vp, i32, vp, i32, vp]
+    lib.rkv_paged_sparse_attention.argtypes = [vp, vp, pagedp, vp, i32, i32, i32, vp, vp, i32, vp]
+    for name in ("rkv_paged_append", "rkv_paged_attention", "rkv_paged_sparse_attention"):
+        getattr(lib, name).restype = i32
     for name in ("rkv_rope_frequencies", "rkv_rope", "rkv_quant_store", "rkv_quant_full_attention", "rkv_quant_score_keys", "rkv_quant_select_topk",
                  "rkv_quant_full_step", "rkv_quant_gather_small"):
         getattr(lib, name).restype = i32
@@ -197,6 +211,32 @@ def quant_cache_struct(k8, v8, k_scale, v_scale, row_offset, cap, length) -> Rkv
     return c
 
 
+def paged_cache_struct(k, v, table, length, k_min=None, k_max=None) -> RkvPagedCache:
+    """Describe a paged K/V cache (see include/rkv.h).  The caller keeps the tensors alive.
+
+    k, v: bfloat16 [n_pages, Hkv, page, 128], page 16, 32, 64 or 128; table: int32 [B, pages of a sequence at most];
+    length: int32 [B]; k_min, k_max: bfloat16 [n_pages, Hkv, 128], the bounds of every page's keys, or both None."""
+    if k.dtype != torch.bfloat16 or k.dim() != 4 or k.shape[3] != 128 or k.shape[2] not in PAGE_SIZES or k.numel() == 0:
+        raise ValueError("k is a bfloat16 tensor [n_pages, Hkv, page, 128], page one of 16, 32, 64, 128")
+    if v.dtype != torch.bfloat16 or v.shape != k.shape:
+        raise ValueError("v has the shape and type of k")
+    if (k_min is None) != (k_max is None):
+        raise ValueError("k_min and k_max come together")
+    for t in (k_min, k_max):
+        if t is not None and (t.dtype != torch.bfloat16 or t.shape != (k.shape[0], k.shape[1], 128)):
+            raise ValueError("k_min and k_max are bfloat16 tensors [n_pages, Hkv, 128]")
+    if table.dtype != torch.int32 or table.dim() != 2 or table.numel() == 0:
+        raise ValueError("table is an int32 tensor [B, pages]")
+    if length.dtype != torch.int32 or length.numel() != table.shape[0]:
+        raise ValueError("length is an int32 tensor with one element per row of the table")
+    if any(t is not None and t.device != k.device for t in (v, k_min, k_max, table, length)):
+        raise ValueError("the tensors of a cache are on one device")
+    c = RkvPagedCache(_ptr(k), _ptr(v), _ptr(k_min), _ptr(k_max), k.shape[0], k.shape[2], table.shape[1], _ptr(table),
+                      _ptr(length))
+    c.device, c.n_seq, c.n_kv = k.device.index, table.shape[0], k.shape[1]
+    return c
+
+
 class RopeTable:
     """What rkv_rope needs of a model's rotary positions, laid out once: the frequencies as fixed-point turns on the
     device, the rotated part, the pairs' layout and the amplitude (formulas: include/rkv.h).
@@ -234,7 +274,8 @@ class _LazyCalls:
         raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw_stream is None:
             raw_stream = lambda device: torch.cuda.current_stream(device).cuda_stream
-        _rkv_calls.setup(torch.bfloat16, torch.float32, torch.int32, RkvQuantCache, RkvCache, RopeTable, raw_stream)
+        _rkv_calls.setup(torch.bfloat16, torch.float32, torch.int32, RkvQuantCache, RkvCache, RopeTable,
+                         RkvPagedCache, raw_stream)
         _calls = _rkv_calls
         return getattr(_rkv_calls, name)
 
@@ -412,6 +453,32 @@ class Context:
         rc = _calls.rope(self._key, qkv, pos, table, q, k, v, stream)
         if rc:
             self._done(rc, _calls.rope, self._key, qkv, pos, table, q, k, v, stream)
+
+    # ------------------------------------------------------------------ the paged cache
+    def paged_append(self, qkv, cache: RkvPagedCache, table: RopeTable | None, q, start=None, count=None, stream=None):
+        """Rows of the fused projection [B, T, (Hq + 2 Hkv) * 128] (bfloat16 or float32; sequences and tokens may be
+        strided): queries go to q [B, T, Hq, 128] (bfloat16), keys and values to their pages, queries and keys turned by
+        their positions in the sequence (table=None: not turned).  start, count: int32 [B] or None."""
+        rc = _calls.paged_append(self._key, qkv, cache, table, q, start, count, stream)
+        if rc:
+            self._done(rc, _calls.paged_append, self._key, qkv, cache, table, q, start, count, stream)
+
+    def paged_attention(self, q, cache: RkvPagedCache, out, active=None, shared=None, max_len_hint=0, stream=None):
+        """Attention over a paged cache.  shared: int32 tensor of the pages that every sequence begins with, or None; they
+        are read once for the whole batch."""
+        rc = _calls.paged_attention(self._key, q, cache, out, active, shared, max_len_hint, stream)
+        if rc:
+            self._done(rc, _calls.paged_attention, self._key, q, cache, out, active, shared, max_len_hint, stream)
+
+    def paged_sparse_attention(self, q, cache: RkvPagedCache, top_pages, page_idx, out, active=None, first_pages=1,
+                               last_pages=1, max_len_hint=0, stream=None):
+        """Attention over the top_pages pages of every sequence and KV head whose keys' bounds promise the largest scores,
+        the first first_pages and the last last_pages in any case.  page_idx: int32 [B, Hkv, top_pages], an output."""
+        rc = _calls.paged_sparse_attention(self._key, q, cache, top_pages, page_idx, out, active, first_pages, last_pages,
+                                           max_len_hint, stream)
+        if rc:
+            self._done(rc, _calls.paged_sparse_attention, self._key, q, cache, top_pages, page_idx, out, active,
+                       first_pages, last_pages, max_len_hint, stream)
 
     def should_refresh(self, q_now, q_last_full, threshold, flag, sim=None, keep=None, stream=None):
         self._check(lib.rkv_should_refresh(self._h, _ptr(q_now), _ptr(q_last_full), float(threshold), _ptr(flag),
