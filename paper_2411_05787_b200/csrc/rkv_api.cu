@@ -127,11 +127,13 @@ bool on_device(const rkv_ctx* ctx) {
 }
 
 // [n_rows][128] bf16 as {64 channels, row, half}: one box = 64 rows x both halves, 128-byte swizzle.
-// quant: [n_rows][128] codes, one box = 128 rows.  paged_box: the rows of a pool of pages, one box = this many of them.
-rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out, bool quant = false, int paged_box = 0) {
+// quant: [n_rows][128] codes, one box = 128 rows.  paged_box: the rows of a pool of pages, one box = this many of them, of
+// both 64-channel halves or of one.
+rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out, bool quant = false, int paged_box = 0,
+                      int halves = 2) {
   // the map depends on nothing else
   const std::pair<uint64_t, int64_t> key(reinterpret_cast<uint64_t>(base),
-                                         quant ? -n_rows : n_rows + ((int64_t)paged_box << 32));
+                                         quant ? -n_rows : n_rows + ((int64_t)(paged_box * halves) << 32) + ((int64_t)halves << 48));
   auto it = ctx->tmaps.find(key);
   if (it != ctx->tmaps.end()) { *out = it->second; return RKV_OK; }
   if (g_encode == nullptr) {
@@ -144,7 +146,7 @@ rkv_status tensor_map(rkv_ctx* ctx, void* base, int64_t n_rows, CUtensorMap* out
   }
   CUtensorMap tm;
   CUresult r = quant           ? rkv::encode_quant_map(g_encode, base, n_rows, &tm)
-               : paged_box > 0 ? rkv::encode_paged_map(g_encode, base, n_rows, paged_box, &tm)
+               : paged_box > 0 ? rkv::encode_paged_map(g_encode, base, n_rows, paged_box, halves, &tm)
                                : rkv::encode_cache_map(g_encode, base, n_rows, &tm);
   if (r != CUDA_SUCCESS) {
     ctx->last_error = "cuTensorMapEncodeTiled failed with CUresult " + std::to_string((int)r);
@@ -505,6 +507,7 @@ rkv_status rkv_create(const rkv_config* cfg, rkv_ctx** out) {
       if (e == cudaSuccess) e = rkv::prepare_quant_attention();
       if (e == cudaSuccess) e = rkv::prepare_page_select();
       if (e == cudaSuccess) e = rkv::prepare_paged_attention();
+      if (e == cudaSuccess) e = rkv::prepare_prefix_attention();
       if (e != cudaSuccess) { delete ctx; return RKV_ERR_CUDA; }
       g_prepared[ctx->device] = true;
     }
@@ -971,8 +974,51 @@ rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cach
   if (n_max < 1 || n_max > ctx->cfg.max_len || n_shared < 0 || (shared == nullptr) != (n_shared == 0))
     return RKV_ERR_INVALID_ARG;
   ctx->pending_full.valid = false;   // its partials and logits are about to be overwritten
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
   rkv::PagedAttnParams p = paged_params(ctx, cache, q, active, out, n_max);
-  return run_paged_attention(ctx, p, cache, n_max, RKV_KERNEL_ATTN_FULL, static_cast<cudaStream_t>(stream));
+  const int64_t from = (int64_t)n_shared * cache->page;
+  // A batch of one shares with nobody; and there has to be a slot for the shared positions beside the sequences' own.
+  if (from == 0 || from > n_max || ctx->cfg.n_seq == 1 || ctx->max_splits < 2)
+    return run_paged_attention(ctx, p, cache, n_max, RKV_KERNEL_ATTN_FULL, st);
+  rkv::PrefixAttnParams x;
+  memset(&x, 0, sizeof(x));
+  x.c = p.c;
+  x.q = q;
+  x.shared = shared;
+  x.partials = ctx->partials;
+  x.ml_t = ctx->ml_t;
+  x.status = ctx->status;
+  x.n_rows = cache->n_pages * ctx->cfg.n_kv_heads * cache->page;
+  x.n_shared = n_shared;
+  x.n_seq = ctx->cfg.n_seq;
+  x.n_q_heads = ctx->cfg.n_q_heads;
+  x.group = ctx->group;
+  x.max_splits = ctx->max_splits;
+  x.scale = ctx->cfg.softmax_scale;
+  CUtensorMap tm_k, tm_v;
+  const int box = cache->page < rkv::kPrefixTile ? cache->page : rkv::kPrefixTile;
+  rkv_status s = tensor_map(ctx, cache->k, x.n_rows, &tm_k, false, box, 1);
+  if (s != RKV_OK) return s;
+  s = tensor_map(ctx, cache->v, x.n_rows, &tm_v, false, box, 1);
+  if (s != RKV_OK) return s;
+  // one wave of CTAs, one to an SM
+  const int tiles = (int)((from + rkv::kPrefixTile - 1) / rkv::kPrefixTile);
+  const int blocks = (ctx->cfg.n_seq * ctx->group + 127) / 128 * ctx->cfg.n_kv_heads;
+  int splits = ctx->sm_count / blocks;
+  if (splits > tiles) splits = tiles;
+  if (splits > ctx->max_splits / 2) splits = ctx->max_splits / 2;
+  if (splits < 1) splits = 1;
+  cudaError_t e;
+  {
+    LaunchScope scope(ctx, st, RKV_KERNEL_ATTN_FULL);
+    e = rkv::launch_prefix_attention(x, tm_k, tm_v, splits, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "shared attention launch");
+  ctx->launches += 1;
+  rkv::note_launch(st, nullptr, nullptr);
+  p.from = (int)from;
+  p.first_slot = splits;
+  return run_paged_attention(ctx, p, cache, n_max > from ? n_max - (int)from : 1, RKV_KERNEL_ATTN_FULL, st);
 }
 
 rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cache* cache, const int32_t* active,

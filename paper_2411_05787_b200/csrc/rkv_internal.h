@@ -226,6 +226,22 @@ cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& 
 cudaError_t launch_paged_fold(const PagedAttnParams& p, int n_seq, int grid_x, cudaStream_t st);
 cudaError_t prepare_paged_attention();
 
+// The positions that all sequences of a batch share.
+constexpr int kPrefixTile = 128;
+struct PrefixAttnParams {
+  PagedDev c;
+  const void* q;
+  const int32_t* shared;      // [n_shared] pages
+  float* partials; float* ml_t;     // as in AttnParams: slots 0 .. splits - 1
+  int32_t* status;
+  int64_t n_rows;             // of the pool
+  int32_t n_shared, n_seq, n_q_heads, group, max_splits;
+  float scale;
+};
+cudaError_t launch_prefix_attention(const PrefixAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int splits,
+                                    cudaStream_t st);
+cudaError_t prepare_prefix_attention();
+
 cudaError_t launch_attention(const AttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                              int n_seq, int grid_x, bool write_logits, cudaStream_t st, bool append = false);
 cudaError_t launch_attention_cluster(const AttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
@@ -328,11 +344,12 @@ inline CUresult encode_cache_map(EncodeTiledFn encode, void* base, int64_t n_row
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-// A pool of pages ([n_pages][Hkv][page][128] bf16): the same with a box of one page, or of 64 rows where a page is larger.
-inline CUresult encode_paged_map(EncodeTiledFn encode, void* base, int64_t n_rows, int box_rows, CUtensorMap* out) {
+// A pool of pages ([n_pages][Hkv][page][128] bf16): the same with a box of one page, or of as many rows as a tile has where
+// a page is larger, of both 64-channel halves or of one.
+inline CUresult encode_paged_map(EncodeTiledFn encode, void* base, int64_t n_rows, int box_rows, int halves, CUtensorMap* out) {
   const cuuint64_t dims[3] = {64, (cuuint64_t)n_rows, 2};
   const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim * 2, 128};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)halves};
   const cuuint32_t estr[3] = {1, 1, 1};
   return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
