@@ -1003,7 +1003,7 @@ rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cach
   if (s != RKV_OK) return s;
   // one wave of CTAs, one to an SM
   const int tiles = (int)((from + rkv::kPrefixTile - 1) / rkv::kPrefixTile);
-  const int blocks = (ctx->cfg.n_seq * ctx->group + 127) / 128 * ctx->cfg.n_kv_heads;
+  const int blocks = (ctx->cfg.n_seq * ctx->group + 255) / 256 * ctx->cfg.n_kv_heads;
   int splits = ctx->sm_count / blocks;
   if (splits > tiles) splits = tiles;
   if (splits > ctx->max_splits / 2) splits = ctx->max_splits / 2;

@@ -227,7 +227,7 @@ cudaError_t launch_paged_fold(const PagedAttnParams& p, int n_seq, int grid_x, c
 cudaError_t prepare_paged_attention();
 
 // The positions that all sequences of a batch share.
-constexpr int kPrefixTile = 128;
+constexpr int kPrefixTile = 64;
 struct PrefixAttnParams {
   PagedDev c;
   const void* q;
