@@ -909,7 +909,12 @@ rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int6
   return RKV_OK;
 }
 
-// The pass over pages, in one of two forms (the rule and its measurements stand at the top of this function).
+// The pass over pages, in one of three forms:
+//   splits    a head's tiles are dealt out in turn to as many CTAs per KV head as fit one wave (two to an SM), a fold finishes
+//   cluster   1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves: while no CTA can get
+//             more than 8 tiles
+//   balanced  longer batches, and what sequences hold behind a shared prefix (whose partials have to be folded in any case):
+//             equal runs of tiles across heads and sequences, then the fold
 static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, const rkv_paged_cache* cache, int most,
                                       int kind, cudaStream_t st) {
   CUtensorMap tm_k, tm_v;
@@ -927,11 +932,17 @@ static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, con
   if (gx < 1) gx = 1;
   const int cluster_gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
   const bool cluster = p.first_slot == 0 && tiles <= 8 * cluster_gx;
+  // tiles that there can be: behind a shared prefix a sequence may be shorter than that, but not as long in all
+  const int64_t units = bg * ((p.max_len + rkv::kTile - 1) / rkv::kTile + 1);
+  const bool balanced = !cluster && ctx->cfg.n_seq > 1 && ctx->cfg.n_seq <= rkv::kBalancedMaxSeq &&
+                        units * (slots + 1) < (int64_t(1) << 32);   // (the kernel cuts the runs in 32 bits)
   if (cluster) gx = cluster_gx;
+  p.counts = balanced ? ctx->split_counts : nullptr;
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, kind);
-    e = rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, st);
+    e = balanced ? rkv::launch_paged_balanced(p, tm_k, tm_v, (int)(units < slots ? units : slots), st)
+                 : rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "paged attention launch");
   ctx->launches += 1;
@@ -958,6 +969,7 @@ static rkv::PagedAttnParams paged_params(const rkv_ctx* ctx, const rkv_paged_cac
   p.partials = ctx->partials;
   p.ml_t = ctx->ml_t;
   p.status = ctx->status;
+  p.n_seq = ctx->cfg.n_seq;
   p.n_q_heads = ctx->cfg.n_q_heads;
   p.group = ctx->group;
   p.max_splits = ctx->max_splits;

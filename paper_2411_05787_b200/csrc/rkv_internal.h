@@ -210,19 +210,23 @@ cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pa
 cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
 cudaError_t prepare_page_select();
 
+constexpr int kBalancedMaxSeq = 256;   // sequences of a batch that the balanced pass over pages takes
 struct PagedAttnParams {
   PagedDev c;
   const void* q; const int32_t* active; void* out;
   const int32_t* page_idx;    // [B][Hkv][top]: the pages attended, or null: all positions from `from` on
   float* partials; float* ml_t;     // as in AttnParams
+  int32_t* counts;            // [B*Hkv]: own partials of each head (balanced form), or null
   int32_t* status;
-  int32_t n_q_heads, group, top, max_splits, max_len;
+  int32_t n_seq, n_q_heads, group, top, max_splits, max_len;
   int32_t from;               // positions that the batch shares: sequences that reach so far begin behind them
   int32_t first_slot;         // split partials of the shared positions
   float scale;
 };
 cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_seq,
                                    int grid_x, bool cluster, cudaStream_t st);
+cudaError_t launch_paged_balanced(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_cta,
+                                  cudaStream_t st);
 cudaError_t launch_paged_fold(const PagedAttnParams& p, int n_seq, int grid_x, cudaStream_t st);
 cudaError_t prepare_paged_attention();
 
