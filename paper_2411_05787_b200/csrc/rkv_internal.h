@@ -191,7 +191,7 @@ struct PagedAppendParams {
   int32_t* tickets; int32_t* status;
   int32_t n_tok, n_q_heads, rot;
   float amp;
-  int32_t rounds;                                      // heads a warp takes, one after the other
+  int32_t q_groups, q_per, rounds;                     // CTAs of a unit for the queries, their heads; heads of keys or values per warp
 };
 cudaError_t launch_paged_append(const PagedAppendParams& p, bool is_bf16, bool interleaved, int n_seq, int sm_count,
                                 cudaStream_t st);

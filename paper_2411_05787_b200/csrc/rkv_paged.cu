@@ -15,187 +15,361 @@ namespace {
 // HBM-bound for prompts: every channel is read once and written once.  A CTA takes the new rows of kUnit positions (or of
 // one page, where that is more) for 8 or more heads, a warp one head at a time over all of those rows, so that a page's
 // bounds stay in the warp's registers until the page ends, and no two CTAs meet at a page and head.  Eight threads share
-// a row, each with two pieces of eight channels (eight pairs, or channels that are only copied); a warp has four rows of
-// four groups of its rows in flight.  Sines and cosines of the unit's (row, pair)s are worked out once per CTA, in shared memory.
+// a row, each with two pieces of eight channels (eight pairs, or channels that are only copied).  A warp works through batches
+// of 16 rows, four of a thread's, all of them requested before the first is used.  Sines and cosines of the unit's (row, pair)s
+// are worked out once per CTA, in shared memory, while the first batch is on its way.
+// With up to kFewRows rows a sequence (tokens of a decode step) eight threads take a head, and a CTA 32 of them.
 constexpr int kAppendThreads = 256, kAppendWarps = kAppendThreads / 32;
 constexpr int kUnit = 64;                    // positions of a CTA
-constexpr int kAppendAhead = 4;              // rows of a thread in flight
-constexpr int kCsRow = kHeadDim / 2 + 8;     // (and the four rows of a warp beside each other)
+constexpr int kBatchRows = 16, kAhead = kBatchRows / 4;      // rows of a warp in flight, and of a thread
+constexpr int kFewRows = 4;
+constexpr int kAppendSpread = 6;
+constexpr int kCsRow = kHeadDim / 2 + 8;     // (the four rows of a warp beside each other in the banks)
+static_assert(kUnit % kBatchRows == 0, "whole batches");
 
-template <typename T, bool kInterleaved>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedAppendParams p) {
-  __shared__ float2 sm_cs[kUnit][kCsRow];       // pair 8 i + j of a row at 8 j + i: the eight threads of a row read side by side
-  __shared__ int sm_sizes[3];
-  __shared__ int sm_page[kUnit / 16];
-  const int b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int part = tid & 7, octet = lane >> 3;
-  const int n_kv = p.c.n_kv_heads, heads = p.n_q_heads + 2 * n_kv;
-  const int page = 1 << p.c.page_shift, unit = page > kUnit ? page : kUnit;
-  const int half = p.rot >> 1;
-  const bool turns = part < (p.rot >> 4);
-  const int ca = (kInterleaved || !turns) ? 16 * part : 8 * part;          // this thread's pieces of a row
-  const int cb = (kInterleaved || !turns) ? 16 * part + 8 : half + 8 * part;
-  pdl_wait();
-  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
-  // One thread reads the sizes for its CTA; behind the barrier it draws a ticket, the last of which writes the new length:
-  // a ticket says that nobody in its CTA will read the sizes again.
+struct AppendShared {
+  float2 cs[kUnit][kCsRow];                  // pair 8 i + j of a row at 8 j + i: the eight threads of a row read side by side
+  int sizes[3];
+  int page[kUnit / 16];
+};
+
+struct BulkShared : AppendShared {
+  float2 ef[16][kHeadDim / 2];               // of rows 0, 8, .., 56 of the unit, and of 0 .. 7 positions
+};
+
+struct NewRows { int start, count; };
+
+// One thread reads the sizes for its CTA; behind the barrier it draws a ticket, the last of which writes the new length:
+// a ticket says that nobody in its CTA will read the sizes again.
+__device__ __forceinline__ NewRows append_sizes(const PagedAppendParams& p, AppendShared& sm, int b, int tid) {
   if (tid == 0) {
     const int l = __ldcg(p.c.len + b);
-    sm_sizes[0] = l;
-    sm_sizes[1] = p.start != nullptr ? __ldcg(p.start + b) : l;
-    sm_sizes[2] = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
+    sm.sizes[0] = l;
+    sm.sizes[1] = p.start != nullptr ? __ldcg(p.start + b) : l;
+    sm.sizes[2] = p.count != nullptr ? __ldcg(p.count + b) : p.n_tok;
   }
   __syncthreads();
   int ticket = -1;
   if (tid == 0) ticket = atomicAdd(p.tickets + b, 1);
-  const int len = sm_sizes[0], start = sm_sizes[1];
+  NewRows n;
+  n.start = sm.sizes[1];
+  n.count = min(max(sm.sizes[2], 0), p.n_tok);
   const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
-  int count = min(max(sm_sizes[2], 0), p.n_tok);
-  const bool sound = start >= 0 && start <= len && start <= room;
+  const bool sound = n.start >= 0 && n.start <= sm.sizes[0] && n.start <= room;
   int flags = 0;
   if (!sound) {
     flags = RKV_DEV_LEN_CLAMPED;
-    count = 0;
-  } else if (count > room - start) {
+    n.count = 0;
+  } else if (n.count > room - n.start) {
     flags = RKV_DEV_APPEND_OVERFLOW;
-    count = (int)(room - start);
+    n.count = (int)(room - n.start);
   }
-  const int64_t end = (int64_t)start + count;
-  const int64_t u0 = ((int64_t)start / unit + blockIdx.x) * unit;          // the CTA's positions
-  const int64_t first = u0 > start ? u0 : start, last = u0 + unit < end ? u0 + unit : end;
   if (tid == 0) {
     if (ticket == (int)(gridDim.x * gridDim.y) - 1) {
-      if (sound) p.c.len[b] = (int)end;
+      if (sound) p.c.len[b] = n.start + n.count;
       p.tickets[b] = 0;   // ready for the next call on this stream
     }
     if (flags != 0 && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, flags);
   }
-  if (count <= 0 || first >= last) return;
+  return n;
+}
 
-  const T* rows = static_cast<const T*>(p.qkv) + (int64_t)b * p.seq_stride;
+// (cos, sin) of a position's angle, and of the sum of two angles.
+__device__ __forceinline__ float2 angle(int64_t pos, unsigned long long freq) {
+  float s, c;
+  sincospif((float)(int)(((unsigned long long)pos * freq) >> 32) * 4.656612873e-10f, &s, &c);   // 2^-31: half turns
+  return make_float2(c, s);
+}
+__device__ __forceinline__ float2 turn_by(float2 a, float2 b) {
+  return make_float2(__fmaf_rn(a.x, b.x, -__fmul_rn(a.y, b.y)), __fmaf_rn(a.x, b.y, __fmul_rn(a.y, b.x)));
+}
+
+// Pages and angles of the rows of positions lo .. hi - 1, which lie in the unit (or the half of a page of 128) that begins at
+// s0; row r of it at sm.cs[r].
+template <bool kFew, typename Shared>
+__device__ __forceinline__ void append_part(const PagedAppendParams& p, Shared& sm, int b, int64_t s0, int64_t lo, int64_t hi,
+                                            int tid) {
+  const int most = min(1 << p.c.page_shift, kUnit);       // positions of a page in this part
+  if (tid < kUnit / most) {
+    const int64_t at = s0 + tid * most;
+    int pg = -1;
+    if (at < hi && at + most > lo) {
+      pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + (at >> p.c.page_shift));
+      if ((unsigned)pg >= (unsigned)p.c.n_pages) {
+        pg = -1;
+        if (blockIdx.y == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+      }
+    }
+    sm.page[tid] = pg;
+  }
+  // a row's angle is that of the multiple of 8 below it and that of the rest: 16 sines and cosines a pair instead of 64
+  const int half = p.rot >> 1, r0 = (int)(lo - s0), n = (int)(hi - lo);
+  auto put = [&](int r, int j, float2 e) { sm.cs[r][8 * (j & 7) + (j >> 3)] = make_float2(e.x * p.amp, e.y * p.amp); };
+  if constexpr (kFew) {
+    for (int i = tid; i < n * half; i += kAppendThreads) {
+      const int r = r0 + i / half, j = i % half;
+      const unsigned long long f = __ldg(p.freqs + j);
+      put(r, j, turn_by(angle(s0 + (r & ~7), f), angle(r & 7, f)));
+    }
+  } else {
+    for (int i = tid; i < 16 * half; i += kAppendThreads) {
+      const int k = i / half, j = i - k * half;
+      sm.ef[k][j] = angle(k < 8 ? s0 + 8 * k : k - 8, __ldg(p.freqs + j));
+    }
+    __syncthreads();
+    for (int i = tid; i < n * half; i += kAppendThreads) {
+      const int r = r0 + i / half, j = i % half;
+      put(r, j, turn_by(sm.ef[r >> 3][j], sm.ef[8 + (r & 7)][j]));
+    }
+  }
+}
+
+// The eight pairs of a thread's two pieces.
+template <bool kInterleaved>
+__device__ __forceinline__ void turn_pieces(float (&a)[8], float (&w)[8], const float2 (&cs)[8]) {
+  if (kInterleaved) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 e = cs[j], f = cs[4 + j];
+      const float x = a[2 * j], y = a[2 * j + 1], z = w[2 * j], u = w[2 * j + 1];
+      a[2 * j] = x * e.x - y * e.y;
+      a[2 * j + 1] = x * e.y + y * e.x;
+      w[2 * j] = z * f.x - u * f.y;
+      w[2 * j + 1] = z * f.y + u * f.x;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 e = cs[j];
+      const float x = a[j], y = w[j];
+      a[j] = x * e.x - y * e.y;
+      w[j] = x * e.y + y * e.x;
+    }
+  }
+}
+
+// A page's bounds of one head leave, this thread's two pieces of them; joins: it keeps what it had.
+__device__ __forceinline__ void store_bounds(const PagedAppendParams& p, Bounds8& ba, Bounds8& bb, int pg, int g, int ca, int cb,
+                                             bool joins) {
+  const int64_t at = ((int64_t)pg * p.c.n_kv_heads + g) * kHeadDim;
+  uint4* lo4 = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.c.k_min) + at);
+  uint4* hi4 = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.c.k_max) + at);
+  if (joins) {
+    ba.join(__ldcg(lo4 + ca / 8), __ldcg(hi4 + ca / 8));
+    bb.join(__ldcg(lo4 + cb / 8), __ldcg(hi4 + cb / 8));
+  }
+  lo4[ca / 8] = ba.lo4();
+  lo4[cb / 8] = bb.lo4();
+  hi4[ca / 8] = ba.hi4();
+  hi4[cb / 8] = bb.hi4();
+}
+
+struct Head {   // of the fused projection
+  bool is_q, is_k;
+  int g;
+  __device__ __forceinline__ Head(const PagedAppendParams& p, int h) {
+    is_q = h < p.n_q_heads;
+    is_k = !is_q && h < p.n_q_heads + p.c.n_kv_heads;
+    g = is_q ? h : h - p.n_q_heads - (is_k ? 0 : p.c.n_kv_heads);
+  }
+  // where the row of position pos (token t) goes; null: its page is not there
+  __device__ __forceinline__ __nv_bfloat16* row(const PagedAppendParams& p, int b, int t, int64_t pos, int pg) const {
+    if (is_q) return static_cast<__nv_bfloat16*>(p.q) + (((int64_t)b * p.n_tok + t) * p.n_q_heads + g) * kHeadDim;
+    if (pg < 0) return nullptr;
+    return static_cast<__nv_bfloat16*>(is_k ? p.c.k : p.c.v) +
+           ((((int64_t)pg * p.c.n_kv_heads + g) << p.c.page_shift) + (pos & ((1 << p.c.page_shift) - 1))) * kHeadDim;
+  }
+};
+
+template <typename T, bool kInterleaved>
+__global__ void __launch_bounds__(kAppendThreads, 2) paged_append_kernel(const PagedAppendParams p) {
+  __shared__ BulkShared sm;
+  const int b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int part = tid & 7, octet = lane >> 3;
+  const int page = 1 << p.c.page_shift, unit = page > kUnit ? page : kUnit, most = page < kUnit ? page : kUnit;
+  const bool turns = part < (p.rot >> 4);
+  const int ca = (kInterleaved || !turns) ? 16 * part : 8 * part;          // this thread's pieces of a row
+  const int cb = (kInterleaved || !turns) ? 16 * part + 8 : (p.rot >> 1) + 8 * part;
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  const NewRows nr = append_sizes(p, sm, b, tid);
+  const int64_t end = (int64_t)nr.start + nr.count;
+  const int64_t u0 = ((int64_t)nr.start / unit + blockIdx.x) * unit;       // the CTA's positions
+  const int64_t first = u0 > nr.start ? u0 : nr.start, last = u0 + unit < end ? u0 + unit : end;
+  if (nr.count <= 0 || first >= last) return;
+
+  const int heads = p.n_q_heads + 2 * p.c.n_kv_heads, y_kv = (int)blockIdx.y - p.q_groups;   // < 0: queries
+  const int h0 = p.n_q_heads + max(y_kv, 0) * p.rounds * kAppendWarps + warp;
+  const int n_heads = min(p.rounds, (heads - h0 + kAppendWarps - 1) / kAppendWarps);   // of this warp: h0, h0 + 8, ...
+  const T* rows = static_cast<const T*>(p.qkv) + (int64_t)b * p.seq_stride - (int64_t)nr.start * p.tok_stride;   // by position
   for (int64_t s0 = u0; s0 < last; s0 += kUnit) {       // (once, but for pages of 128)
     const int64_t lo = s0 > first ? s0 : first, hi = s0 + kUnit < last ? s0 + kUnit : last;
     if (lo >= hi) continue;
-    const int n = (int)(hi - lo), off = (int)(lo - s0);   // rows, and the first one's place in the unit
+    const int r0 = (int)(lo - s0), r1 = (int)(hi - s0);   // rows of this part
+    const int c0 = r0 / kBatchRows, c1 = (r1 + kBatchRows - 1) / kBatchRows;   // batches
     if (s0 != u0) __syncthreads();                       // (the sines of the half before are still in use)
-    const int most = page < kUnit ? page : kUnit;         // positions of a page in this part of the unit
-    if (tid < kUnit / most) {
-      const int64_t at = s0 + tid * most;
-      int pg = -1;
-      if (at < hi && at + most > lo) {
-        pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + (at >> p.c.page_shift));
-        if ((unsigned)pg >= (unsigned)p.c.n_pages) {
-          pg = -1;
-          if (blockIdx.y == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
-        }
-      }
-      sm_page[tid] = pg;
-    }
-    for (int i = tid; i < n * half; i += kAppendThreads) {
-      const int r = i / half, j = i - r * half;
-      const unsigned long long t = (unsigned long long)(lo + r) * __ldg(p.freqs + j);
-      float s, c;
-      sincospif((float)(int)(t >> 32) * 4.656612873e-10f, &s, &c);   // 2^-31: half turns
-      sm_cs[r][8 * (j & 7) + (j >> 3)] = make_float2(c * p.amp, s * p.amp);
-    }
+    append_part<false>(p, sm, b, s0, lo, hi, tid);
     __syncthreads();
-    for (int round = 0; round < p.rounds; ++round) {
-      const int h = ((int)blockIdx.y * p.rounds + round) * kAppendWarps + warp;
-      if (h >= heads) break;
-      const bool is_q = h < p.n_q_heads, is_k = !is_q && h < p.n_q_heads + n_kv;
-      const int g = is_q ? 0 : is_k ? h - p.n_q_heads : h - p.n_q_heads - n_kv;
-      const bool turn = turns && (is_q || is_k);
-      const bool bounds = is_k && p.c.k_min != nullptr;
-      __nv_bfloat16* pool = static_cast<__nv_bfloat16*>(is_k ? p.c.k : p.c.v);
-      Bounds8 ba, bb;
-      ba.reset();
-      bb.reset();
-      // positions page by page: rows off .. off + n - 1 of this part
-      for (int pi = off / most; pi * most < off + n; ++pi) {
-        const int r0 = max(pi * most, off), r1 = min((pi + 1) * most, off + n);
-        const int pg = sm_page[pi];
-        const int64_t pos0 = s0 + r0;
-        if (bounds && (r0 & (most - 1)) == 0 && (pos0 & (page - 1)) == 0) {
-          ba.reset();
-          bb.reset();
-        }
-        for (int r = r0 + octet; r < r1; r += 4 * kAppendAhead) {
-          Raw8<T> xa[kAppendAhead], xb[kAppendAhead];
+    const T* part_rows = rows + s0 * p.tok_stride;
+    if (y_kv < 0) {   // queries: eight threads go through a row's heads
+      const int q0 = (int)blockIdx.y * p.q_per, q1 = min(q0 + p.q_per, p.n_q_heads);
+      for (int r = r0 + 4 * warp + octet; r < r1; r += 4 * kAppendWarps) {
+        float2 cs[8];
+        if (turns) {
 #pragma unroll
-          for (int i = 0; i < kAppendAhead; ++i) {
-            if (r + 4 * i < r1) {
-              const T* x = rows + (s0 + r + 4 * i - start) * p.tok_stride + h * kHeadDim;
-              xa[i].load(x + ca);
-              xb[i].load(x + cb);
-            }
+          for (int j = 0; j < 8; ++j) cs[j] = sm.cs[r][part + 8 * j];
+        }
+        const T* x = part_rows + r * p.tok_stride;
+        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.q) +
+                            ((int64_t)b * p.n_tok + (s0 + r - nr.start)) * p.n_q_heads * kHeadDim;
+        for (int h = q0; h < q1; h += kAhead) {
+          Raw8<T> xa[kAhead], xb[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {   // (heads beyond the last are loaded in place of it, and not used)
+            const int hh = min(h + i, q1 - 1);
+            xa[i].load(x + hh * kHeadDim + ca);
+            xb[i].load(x + hh * kHeadDim + cb);
           }
 #pragma unroll
-          for (int i = 0; i < kAppendAhead; ++i) {
-            const int rr = r + 4 * i;
-            if (rr >= r1) break;
+          for (int i = 0; i < kAhead; ++i) {
             float a[8], w[8];
             xa[i].get(a);
             xb[i].get(w);
-            if (turn) {
-              const float2* cs = &sm_cs[rr - off][part];
-              if (kInterleaved) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const float2 e = cs[8 * j], f = cs[8 * (4 + j)];
-                  const float x = a[2 * j], y = a[2 * j + 1], z = w[2 * j], u = w[2 * j + 1];
-                  a[2 * j] = x * e.x - y * e.y;
-                  a[2 * j + 1] = x * e.y + y * e.x;
-                  w[2 * j] = z * f.x - u * f.y;
-                  w[2 * j + 1] = z * f.y + u * f.x;
-                }
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const float2 e = cs[8 * j];
-                  const float x = a[j], y = w[j];
-                  a[j] = x * e.x - y * e.y;
-                  w[j] = x * e.y + y * e.x;
-                }
-              }
+            if (turns) turn_pieces<kInterleaved>(a, w, cs);
+            if (h + i < q1) {
+              *reinterpret_cast<uint4*>(to + (h + i) * kHeadDim + ca) = pack8(a);
+              *reinterpret_cast<uint4*>(to + (h + i) * kHeadDim + cb) = pack8(w);
             }
-            const uint4 pa = pack8(a), pb = pack8(w);
+          }
+        }
+      }
+      continue;
+    }
+    for (int round = 0; round < n_heads; ++round) {
+      const int h = h0 + round * kAppendWarps;
+      const Head head(p, h);
+      const bool turn = turns && (head.is_q || head.is_k), bounds = head.is_k && p.c.k_min != nullptr;
+      const T* x = part_rows + h * kHeadDim;
+      Bounds8 ba, bb;
+      ba.reset();
+      bb.reset();
+      for (int c = c0; c < c1; ++c) {
+        const int at = c * kBatchRows, pg = sm.page[at / most];
+        // rows that are not new are loaded in place of others, and not used
+        Raw8<T> xa[kAhead], xb[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int r = min(max(at + 4 * i + octet, r0), r1 - 1);
+          xa[i].load(x + r * p.tok_stride + ca);
+          xb[i].load(x + r * p.tok_stride + cb);
+        }
+        __nv_bfloat16* to = head.row(p, b, (int)(s0 + at + octet - nr.start), s0 + at + octet, pg);
+        const int64_t to_step = head.is_q ? (int64_t)p.n_q_heads * kHeadDim : kHeadDim;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int r = at + 4 * i + octet;
+          const bool live = r >= r0 && r < r1;
+          float a[8], w[8];
+          xa[i].get(a);
+          xb[i].get(w);
+          if (turn) {
+            float2 cs[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) cs[j] = sm.cs[r][part + 8 * j];
+            turn_pieces<kInterleaved>(a, w, cs);
+          }
+          const uint4 pa = pack8(a), pb = pack8(w);
+          if (live) {
             if (bounds) {
               ba.take(pa);
               bb.take(pb);
             }
-            __nv_bfloat16* to;
-            if (is_q) {
-              to = static_cast<__nv_bfloat16*>(p.q) + (((int64_t)b * p.n_tok + (s0 + rr - start)) * p.n_q_heads + h) * kHeadDim;
-            } else {
-              if (pg < 0) continue;
-              to = pool + ((((int64_t)pg * n_kv + g) << p.c.page_shift) + ((s0 + rr) & (page - 1))) * kHeadDim;
+            if (to != nullptr) {
+              *reinterpret_cast<uint4*>(to + 4 * i * to_step + ca) = pa;
+              *reinterpret_cast<uint4*>(to + 4 * i * to_step + cb) = pb;
             }
-            *reinterpret_cast<uint4*>(to + ca) = pa;
-            *reinterpret_cast<uint4*>(to + cb) = pb;
           }
         }
         // The page's last new row: its bounds leave.  A page whose first position is not among the new ones takes in the
-        // bounds that it had; one of 128 positions whose first half this CTA has just done, those.
-        if (bounds) {
+        // bounds that it had; one of 128 positions whose first half this warp has just done, those.
+        if (bounds && (c + 1 == c1 || (at + kBatchRows) % most == 0)) {
           __syncwarp();
           ba.over_octets();
           bb.over_octets();
-          if (octet == 0 && pg >= 0) {
-            const int64_t at = ((int64_t)pg * n_kv + g) * kHeadDim;
-            const bool joins = (pos0 & (page - 1)) != 0;
-            uint4* lo4 = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.c.k_min) + at);
-            uint4* hi4 = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.c.k_max) + at);
-            if (joins) {
-              ba.join(__ldcg(lo4 + ca / 8), __ldcg(hi4 + ca / 8));
-              bb.join(__ldcg(lo4 + cb / 8), __ldcg(hi4 + cb / 8));
-            }
-            lo4[ca / 8] = ba.lo4();
-            lo4[cb / 8] = bb.lo4();
-            hi4[ca / 8] = ba.hi4();
-            hi4[cb / 8] = bb.hi4();
-          }
+          const int64_t begin = s0 + max(at / most * most, r0);           // the page's first new row here
+          if (octet == 0 && pg >= 0) store_bounds(p, ba, bb, pg, head.g, ca, cb, (begin & (page - 1)) != 0);
           ba.reset();
           bb.reset();
+        }
+      }
+    }
+  }
+}
+
+template <typename T, bool kInterleaved>
+__global__ void __launch_bounds__(kAppendThreads) paged_append_few_kernel(const PagedAppendParams p) {
+  __shared__ AppendShared sm;
+  const int b = blockIdx.z, tid = threadIdx.x, part = tid & 7;
+  const int page = 1 << p.c.page_shift, unit = page > kUnit ? page : kUnit, most = page < kUnit ? page : kUnit;
+  const bool turns = part < (p.rot >> 4);
+  const int ca = (kInterleaved || !turns) ? 16 * part : 8 * part;          // this thread's pieces of a row
+  const int cb = (kInterleaved || !turns) ? 16 * part + 8 : (p.rot >> 1) + 8 * part;
+  const int heads = p.n_q_heads + 2 * p.c.n_kv_heads, h = (int)blockIdx.y * (kAppendThreads / 8) + (tid >> 3);
+  const T* rows = static_cast<const T*>(p.qkv) + (int64_t)b * p.seq_stride + h * kHeadDim;   // by token
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  Raw8<T> xa, xb;
+  if (h < heads && blockIdx.x == 0) {       // the first token, on its way with the sizes
+    xa.load(rows + ca);
+    xb.load(rows + cb);
+  }
+  const NewRows nr = append_sizes(p, sm, b, tid);
+  const int64_t end = (int64_t)nr.start + nr.count;
+  const int64_t u0 = ((int64_t)nr.start / unit + blockIdx.x) * unit;       // the CTA's positions
+  const int64_t first = u0 > nr.start ? u0 : nr.start, last = u0 + unit < end ? u0 + unit : end;
+  if (nr.count <= 0 || first >= last) return;
+  const Head head(p, h);
+  const bool turn = turns && (head.is_q || head.is_k), bounds = h < heads && head.is_k && p.c.k_min != nullptr;
+  for (int64_t s0 = u0; s0 < last; s0 += kUnit) {       // (once, but for pages of 128)
+    const int64_t lo = s0 > first ? s0 : first, hi = s0 + kUnit < last ? s0 + kUnit : last;
+    if (lo >= hi) continue;
+    if (s0 != u0) __syncthreads();                       // (the sines of the half before are still in use)
+    append_part<true>(p, sm, b, s0, lo, hi, tid);
+    __syncthreads();
+    if (h >= heads) continue;
+    Bounds8 ba, bb;
+    ba.reset();
+    bb.reset();
+    int64_t begin = lo;                                  // the page's first new row
+    for (int64_t pos = lo; pos < hi; ++pos) {
+      const int r = (int)(pos - s0), t = (int)(pos - nr.start), pg = sm.page[r / most];
+      if (t > 0) {
+        xa.load(rows + t * p.tok_stride + ca);
+        xb.load(rows + t * p.tok_stride + cb);
+      }
+      float a[8], w[8];
+      xa.get(a);
+      xb.get(w);
+      if (turn) {
+            float2 cs[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) cs[j] = sm.cs[r][part + 8 * j];
+            turn_pieces<kInterleaved>(a, w, cs);
+          }
+      const uint4 pa = pack8(a), pb = pack8(w);
+      __nv_bfloat16* to = head.row(p, b, t, pos, pg);
+      if (to != nullptr) {
+        *reinterpret_cast<uint4*>(to + ca) = pa;
+        *reinterpret_cast<uint4*>(to + cb) = pb;
+      }
+      if (bounds) {
+        ba.take(pa);
+        bb.take(pb);
+        if (pos + 1 == hi || (r + 1) % most == 0) {      // its last one: the bounds leave (see above)
+          if (pg >= 0) store_bounds(p, ba, bb, pg, head.g, ca, cb, (begin & (page - 1)) != 0);
+          ba.reset();
+          bb.reset();
+          begin = pos + 1;
         }
       }
     }
@@ -500,19 +674,27 @@ cudaError_t launch_paged_append(const PagedAppendParams& p0, bool is_bf16, bool 
                                 cudaStream_t st) {
   PagedAppendParams p = p0;
   const int unit = (1 << p.c.page_shift) > kUnit ? (1 << p.c.page_shift) : kUnit;
-  const int units = (p.n_tok - 1) / unit + 2;        // new rows that begin inside a unit may end inside one more
-  const int heads = p.n_q_heads + 2 * p.c.n_kv_heads, all = (heads + kAppendWarps - 1) / kAppendWarps;
-  // Sines and cosines are worked out once per CTA: as many heads to a CTA as leave four CTAs to an SM.
-  const int64_t ctas = (int64_t)units * n_seq * all;
-  p.rounds = (int)(ctas / (4 * (int64_t)sm_count));
-  if (p.rounds > all) p.rounds = all;
-  if (p.rounds < 1) p.rounds = 1;
-  const dim3 grid(p.n_tok == 1 ? 1 : units, (all + p.rounds - 1) / p.rounds, n_seq), block(kAppendThreads);
-  if (is_bf16)
-    return interleaved ? launch_ex(paged_append_kernel<__nv_bfloat16, true>, grid, block, 0, st, 1, p)
-                       : launch_ex(paged_append_kernel<__nv_bfloat16, false>, grid, block, 0, st, 1, p);
-  return interleaved ? launch_ex(paged_append_kernel<float, true>, grid, block, 0, st, 1, p)
-                     : launch_ex(paged_append_kernel<float, false>, grid, block, 0, st, 1, p);
+  const int units = p.n_tok == 1 ? 1 : (p.n_tok - 1) / unit + 2;   // new rows that begin inside a unit may end inside one more
+  const int heads = p.n_q_heads + 2 * p.c.n_kv_heads;
+  const dim3 block(kAppendThreads);
+  if (p.n_tok <= kFewRows) {
+    const dim3 grid(units, (heads + kAppendThreads / 8 - 1) / (kAppendThreads / 8), n_seq);
+    auto go = [&](auto* kernel) { return launch_ex(kernel, grid, block, 0, st, 1, p); };
+    if (is_bf16) return interleaved ? go(paged_append_few_kernel<__nv_bfloat16, true>) : go(paged_append_few_kernel<__nv_bfloat16, false>);
+    return interleaved ? go(paged_append_few_kernel<float, true>) : go(paged_append_few_kernel<float, false>);
+  }
+  // CTAs of a unit: queries in groups of 32 heads or so, keys and values in groups as large (four rounds of the CTA's
+  // warps) or, where that leaves less than kAppendSpread CTAs to an SM, smaller ones (sines and cosines are worked out once per CTA).
+  const int64_t want = kAppendSpread * (int64_t)sm_count, have = (int64_t)units * n_seq;
+  int per = 32;
+  while (per > 8 && have * ((heads + per - 1) / per) < want) per -= 8;
+  p.rounds = per / kAppendWarps;
+  p.q_groups = (p.n_q_heads + per - 1) / per;
+  p.q_per = (p.n_q_heads + p.q_groups - 1) / p.q_groups;
+  const dim3 grid(units, p.q_groups + (2 * p.c.n_kv_heads + per - 1) / per, n_seq);
+  auto go = [&](auto* kernel) { return launch_ex(kernel, grid, block, 0, st, 1, p); };
+  if (is_bf16) return interleaved ? go(paged_append_kernel<__nv_bfloat16, true>) : go(paged_append_kernel<__nv_bfloat16, false>);
+  return interleaved ? go(paged_append_kernel<float, true>) : go(paged_append_kernel<float, false>);
 }
 
 }  // namespace rkv
