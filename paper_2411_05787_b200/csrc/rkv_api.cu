@@ -915,6 +915,19 @@ rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int6
 //             more than 8 tiles
 //   balanced  longer batches, and what sequences hold behind a shared prefix (whose partials have to be folded in any case):
 //             equal runs of tiles across heads and sequences, then the fold
+struct PagedForm { bool cluster; int gx; };
+static PagedForm paged_form(const rkv_ctx* ctx, int first_slot, int most) {
+  const int64_t bg = (int64_t)ctx->cfg.n_seq * ctx->cfg.n_kv_heads, slots = 2 * ctx->sm_count;
+  const int tiles = (most + rkv::kTile - 1) / rkv::kTile, room = ctx->max_splits - first_slot;
+  int gx = (int)(slots / bg);
+  if (gx > room) gx = room;
+  if (gx > tiles) gx = tiles;
+  if (gx < 1) gx = 1;
+  const int cluster_gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
+  const bool cluster = first_slot == 0 && tiles <= 8 * cluster_gx;
+  return {cluster, cluster ? cluster_gx : gx};
+}
+
 static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, const rkv_paged_cache* cache, int most,
                                       int kind, cudaStream_t st) {
   CUtensorMap tm_k, tm_v;
@@ -925,18 +938,13 @@ static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, con
   s = tensor_map(ctx, cache->v, rows, &tm_v, false, box);
   if (s != RKV_OK) return s;
   const int64_t bg = (int64_t)ctx->cfg.n_seq * ctx->cfg.n_kv_heads, slots = 2 * ctx->sm_count;
-  const int tiles = (most + rkv::kTile - 1) / rkv::kTile, room = ctx->max_splits - p.first_slot;
-  int gx = (int)(slots / bg);
-  if (gx > room) gx = room;
-  if (gx > tiles) gx = tiles;
-  if (gx < 1) gx = 1;
-  const int cluster_gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
-  const bool cluster = p.first_slot == 0 && tiles <= 8 * cluster_gx;
+  const PagedForm form = paged_form(ctx, p.first_slot, most);
+  const bool cluster = form.cluster;
+  const int gx = form.gx;
   // tiles that there can be: behind a shared prefix a sequence may be shorter than that, but not as long in all
   const int64_t units = bg * ((p.max_len + rkv::kTile - 1) / rkv::kTile + 1);
   const bool balanced = !cluster && ctx->cfg.n_seq > 1 && ctx->cfg.n_seq <= rkv::kBalancedMaxSeq &&
                         units * (slots + 1) < (int64_t(1) << 32);   // (the kernel cuts the runs in 32 bits)
-  if (cluster) gx = cluster_gx;
   p.counts = balanced ? ctx->split_counts : nullptr;
   cudaError_t e;
   {
@@ -1068,17 +1076,24 @@ rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_pag
   if (e != cudaSuccess) return cuda_fail(ctx, e, "page score launch");
   ctx->launches += 1;
   rkv::note_launch(st, nullptr, nullptr);
-  {
-    LaunchScope scope(ctx, st, RKV_KERNEL_SELECT);
-    e = rkv::launch_page_select(sp, ctx->cfg.n_seq, most, st);
-  }
-  if (e != cudaSuccess) return cuda_fail(ctx, e, "page selection launch");
-  ctx->launches += 1;
-  rkv::note_launch(st, nullptr, nullptr);
   rkv::PagedAttnParams p = paged_params(ctx, cache, q, active, out, n_max);
   p.page_idx = page_idx;
   p.top = top_pages;
   const int taken = top_pages < most ? top_pages : most;
+  if (paged_form(ctx, 0, taken * cache->page).cluster && most <= rkv::kMaxPickFrom && taken <= rkv::kMaxPicked) {
+    p.scores = sp.scores;
+    p.score_stride = sp.score_stride;
+    p.first = first_pages;
+    p.last = last_pages;
+  } else {
+    {
+      LaunchScope scope(ctx, st, RKV_KERNEL_SELECT);
+      e = rkv::launch_page_select(sp, ctx->cfg.n_seq, most, st);
+    }
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "page selection launch");
+    ctx->launches += 1;
+    rkv::note_launch(st, nullptr, nullptr);
+  }
   return run_paged_attention(ctx, p, cache, taken * cache->page, RKV_KERNEL_ATTN_SMALL, st);
 }
 

@@ -210,11 +210,15 @@ cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pa
 cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
 cudaError_t prepare_page_select();
 
+constexpr int kMaxPickFrom = 8192, kMaxPicked = 512;   // pages that the attention's CTAs pick from, and pick, themselves
 constexpr int kBalancedMaxSeq = 256;   // sequences of a batch that the balanced pass over pages takes
 struct PagedAttnParams {
   PagedDev c;
   const void* q; const int32_t* active; void* out;
-  const int32_t* page_idx;    // [B][Hkv][top]: the pages attended, or null: all positions from `from` on
+  int32_t* page_idx;          // [B][Hkv][top]: the pages attended (with scores: written here), or null: all positions from `from` on
+  const double* scores;       // [B*Hkv][score_stride]: the CTAs pick the pages themselves, or null
+  int64_t score_stride;
+  int32_t first, last;        // pages that are picked in any case
   float* partials; float* ml_t;     // as in AttnParams
   int32_t* counts;            // [B*Hkv]: own partials of each head (balanced form), or null
   int32_t* status;

@@ -2,6 +2,7 @@
 #include <cuda_bf16.h>
 
 #include "rkv_internal.h"
+#include "rkv_pick.cuh"
 #include "rkv_ptx.cuh"
 #include "rkv_rows.cuh"
 
@@ -482,61 +483,14 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
 }
 
 // -------------------------------------------------------------------------------------------------------- selection
-// The m foremost pages of one (sequence, KV head), one CTA: forced pages first, then by score, then the lower page.  The
-// candidates for the last places are narrowed down: the range of their scores is cut into kBins equal parts (the part is a
-// monotone function of the score), those in parts above the one that holds the last place are in, those below are out, and what
-// is left goes round again until it is no more than one thread can be had for each; these are ranked by comparing all with all.
-constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
-constexpr int kBins = 1024, kRanked = 256;
-constexpr int kMostPages = kSelectCluster * kSelectMaxKeysPerCta / 16;   // longest context in pages of 16
-constexpr int kPickWords = (kMostPages + 31) / 32;
-
-__device__ __forceinline__ void block_range(double& lo, double& hi, double (*sm)[2], int tid) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    lo = fmin(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmax(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  if ((tid & 31) == 0) {
-    sm[tid >> 5][0] = lo;
-    sm[tid >> 5][1] = hi;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kPickWarps; ++w) {
-    lo = fmin(lo, sm[w][0]);
-    hi = fmax(hi, sm[w][1]);
-  }
-  __syncthreads();
-}
-
-__device__ __forceinline__ int block_scan(int x, int* sm, int tid, int* total) {   // exclusive
-  int inc = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, inc, o);
-    if ((tid & 31) >= o) inc += y;
-  }
-  if ((tid & 31) == 31) sm[tid >> 5] = inc;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kPickWarps; ++w) {
-    const int y = sm[w];
-    if (w < (tid >> 5)) before += y;
-    all += y;
-  }
-  __syncthreads();
-  *total = all;
-  return before + inc - x;
-}
+// As a launch of its own, one CTA per (sequence, KV head): for batches, and where the scores do not fit beside the attention's
+// buffers (otherwise the CTAs that attend pick for themselves: rkv_paged_attn.cu).
+constexpr int kPickThreads = 512;
 
 __global__ void __launch_bounds__(kPickThreads) page_select_kernel(const PageSelectParams p) {
   extern __shared__ double sm_s[];
-  __shared__ double sm_range[kPickWarps][2], sm_cand[kRanked];
-  __shared__ int sm_at[kRanked], sm_scan[kPickWarps], sm_bins[kBins], sm_pick[3];
-  __shared__ uint32_t sm_in[kPickWords];
-  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+  __shared__ PickShared<kPickThreads> sh;
+  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
   const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
@@ -545,114 +499,10 @@ __global__ void __launch_bounds__(kPickThreads) page_select_kernel(const PageSel
   const int n = min(max(__ldcg(p.c.len + b), 0), lim);
   if (act == 0) return;
   const int pages = (n + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
-  const int m = min(p.top, pages);
   int32_t* out = p.page_idx + ((int64_t)b * gridDim.x + g) * p.top;
-  for (int i = m + tid; i < p.top; i += kPickThreads) out[i] = -1;
-  if (m == pages) {
-    for (int i = tid; i < m; i += kPickThreads) out[i] = i;
-    return;
-  }
-  const int first = min(p.first, pages), last = min(p.last, pages - first);
-  if (first + last >= m) {   // no room beside the forced pages: the lower ones
-    for (int i = tid; i < m; i += kPickThreads) out[i] = i < first ? i : pages - last + (i - first);
-    return;
-  }
-  const int lo_i = first, hi_i = pages - last;   // the pages that compete
-  int want = m - first - last;
-  const double* score = p.scores + ((int64_t)b * gridDim.x + g) * p.score_stride;
-  double c_lo = INFINITY, c_hi = -INFINITY;      // the candidates: those with a score of c_lo .. c_hi
-  for (int i = lo_i + tid; i < hi_i; i += kPickThreads) {
-    const double s = __ldcg(score + i);
-    sm_s[i] = s;
-    c_lo = fmin(c_lo, s);
-    c_hi = fmax(c_hi, s);
-  }
-  block_range(c_lo, c_hi, sm_range, tid);
-  int count = hi_i - lo_i;
-  while (count > kRanked && count != want && c_lo < c_hi) {
-    for (int i = tid; i < kBins; i += kPickThreads) sm_bins[i] = 0;
-    __syncthreads();
-    const double f = kBins / (c_hi - c_lo);
-    auto bin = [&](double s) { return min(kBins - 1, (int)((c_hi - s) * f)); };
-    for (int i = lo_i + tid; i < hi_i; i += kPickThreads) {
-      const double s = sm_s[i];
-      if (s >= c_lo && s <= c_hi) atomicAdd(&sm_bins[bin(s)], 1);
-    }
-    __syncthreads();
-    const int a0 = sm_bins[2 * tid], a1 = sm_bins[2 * tid + 1];
-    int all;
-    const int at = block_scan(a0 + a1, sm_scan, tid, &all);
-    if (at < want && want <= at + a0 + a1) {       // one thread's
-      const bool second = want > at + a0;
-      sm_pick[0] = 2 * tid + second;
-      sm_pick[1] = second ? at + a0 : at;
-      sm_pick[2] = second ? a1 : a0;
-    }
-    __syncthreads();
-    const int pick = sm_pick[0];
-    want -= sm_pick[1];
-    count = sm_pick[2];
-    double n_lo = INFINITY, n_hi = -INFINITY;
-    for (int i = lo_i + tid; i < hi_i; i += kPickThreads) {
-      const double s = sm_s[i];
-      if (s >= c_lo && s <= c_hi && bin(s) == pick) {
-        n_lo = fmin(n_lo, s);
-        n_hi = fmax(n_hi, s);
-      }
-    }
-    block_range(n_lo, n_hi, sm_range, tid);
-    c_lo = n_lo;
-    c_hi = n_hi;
-  }
-  // in: the forced ones and those above the candidates
-  const int words = (pages + 31) >> 5;
-  if (tid == 0) sm_pick[0] = 0;
-  __syncthreads();
-  const bool ties = count > kRanked && count != want;      // more candidates of one score than can be ranked
-  for (int i0 = (tid >> 5) * 32; i0 < words * 32; i0 += kPickThreads) {
-    const int i = i0 + lane;
-    const bool competes = i >= lo_i && i < hi_i;
-    const double s = competes ? sm_s[i] : 0.0;
-    const bool in = i < pages && (!competes || s > c_hi || (count == want && s >= c_lo));
-    const uint32_t mask = __ballot_sync(0xffffffffu, in);
-    if (lane == 0) sm_in[i0 >> 5] = mask;
-    if (competes && count != want && !ties && s >= c_lo && s <= c_hi) {
-      const int k = atomicAdd(&sm_pick[0], 1);             // (any order: they are ranked)
-      sm_cand[k] = s;
-      sm_at[k] = i;
-    }
-  }
-  __syncthreads();
-  if (count != want && !ties) {
-    if (tid < count) {
-      const double s = sm_cand[tid];
-      const int i = sm_at[tid];
-      int rank = 0;
-      for (int k = 0; k < count; ++k) rank += sm_cand[k] > s || (sm_cand[k] == s && sm_at[k] < i);
-      if (rank < want) atomicOr(&sm_in[i >> 5], 1u << (i & 31));
-    }
-    __syncthreads();
-  }
-  if (ties) {   // the first `want` of them
-    int before = 0;
-    for (int i0 = 0; i0 < pages; i0 += kPickThreads) {
-      const int i = i0 + tid;
-      const bool c = i >= lo_i && i < hi_i && sm_s[i] >= c_lo && sm_s[i] <= c_hi;
-      int all;
-      const int at = before + block_scan(c ? 1 : 0, sm_scan, tid, &all);
-      if (c && at < want) atomicOr(&sm_in[i >> 5], 1u << (i & 31));
-      before += all;
-    }
-    __syncthreads();
-  }
-  int before = 0;
-  for (int w0 = 0; w0 < words; w0 += kPickThreads) {
-    uint32_t mask = w0 + tid < words ? sm_in[w0 + tid] : 0u;
-    int all;
-    int at = before + block_scan(__popc(mask), sm_scan, tid, &all);
-    for (; mask != 0u; mask &= mask - 1u) out[at++] = (w0 + tid) * 32 + __ffs(mask) - 1;
-    before += all;
-  }
+  for (int i = min(p.top, pages) + tid; i < p.top; i += kPickThreads) out[i] = -1;
+  pick_pages<kPickThreads>(p.scores + ((int64_t)b * gridDim.x + g) * p.score_stride, pages, p.top, p.first, p.last, sm_s, sh, tid,
+                           [&](int k, int page) { out[k] = page; });
 }
 
 }  // namespace

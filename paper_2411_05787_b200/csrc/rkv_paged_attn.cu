@@ -20,6 +20,7 @@
 #include <cuda_bf16.h>
 
 #include "rkv_internal.h"
+#include "rkv_pick.cuh"
 #include "rkv_ptx.cuh"
 
 namespace rkv {
@@ -36,11 +37,14 @@ constexpr int kPBarsAt = kPStages * kPStageBytes;
 constexpr int kPRowsAt = kPBarsAt + 64;                 // int [stages][4]: rows that count in each 16-row block
 constexpr int kPQAt = kPRowsAt + kPStages * 16 + 16;
 constexpr int kPMaxAt = kPQAt + kMaxGroup * kPQPad * 4;
-constexpr int kPSmem = kPMaxAt + kPWarps * kMaxGroup * 4 + 1024;
+constexpr int kPListAt = (kPMaxAt + kPWarps * kMaxGroup * 4 + 15) & ~15;   // int [kMaxPicked]: pages picked by this CTA
+constexpr int kPSmem = kPListAt + kMaxPicked * 4 + 1024;
 static_assert(kPQAt % 16 == 0, "ldmatrix rows");
 static_assert(2 * (kPSmem + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kPMergeL = kPWarps * kMaxGroup * kPOPad;  // merge buffer, in floats, over the stages
 constexpr int kPMergeM = kPMergeL + kPWarps * kMaxGroup;
+constexpr int kPickSharedAt = kMaxPickFrom * 8;         // behind the scores, in the stages
+static_assert(kPickSharedAt + (int)sizeof(PickShared<kPThreads>) <= kPStages * kPStageBytes, "selection in the stages");
 constexpr int kPSumAt = kPStageBytes;                   // cluster: this CTA's share, [8][128] and [8][2] floats
 constexpr int kPMergeBytes = (kPMergeM + kMaxGroup) * 4;
 static_assert(kPMergeBytes <= kPStageBytes, "merge buffer in one stage");
@@ -251,11 +255,14 @@ __device__ __forceinline__ float2 head_ml(const float* sm, int h) {
 struct Pieces {
   int y, live;                     // first row in the pool, positions that count
   // virtual position v of a (sequence, KV head) that attends s (v >= s.count: nothing there)
-  __device__ __forceinline__ void look_up(const PagedAttnParams& p, const Span& s, int b, int g, int v, bool listed) {
+  __device__ __forceinline__ void look_up(const PagedAttnParams& p, const Span& s, int b, int g, int v, bool listed,
+                                          const int* picked = nullptr) {
     const int shift = p.c.page_shift, n_kv = p.c.n_kv_heads, piece = min(1 << shift, kTile);
     live = 0;
     if (v >= s.count) return;
-    const int i = listed ? __ldcg(p.page_idx + ((int64_t)b * n_kv + g) * p.top + (v >> shift)) : (s.from + v) >> shift;
+    const int i = !listed             ? (s.from + v) >> shift
+                  : picked != nullptr ? picked[v >> shift]
+                                      : __ldcg(p.page_idx + ((int64_t)b * n_kv + g) * p.top + (v >> shift));
     const int off = (listed ? v : s.from + v) & ((1 << shift) - 1);
     if (i < 0) return;
     const int left = s.n - ((i << shift) + off);
@@ -295,7 +302,9 @@ __device__ __forceinline__ uint4 load_query(const PagedAttnParams& p, int b, int
   return qv;
 }
 
-template <bool kCluster, bool kListed>
+// kPick: every CTA picks the pages of its (sequence, KV head) from their scores, all CTAs of a cluster the same ones, before it
+// attends its share of them (a launch of the selection's own takes as long as the attention).
+template <bool kCluster, bool kListed, bool kPick>
 __global__ void __launch_bounds__(kPThreads, 2)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const PagedAttnParams p) {
@@ -331,9 +340,26 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   if (act == 0) return;
   if (sp.cut && tid == 0 && split == 0 && g == 0) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
   if (sp.count <= 0 && (kCluster || sp.n == 0)) {   // nothing cached (the fold knows of it by itself)
+    if (kPick && split == 0)
+      for (int i = tid; i < p.top; i += kPThreads) p.page_idx[((int64_t)b * n_kv + g) * p.top + i] = -1;
     if (kCluster && split == 0 && tid < kHeadDim)
       for (int h = 0; h < G; ++h) static_cast<__nv_bfloat16*>(p.out)[head0 + h * kHeadDim + tid] = __float2bfloat16(0.f);
     return;
+  }
+  int* picked = kPick ? reinterpret_cast<int*>(smem + kPListAt) : nullptr;
+  if constexpr (kPick) {   // in the stages, which are empty yet
+    const int pages = (sp.n + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
+    int32_t* idx = p.page_idx + ((int64_t)b * n_kv + g) * p.top;
+    if (split == 0)
+      for (int i = min(p.top, pages) + tid; i < p.top; i += kPThreads) idx[i] = -1;
+    pick_pages<kPThreads>(p.scores + ((int64_t)b * n_kv + g) * p.score_stride, pages, p.top, p.first, p.last,
+                          reinterpret_cast<double*>(smem), *reinterpret_cast<PickShared<kPThreads>*>(smem + kPickSharedAt), tid,
+                          [&](int k, int page) {
+                            picked[k] = page;
+                            if (split == 0) idx[k] = page;
+                          });
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // tiles will be copied to where the scores were
+    __syncthreads();
   }
   const int total_tiles = (sp.count + kTile - 1) / kTile;
   const int n_tiles = total_tiles > split ? (total_tiles - split + n_cta - 1) / n_cta : 0;
@@ -349,7 +375,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (int t = 0; t < n_tiles; ++t) {
       if (t % per == 0) {
         const int tt = t + lane / pieces;
-        pc.look_up(p, sp, b, g, tt < n_tiles ? (split + tt * n_cta) * kTile + (lane & (pieces - 1)) * piece : sp.count, kListed);
+        pc.look_up(p, sp, b, g, tt < n_tiles ? (split + tt * n_cta) * kTile + (lane & (pieces - 1)) * piece : sp.count, kListed,
+                   picked);
         __syncwarp();
       }
       const int s = t % kPStages, use = t / kPStages;
@@ -688,8 +715,9 @@ __global__ void __launch_bounds__(32 * kPFoldWarps) paged_fold_kernel(const Page
 
 cudaError_t prepare_paged_attention() {
   cudaError_t e = cudaSuccess;
-  for (auto kernel : {paged_attn_kernel<true, false>, paged_attn_kernel<false, false>, paged_attn_kernel<true, true>,
-                      paged_attn_kernel<false, true>})
+  for (auto kernel : {paged_attn_kernel<true, false, false>, paged_attn_kernel<false, false, false>,
+                      paged_attn_kernel<true, true, false>, paged_attn_kernel<false, true, false>,
+                      paged_attn_kernel<true, true, true>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPSmem);
   for (auto kernel : {paged_balanced_kernel<true>, paged_balanced_kernel<false>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBSmem);
@@ -699,8 +727,9 @@ cudaError_t prepare_paged_attention() {
 cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_seq,
                                    int grid_x, bool cluster, cudaStream_t st) {
   const bool listed = p.page_idx != nullptr;
-  auto kernel = cluster ? (listed ? paged_attn_kernel<true, true> : paged_attn_kernel<true, false>)
-                        : (listed ? paged_attn_kernel<false, true> : paged_attn_kernel<false, false>);
+  auto kernel = p.scores != nullptr ? paged_attn_kernel<true, true, true>
+                : cluster           ? (listed ? paged_attn_kernel<true, true, false> : paged_attn_kernel<true, false, false>)
+                                    : (listed ? paged_attn_kernel<false, true, false> : paged_attn_kernel<false, false, false>);
   return launch_ex(kernel, dim3(grid_x, p.c.n_kv_heads, n_seq), dim3(kPThreads), (size_t)kPSmem, st, cluster ? grid_x : 1,
                    tm_k, tm_v, p);
 }
