@@ -1058,8 +1058,8 @@ rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_pag
   sp.c = dev_of(ctx, cache);
   sp.q = q;
   sp.active = active;
-  sp.scores = reinterpret_cast<double*>(ctx->logits);     // (8 bytes a page of 16 positions or more, of 16 or more a position)
-  sp.score_stride = ctx->logit_stride * ctx->gp / 2;
+  sp.keys = reinterpret_cast<uint64_t*>(ctx->logits);       // (8 bytes a page of 16 positions or more, of 16 or more a position)
+  sp.key_stride = ctx->logit_stride * ctx->gp / 2;
   sp.page_idx = page_idx;
   sp.status = ctx->status;
   sp.n_q_heads = ctx->cfg.n_q_heads;
@@ -1081,8 +1081,8 @@ rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_pag
   p.top = top_pages;
   const int taken = top_pages < most ? top_pages : most;
   if (paged_form(ctx, 0, taken * cache->page).cluster && most <= rkv::kMaxPickFrom && taken <= rkv::kMaxPicked) {
-    p.scores = sp.scores;
-    p.score_stride = sp.score_stride;
+    p.keys = sp.keys;
+    p.key_stride = sp.key_stride;
     p.first = first_pages;
     p.last = last_pages;
   } else {

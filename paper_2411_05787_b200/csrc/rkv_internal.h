@@ -200,10 +200,10 @@ cudaError_t launch_paged_append(const PagedAppendParams& p, bool is_bf16, bool i
 struct PageSelectParams {
   PagedDev c;
   const void* q; const int32_t* active;
-  double* scores;             // [B*Hkv][score_stride]
+  uint64_t* keys;             // [B*Hkv][key_stride]: scores as numbers of the same order
   int32_t* page_idx;          // [B][Hkv][top]
   int32_t* status;
-  int64_t score_stride;
+  int64_t key_stride;
   int32_t n_q_heads, group, top, first, last, max_len;
 };
 cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
@@ -215,9 +215,9 @@ constexpr int kBalancedMaxSeq = 256;   // sequences of a batch that the balanced
 struct PagedAttnParams {
   PagedDev c;
   const void* q; const int32_t* active; void* out;
-  int32_t* page_idx;          // [B][Hkv][top]: the pages attended (with scores: written here), or null: all positions from `from` on
-  const double* scores;       // [B*Hkv][score_stride]: the CTAs pick the pages themselves, or null
-  int64_t score_stride;
+  int32_t* page_idx;          // [B][Hkv][top]: the pages attended (with keys: written here), or null: all positions from `from` on
+  const uint64_t* keys;       // [B*Hkv][key_stride]: the CTAs pick the pages themselves, or null
+  int64_t key_stride;
   int32_t first, last;        // pages that are picked in any case
   float* partials; float* ml_t;     // as in AttnParams
   int32_t* counts;            // [B*Hkv]: own partials of each head (balanced form), or null

@@ -474,10 +474,10 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
   const int u = l >> 2;
   if ((l & 3) == 0 && i0 + u < pages) {
     if ((bad >> u) & 1) {   // a page that is not there comes after all others
-      best = -1.7e308;
+      best = -INFINITY;
       if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
     }
-    p.scores[((int64_t)b * n_kv + g) * p.score_stride + i0 + u] = best;
+    p.keys[((int64_t)b * n_kv + g) * p.key_stride + i0 + u] = score_key(best);
   }
   if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
 }
@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
 constexpr int kPickThreads = 512;
 
 __global__ void __launch_bounds__(kPickThreads) page_select_kernel(const PageSelectParams p) {
-  extern __shared__ double sm_s[];
+  extern __shared__ uint64_t sm_k[];
   __shared__ PickShared<kPickThreads> sh;
   const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
@@ -501,8 +501,8 @@ __global__ void __launch_bounds__(kPickThreads) page_select_kernel(const PageSel
   const int pages = (n + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
   int32_t* out = p.page_idx + ((int64_t)b * gridDim.x + g) * p.top;
   for (int i = min(p.top, pages) + tid; i < p.top; i += kPickThreads) out[i] = -1;
-  pick_pages<kPickThreads>(p.scores + ((int64_t)b * gridDim.x + g) * p.score_stride, pages, p.top, p.first, p.last, sm_s, sh, tid,
-                           [&](int k, int page) { out[k] = page; });
+  pick_pages<kPickThreads>(p.keys + ((int64_t)b * gridDim.x + g) * p.key_stride, pages, p.top, p.first, p.last, sm_k, sh, tid,
+                           [&](int k, int page) { out[k] = page; }, [](int) {});
 }
 
 }  // namespace

@@ -34,18 +34,19 @@ constexpr int kPThreads = 32 * (kPWarps + 1);
 constexpr int kPOPad = 132;                             // floats per head row in the merge buffer
 constexpr int kPQPad = 68;                              // words per query row
 constexpr int kPBarsAt = kPStages * kPStageBytes;
+constexpr int kPRecvBar = 2 * kPStages;                 // (index of the barrier that peers' shares are credited to)
 constexpr int kPRowsAt = kPBarsAt + 64;                 // int [stages][4]: rows that count in each 16-row block
 constexpr int kPQAt = kPRowsAt + kPStages * 16 + 16;
 constexpr int kPMaxAt = kPQAt + kMaxGroup * kPQPad * 4;
 constexpr int kPListAt = (kPMaxAt + kPWarps * kMaxGroup * 4 + 15) & ~15;   // int [kMaxPicked]: pages picked by this CTA
-constexpr int kPSmem = kPListAt + kMaxPicked * 4 + 1024;
+constexpr int kPRecvAt = kPListAt + kMaxPicked * 4;     // cluster: float [sources][heads][128 / C], then (m, l) [sources][heads]
+constexpr int kPSmem = kPRecvAt + (kMaxGroup * kHeadDim + kAttnCluster * kMaxGroup * 2) * 4 + 1024;
 static_assert(kPQAt % 16 == 0, "ldmatrix rows");
 static_assert(2 * (kPSmem + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kPMergeL = kPWarps * kMaxGroup * kPOPad;  // merge buffer, in floats, over the stages
 constexpr int kPMergeM = kPMergeL + kPWarps * kMaxGroup;
 constexpr int kPickSharedAt = kMaxPickFrom * 8;         // behind the scores, in the stages
 static_assert(kPickSharedAt + (int)sizeof(PickShared<kPThreads>) <= kPStages * kPStageBytes, "selection in the stages");
-constexpr int kPSumAt = kPStageBytes;                   // cluster: this CTA's share, [8][128] and [8][2] floats
 constexpr int kPMergeBytes = (kPMergeM + kMaxGroup) * 4;
 static_assert(kPMergeBytes <= kPStageBytes, "merge buffer in one stage");
 // the balanced form: its merge buffer beside the stages (the next head's tiles are in them), and the sequences' tables
@@ -59,17 +60,6 @@ constexpr int kBTablesAt = (kBMergeAt + kPMergeBytes + 15) & ~15;
 constexpr int kBSmem = kBTablesAt + kBalancedMaxSeq * 5 * 4 + 16 + 1024;
 static_assert(2 * (kBSmem + 1024) <= 228 * 1024, "two CTAs per SM");
 static_assert((kBalancedMaxSeq & (kBalancedMaxSeq - 1)) == 0, "binary search over the sequences");
-
-__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
-  return v;
-}
 
 // What a (sequence, KV head) attends: virtual positions 0 .. count - 1, either from .. n - 1 or the listed pages' one
 // behind the other.
@@ -228,21 +218,23 @@ struct Consumer {
   }
 };
 
-// Sums over the warps of what merge() left: o into to[head][128], (m, l) of one head.
-__device__ __forceinline__ void publish(const float* sm, int G, int tid, float* to) {
-  for (int item = tid; item < G * 32; item += 32 * kPWarps) {   // (head, four channels)
-    const float* src = sm + (item >> 5) * kPOPad + (item & 31) * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+// Sums over the warps of what merge() left: item = (head, four channels); o into to[head][128]; (m, l) of one head.
+__device__ __forceinline__ float4 warps_sum(const float* sm, int item) {
+  const float* src = sm + (item >> 5) * kPOPad + (item & 31) * 4;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < kPWarps; ++w) {
-      const float4 v = *reinterpret_cast<const float4*>(src + w * kMaxGroup * kPOPad);
-      acc.x += v.x;
-      acc.y += v.y;
-      acc.z += v.z;
-      acc.w += v.w;
-    }
-    *reinterpret_cast<float4*>(to + (item >> 5) * kHeadDim + (item & 31) * 4) = acc;
+  for (int w = 0; w < kPWarps; ++w) {
+    const float4 v = *reinterpret_cast<const float4*>(src + w * kMaxGroup * kPOPad);
+    acc.x += v.x;
+    acc.y += v.y;
+    acc.z += v.z;
+    acc.w += v.w;
   }
+  return acc;
+}
+__device__ __forceinline__ void publish(const float* sm, int G, int tid, float* to) {
+  for (int item = tid; item < G * 32; item += 32 * kPWarps)
+    *reinterpret_cast<float4*>(to + (item >> 5) * kHeadDim + (item & 31) * 4) = warps_sum(sm, item);
 }
 __device__ __forceinline__ float2 head_ml(const float* sm, int h) {
   float2 ml = make_float2(sm[kPMergeM + h], 0.f);
@@ -313,7 +305,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t bar_full = smem_base + kPBarsAt, bar_empty = bar_full + 8 * kPStages;
+  const uint32_t bar_full = smem_base + kPBarsAt, bar_empty = bar_full + 8 * kPStages, bar_recv = bar_full + 8 * kPRecvBar;
   int* sm_rows = reinterpret_cast<int*>(smem + kPRowsAt);
   uint32_t* sm_q = reinterpret_cast<uint32_t*>(smem + kPQAt);
   float* sm_wm = reinterpret_cast<float*>(smem + kPMaxAt);
@@ -322,6 +314,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       mbar_init(bar_full + 8 * s, 1);
       mbar_init(bar_empty + 8 * s, kPWarps);
     }
+    if (kCluster) mbar_init(bar_recv, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid == 32 * kPWarps) {
@@ -332,6 +325,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   const int piece = min(1 << p.c.page_shift, kTile), pieces = kTile / piece;   // positions of a piece, pieces of a tile
   const int64_t head0 = ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim;
   __syncthreads();
+  if (kCluster && n_cta > 1) {
+    // Every CTA sends each of its peers that peer's share of the channels, with stores that credit the receiver's barrier.  It
+    // is armed before the one cluster-wide barrier of the kernel, up here where it costs nothing.
+    if (tid == 0) mbar_expect_tx(bar_recv, (uint32_t)(G * kHeadDim * 4 + n_cta * G * 8));
+    __syncwarp();
+    cluster_sync_alive();
+  }
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
   const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
@@ -352,12 +352,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     int32_t* idx = p.page_idx + ((int64_t)b * n_kv + g) * p.top;
     if (split == 0)
       for (int i = min(p.top, pages) + tid; i < p.top; i += kPThreads) idx[i] = -1;
-    pick_pages<kPThreads>(p.scores + ((int64_t)b * n_kv + g) * p.score_stride, pages, p.top, p.first, p.last,
-                          reinterpret_cast<double*>(smem), *reinterpret_cast<PickShared<kPThreads>*>(smem + kPickSharedAt), tid,
+    pick_pages<kPThreads>(p.keys + ((int64_t)b * n_kv + g) * p.key_stride, pages, p.top, p.first, p.last,
+                          reinterpret_cast<uint64_t*>(smem), *reinterpret_cast<PickShared<kPThreads>*>(smem + kPickSharedAt), tid,
                           [&](int k, int page) {
                             picked[k] = page;
                             if (split == 0) idx[k] = page;
-                          });
+                          },
+                          [](int) {});
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // tiles will be copied to where the scores were
     __syncthreads();
   }
@@ -411,62 +412,62 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
   float* sm = reinterpret_cast<float*>(smem);      // (the stages are free by then)
   mma.merge(sm, sm_wm, warp, lane);
-  const int64_t bg = (int64_t)b * n_kv + g;
-  const int slot = p.first_slot + split;
-  float* sm_sum = reinterpret_cast<float*>(smem + kPSumAt);
-  float* sm_ml = sm_sum + kMaxGroup * kHeadDim;
-  publish(sm, G, tid, kCluster ? sm_sum : p.partials + (bg * p.max_splits + slot) * PartialLayout::kFloats);
-  if (tid < G) {
-    const float2 v = head_ml(sm, tid);
-    if (kCluster) {
-      *reinterpret_cast<float2*>(sm_ml + 2 * tid) = v;
-    } else {
+  if (!kCluster) {
+    const int64_t bg = (int64_t)b * n_kv + g;
+    const int slot = p.first_slot + split;
+    publish(sm, G, tid, p.partials + (bg * p.max_splits + slot) * PartialLayout::kFloats);
+    if (tid < G) {
+      const float2 v = head_ml(sm, tid);
       float* ml = p.ml_t + bg * 16 * p.max_splits + slot;
       ml[(int64_t)tid * p.max_splits] = v.x;
       ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = v.y;
     }
+    return;
   }
-  if (kCluster) {
-    // Every CTA finishes 128 / C channels of every head from its peers' shared memory; the second barrier keeps that
-    // memory until the last reader is done.  (Threads that have left count as arrived.)
-    __syncwarp();
-    cluster_sync_alive();
+  // C = 1, 2, 4 or 8 CTAs; each finishes 128 / C channels of every head
+  const int c_sh = __ffs(n_cta) - 1, own = kHeadDim >> c_sh;
+  float* recv = reinterpret_cast<float*>(smem + kPRecvAt);
+  float* recv_ml = recv + kMaxGroup * kHeadDim;
+  for (int item = tid; item < G * 32; item += 32 * kPWarps) {   // (head, four channels)
+    const float4 acc = warps_sum(sm, item);
+    const int h = item >> 5, ch = (item & 31) * 4, to = ch / own;
+    float* at = recv + (split * G + h) * own + (ch & (own - 1));
+    if (n_cta == 1) *reinterpret_cast<float4*>(at) = acc;
+    else st_async_f32x4(map_rank(smem_u32(at), to), acc, map_rank(bar_recv, to));
+  }
+  for (int i = tid; i < (G << c_sh); i += 32 * kPWarps) {
+    const int h = i >> c_sh, to = i & (n_cta - 1);
+    const float2 v = head_ml(sm, h);
+    float* at = recv_ml + 2 * (split * G + h);
+    if (n_cta == 1) *reinterpret_cast<float2*>(at) = v;
+    else st_async_f32x2(map_rank(smem_u32(at), to), v.x, v.y, map_rank(bar_recv, to));
+  }
+  if (n_cta == 1) {
+    consumer_bar_n<32 * kPWarps>();
+  } else if (!mbar_wait(bar_recv, 0)) {
+    if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+    return;
+  }
+  const int per_sh = 5 - c_sh;                     // log2 of the items per head
+  for (int item = tid; item < (G << per_sh); item += 32 * kPWarps) {
+    const int h = item >> per_sh, ch = (item & ((1 << per_sh) - 1)) * 4;
     const float ninf = -INFINITY;
-    const int c_sh = __ffs(n_cta) - 1, per_sh = 5 - c_sh;      // C = 1, 2, 4 or 8; log2 of the items per head
-    const int ch = (split << (7 - c_sh)) + (tid & ((1 << per_sh) - 1)) * 4;
-    for (int h = tid >> per_sh; h < G; h += (32 * kPWarps) >> per_sh) {
-      const uint32_t at = smem_u32(sm_sum + h * kHeadDim + ch), ml_at = smem_u32(sm_ml + 2 * h);
-      float4 v[kAttnCluster];
-      float2 e[kAttnCluster];
-      float M = ninf, L = 0.f;
-#pragma unroll
-      for (int r = 0; r < kAttnCluster; ++r) {
-        if (r < n_cta) {
-          v[r] = ld_cluster4(map_rank(at, r));
-          e[r] = ld_cluster2(map_rank(ml_at, r));
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < kAttnCluster; ++r)
-        if (r < n_cta) M = fmaxf(M, e[r].x);
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int r = 0; r < kAttnCluster; ++r) {
-        if (r < n_cta) {
-          const float w = (e[r].x == ninf) ? 0.f : ex2(e[r].x - M);
-          L = fmaf(e[r].y, w, L);
-          acc.x = fmaf(v[r].x, w, acc.x);
-          acc.y = fmaf(v[r].y, w, acc.y);
-          acc.z = fmaf(v[r].z, w, acc.z);
-          acc.w = fmaf(v[r].w, w, acc.w);
-        }
-      }
-      const float inv = L == 0.f ? 0.f : 1.f / L;   // (every page of the sequence may be missing)
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + head0 + h * kHeadDim + ch) =
-          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    float M = ninf, L = 0.f;
+    for (int r = 0; r < n_cta; ++r) M = fmaxf(M, recv_ml[2 * (r * G + h)]);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int r = 0; r < n_cta; ++r) {
+      const float2 e = *reinterpret_cast<const float2*>(recv_ml + 2 * (r * G + h));
+      const float4 v = *reinterpret_cast<const float4*>(recv + (r * G + h) * own + ch);
+      const float w = (e.x == ninf) ? 0.f : ex2(e.x - M);
+      L = fmaf(e.y, w, L);
+      acc.x = fmaf(v.x, w, acc.x);
+      acc.y = fmaf(v.y, w, acc.y);
+      acc.z = fmaf(v.z, w, acc.z);
+      acc.w = fmaf(v.w, w, acc.w);
     }
-    __syncwarp();
-    cluster_sync_alive();
+    const float inv = L == 0.f ? 0.f : 1.f / L;    // (every page of the sequence may be missing)
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + head0 + h * kHeadDim + split * own + ch) =
+        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
   }
 }
 
@@ -727,7 +728,7 @@ cudaError_t prepare_paged_attention() {
 cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_seq,
                                    int grid_x, bool cluster, cudaStream_t st) {
   const bool listed = p.page_idx != nullptr;
-  auto kernel = p.scores != nullptr ? paged_attn_kernel<true, true, true>
+  auto kernel = p.keys != nullptr ? paged_attn_kernel<true, true, true>
                 : cluster           ? (listed ? paged_attn_kernel<true, true, false> : paged_attn_kernel<true, false, false>)
                                     : (listed ? paged_attn_kernel<false, true, false> : paged_attn_kernel<false, false, false>);
   return launch_ex(kernel, dim3(grid_x, p.c.n_kv_heads, n_seq), dim3(kPThreads), (size_t)kPSmem, st, cluster ? grid_x : 1,
