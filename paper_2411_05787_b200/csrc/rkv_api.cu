@@ -950,7 +950,7 @@ static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, con
   {
     LaunchScope scope(ctx, st, kind);
     e = balanced ? rkv::launch_paged_balanced(p, tm_k, tm_v, (int)(units < slots ? units : slots), st)
-                 : rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, st);
+                 : rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, cluster && gx * bg <= ctx->sm_count, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "paged attention launch");
   ctx->launches += 1;

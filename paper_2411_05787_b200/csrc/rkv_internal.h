@@ -228,7 +228,7 @@ struct PagedAttnParams {
   float scale;
 };
 cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_seq,
-                                   int grid_x, bool cluster, cudaStream_t st);
+                                   int grid_x, bool cluster, bool wide, cudaStream_t st);
 cudaError_t launch_paged_balanced(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_cta,
                                   cudaStream_t st);
 cudaError_t launch_paged_fold(const PagedAttnParams& p, int n_seq, int grid_x, cudaStream_t st);

@@ -26,37 +26,48 @@
 namespace rkv {
 namespace {
 
-constexpr int kPStages = 3;
 constexpr int kPHalfBytes = kTile * kHeadDim * 2;       // K (or V) of one tile
 constexpr int kPStageBytes = 2 * kPHalfBytes;
-constexpr int kPWarps = 4;                              // MMA warps; warp kPWarps is the copy warp
-constexpr int kPThreads = 32 * (kPWarps + 1);
+constexpr int kPTileWarps = 4;                          // MMA warps that share a tile
 constexpr int kPOPad = 132;                             // floats per head row in the merge buffer
 constexpr int kPQPad = 68;                              // words per query row
-constexpr int kPBarsAt = kPStages * kPStageBytes;
-constexpr int kPRecvBar = 2 * kPStages;                 // (index of the barrier that peers' shares are credited to)
-constexpr int kPRowsAt = kPBarsAt + 64;                 // int [stages][4]: rows that count in each 16-row block
-constexpr int kPQAt = kPRowsAt + kPStages * 16 + 16;
-constexpr int kPMaxAt = kPQAt + kMaxGroup * kPQPad * 4;
-constexpr int kPListAt = (kPMaxAt + kPWarps * kMaxGroup * 4 + 15) & ~15;   // int [kMaxPicked]: pages picked by this CTA
-constexpr int kPRecvAt = kPListAt + kMaxPicked * 4;     // cluster: float [sources][heads][128 / C], then (m, l) [sources][heads]
-constexpr int kPSmem = kPRecvAt + (kMaxGroup * kHeadDim + kAttnCluster * kMaxGroup * 2) * 4 + 1024;
-static_assert(kPQAt % 16 == 0, "ldmatrix rows");
-static_assert(2 * (kPSmem + 1024) <= 228 * 1024, "two CTAs per SM");
-constexpr int kPMergeL = kPWarps * kMaxGroup * kPOPad;  // merge buffer, in floats, over the stages
-constexpr int kPMergeM = kPMergeL + kPWarps * kMaxGroup;
-constexpr int kPickSharedAt = kMaxPickFrom * 8;         // behind the scores, in the stages
-static_assert(kPickSharedAt + (int)sizeof(PickShared<kPThreads>) <= kPStages * kPStageBytes, "selection in the stages");
-constexpr int kPMergeBytes = (kPMergeM + kMaxGroup) * 4;
-static_assert(kPMergeBytes <= kPStageBytes, "merge buffer in one stage");
+
+// Merge buffer of W MMA warps, in floats: o [W][8][kPOPad], l [W][8], m [8].
+template <int W>
+struct Merge {
+  static constexpr int kL = W * kMaxGroup * kPOPad, kM = kL + W * kMaxGroup, kBytes = (kM + kMaxGroup) * 4;
+};
+
+// Buffers of the first kernel.  Its wide form, for few CTAs, has a whole SM: two groups of MMA warps take alternate tiles.
+// (Stages are a multiple of the groups: a stage must always be consumed by the same group, since a warp may only wait for its second
+// phase after it has seen the first.)
+template <bool kWide>
+struct Lay {
+  static constexpr int kStages = kWide ? 6 : 3, kGroups = kWide ? 2 : 1, kWarps = kPTileWarps * kGroups;
+  static constexpr int kThreads = 32 * (kWarps + 1);    // warp kWarps is the copy warp
+  static constexpr int kBarsAt = kStages * kPStageBytes;                     // full, empty [stages], peers' shares
+  static constexpr int kRowsAt = (kBarsAt + 8 * (2 * kStages + 1) + 15) & ~15;   // int [stages][4]: rows that count in each block
+  static constexpr int kQAt = kRowsAt + kStages * 16;
+  static constexpr int kMaxAt = kQAt + kMaxGroup * kPQPad * 4;
+  static constexpr int kListAt = kMaxAt + kWarps * kMaxGroup * 4;            // int [kMaxPicked]: pages picked by this CTA
+  static constexpr int kRecvAt = kListAt + kMaxPicked * 4;   // cluster: float [sources][heads][128 / C], then (m, l) [sources][heads]
+  static constexpr int kSmem = kRecvAt + (kMaxGroup * kHeadDim + kAttnCluster * kMaxGroup * 2) * 4 + 1024;
+  static constexpr int kPickSharedAt = kMaxPickFrom * 8;     // behind the keys, in the stages
+  static_assert(kStages % kGroups == 0 && kListAt % 16 == 0, "stages of one group, aligned buffers");
+  static_assert(kPickSharedAt + (int)sizeof(PickShared<kThreads>) <= kStages * kPStageBytes, "selection in the stages");
+  static_assert(Merge<kWarps>::kBytes <= kStages * kPStageBytes, "merge buffer in the stages");
+};
+static_assert(2 * (Lay<false>::kSmem + 1024) <= 228 * 1024, "two CTAs per SM");
+static_assert(Lay<true>::kSmem <= 227 * 1024, "one CTA per SM");
+
 // the balanced form: its merge buffer beside the stages (the next head's tiles are in them), and the sequences' tables
-constexpr int kBStages = 2;
+constexpr int kBStages = 2, kPWarps = kPTileWarps, kPThreads = 32 * (kPWarps + 1);
 constexpr int kBBarsAt = kBStages * kPStageBytes;
 constexpr int kBRowsAt = kBBarsAt + 64;
 constexpr int kBQAt = kBRowsAt + 64;
 constexpr int kBMaxAt = kBQAt + kMaxGroup * kPQPad * 4;
 constexpr int kBMergeAt = (kBMaxAt + kPWarps * kMaxGroup * 4 + 15) & ~15;
-constexpr int kBTablesAt = (kBMergeAt + kPMergeBytes + 15) & ~15;
+constexpr int kBTablesAt = (kBMergeAt + Merge<kPWarps>::kBytes + 15) & ~15;
 constexpr int kBSmem = kBTablesAt + kBalancedMaxSeq * 5 * 4 + 16 + 1024;
 static_assert(2 * (kBSmem + 1024) <= 228 * 1024, "two CTAs per SM");
 static_assert((kBalancedMaxSeq & (kBalancedMaxSeq - 1)) == 0, "binary search over the sequences");
@@ -84,6 +95,7 @@ __device__ __forceinline__ Span span_of(const PagedAttnParams& p, int b, bool li
 }
 
 // State and steps of an MMA warp.  One (sequence, KV head) at a time: queries(), tile() for each of its tiles, merge().
+template <int W>   // MMA warps of the CTA
 struct Consumer {
   uint32_t qb[8][2];              // B fragments of Q^T: [16-channel segment][k half]
   float m0, m1, l0, l1;           // running maximum (log 2) and sum of heads qc, qc + 1
@@ -99,8 +111,8 @@ struct Consumer {
   // qv: this thread's 16 bytes of the group's query rows (16 threads to a head; zeros for heads beyond the group)
   __device__ __forceinline__ void queries(uint4 qv, uint32_t* sm_q, int tid) {
     const int lane = tid & 31;
-    *reinterpret_cast<uint4*>(sm_q + (tid >> 4) * kPQPad + (tid & 15) * 4) = qv;
-    consumer_bar_n<32 * kPWarps>();
+    if (tid < kMaxGroup * 16) *reinterpret_cast<uint4*>(sm_q + (tid >> 4) * kPQPad + (tid & 15) * 4) = qv;
+    consumer_bar_n<32 * W>();
     const uint32_t q_at = smem_u32(sm_q) + (uint32_t)(lane & 7) * (kPQPad * 4) + (uint32_t)(lane >> 3) * 16u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -179,7 +191,7 @@ struct Consumer {
     }
   }
 
-  // The four warps' accumulators, scaled to the CTA-wide maximum, into sm (kPMergeBytes); sm_wm: [warps][8].
+  // The warps' accumulators, scaled to the CTA-wide maximum, into sm (Merge<W>); sm_wm: [warps][8].
   __device__ __forceinline__ void merge(float* sm, float* sm_wm, int warp, int lane) {
     const float ninf = -INFINITY;
     const int qd = lane >> 2, qc = (lane & 3) * 2;
@@ -189,10 +201,10 @@ struct Consumer {
       l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
     }
     if (lane < 4) *reinterpret_cast<float2*>(sm_wm + warp * kMaxGroup + qc) = make_float2(m0, m1);
-    consumer_bar_n<32 * kPWarps>();   // every warp's maxima are visible, and nobody reads the stages any more
+    consumer_bar_n<32 * W>();   // every warp's maxima are visible, and nobody reads the stages any more
     float M0 = ninf, M1 = ninf;
 #pragma unroll
-    for (int w = 0; w < kPWarps; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float2 mw = *reinterpret_cast<const float2*>(sm_wm + w * kMaxGroup + qc);
       M0 = fmaxf(M0, mw.x);
       M1 = fmaxf(M1, mw.y);
@@ -207,23 +219,24 @@ struct Consumer {
       to[kPOPad + 16 * i + 8] = o[i][3] * e1;
     }
     if (lane < 4) {
-      sm[kPMergeL + warp * kMaxGroup + qc] = l0 * e0;
-      sm[kPMergeL + warp * kMaxGroup + qc + 1] = l1 * e1;
+      sm[Merge<W>::kL + warp * kMaxGroup + qc] = l0 * e0;
+      sm[Merge<W>::kL + warp * kMaxGroup + qc + 1] = l1 * e1;
       if (warp == 0) {
-        sm[kPMergeM + qc] = M0;
-        sm[kPMergeM + qc + 1] = M1;
+        sm[Merge<W>::kM + qc] = M0;
+        sm[Merge<W>::kM + qc + 1] = M1;
       }
     }
-    consumer_bar_n<32 * kPWarps>();
+    consumer_bar_n<32 * W>();
   }
 };
 
 // Sums over the warps of what merge() left: item = (head, four channels); o into to[head][128]; (m, l) of one head.
+template <int W>
 __device__ __forceinline__ float4 warps_sum(const float* sm, int item) {
   const float* src = sm + (item >> 5) * kPOPad + (item & 31) * 4;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int w = 0; w < kPWarps; ++w) {
+  for (int w = 0; w < W; ++w) {
     const float4 v = *reinterpret_cast<const float4*>(src + w * kMaxGroup * kPOPad);
     acc.x += v.x;
     acc.y += v.y;
@@ -232,14 +245,16 @@ __device__ __forceinline__ float4 warps_sum(const float* sm, int item) {
   }
   return acc;
 }
+template <int W>
 __device__ __forceinline__ void publish(const float* sm, int G, int tid, float* to) {
-  for (int item = tid; item < G * 32; item += 32 * kPWarps)
-    *reinterpret_cast<float4*>(to + (item >> 5) * kHeadDim + (item & 31) * 4) = warps_sum(sm, item);
+  for (int item = tid; item < G * 32; item += 32 * W)
+    *reinterpret_cast<float4*>(to + (item >> 5) * kHeadDim + (item & 31) * 4) = warps_sum<W>(sm, item);
 }
+template <int W>
 __device__ __forceinline__ float2 head_ml(const float* sm, int h) {
-  float2 ml = make_float2(sm[kPMergeM + h], 0.f);
+  float2 ml = make_float2(sm[Merge<W>::kM + h], 0.f);
 #pragma unroll
-  for (int w = 0; w < kPWarps; ++w) ml.y += sm[kPMergeL + w * kMaxGroup + h];
+  for (int w = 0; w < W; ++w) ml.y += sm[Merge<W>::kL + w * kMaxGroup + h];
   return ml;
 }
 
@@ -296,28 +311,30 @@ __device__ __forceinline__ uint4 load_query(const PagedAttnParams& p, int b, int
 
 // kPick: every CTA picks the pages of its (sequence, KV head) from their scores, all CTAs of a cluster the same ones, before it
 // attends its share of them (a launch of the selection's own takes as long as the attention).
-template <bool kCluster, bool kListed, bool kPick>
-__global__ void __launch_bounds__(kPThreads, 2)
+template <bool kCluster, bool kListed, bool kPick, bool kWide>
+__global__ void __launch_bounds__(Lay<kWide>::kThreads, kWide ? 1 : 2)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const PagedAttnParams p) {
+  using L = Lay<kWide>;
+  constexpr int kStg = L::kStages, W = L::kWarps, NT = L::kThreads;
   extern __shared__ uint8_t smem_raw[];
   const int b = blockIdx.z, g = blockIdx.y, split = blockIdx.x, n_cta = gridDim.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t bar_full = smem_base + kPBarsAt, bar_empty = bar_full + 8 * kPStages, bar_recv = bar_full + 8 * kPRecvBar;
-  int* sm_rows = reinterpret_cast<int*>(smem + kPRowsAt);
-  uint32_t* sm_q = reinterpret_cast<uint32_t*>(smem + kPQAt);
-  float* sm_wm = reinterpret_cast<float*>(smem + kPMaxAt);
+  const uint32_t bar_full = smem_base + L::kBarsAt, bar_empty = bar_full + 8 * kStg, bar_recv = bar_empty + 8 * kStg;
+  int* sm_rows = reinterpret_cast<int*>(smem + L::kRowsAt);
+  uint32_t* sm_q = reinterpret_cast<uint32_t*>(smem + L::kQAt);
+  float* sm_wm = reinterpret_cast<float*>(smem + L::kMaxAt);
   if (tid == 0) {
-    for (int s = 0; s < kPStages; ++s) {
+    for (int s = 0; s < kStg; ++s) {
       mbar_init(bar_full + 8 * s, 1);
-      mbar_init(bar_empty + 8 * s, kPWarps);
+      mbar_init(bar_empty + 8 * s, kPTileWarps);
     }
     if (kCluster) mbar_init(bar_recv, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (tid == 32 * kPWarps) {
+  if (tid == 32 * W) {
     prefetch_tensormap(&tm_k);
     prefetch_tensormap(&tm_v);
   }
@@ -341,19 +358,19 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   if (sp.cut && tid == 0 && split == 0 && g == 0) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
   if (sp.count <= 0 && (kCluster || sp.n == 0)) {   // nothing cached (the fold knows of it by itself)
     if (kPick && split == 0)
-      for (int i = tid; i < p.top; i += kPThreads) p.page_idx[((int64_t)b * n_kv + g) * p.top + i] = -1;
+      for (int i = tid; i < p.top; i += NT) p.page_idx[((int64_t)b * n_kv + g) * p.top + i] = -1;
     if (kCluster && split == 0 && tid < kHeadDim)
       for (int h = 0; h < G; ++h) static_cast<__nv_bfloat16*>(p.out)[head0 + h * kHeadDim + tid] = __float2bfloat16(0.f);
     return;
   }
-  int* picked = kPick ? reinterpret_cast<int*>(smem + kPListAt) : nullptr;
+  int* picked = kPick ? reinterpret_cast<int*>(smem + L::kListAt) : nullptr;
   if constexpr (kPick) {   // in the stages, which are empty yet
     const int pages = (sp.n + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
     int32_t* idx = p.page_idx + ((int64_t)b * n_kv + g) * p.top;
     if (split == 0)
-      for (int i = min(p.top, pages) + tid; i < p.top; i += kPThreads) idx[i] = -1;
-    pick_pages<kPThreads>(p.keys + ((int64_t)b * n_kv + g) * p.key_stride, pages, p.top, p.first, p.last,
-                          reinterpret_cast<uint64_t*>(smem), *reinterpret_cast<PickShared<kPThreads>*>(smem + kPickSharedAt), tid,
+      for (int i = min(p.top, pages) + tid; i < p.top; i += NT) idx[i] = -1;
+    pick_pages<NT>(p.keys + ((int64_t)b * n_kv + g) * p.key_stride, pages, p.top, p.first, p.last,
+                          reinterpret_cast<uint64_t*>(smem), *reinterpret_cast<PickShared<NT>*>(smem + L::kPickSharedAt), tid,
                           [&](int k, int page) {
                             picked[k] = page;
                             if (split == 0) idx[k] = page;
@@ -366,7 +383,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   const int n_tiles = total_tiles > split ? (total_tiles - split + n_cta - 1) / n_cta : 0;
   if (!kCluster && n_tiles == 0) return;   // (in a cluster an idle CTA still owns channels of the output)
 
-  if (warp == kPWarps) {
+  if (warp == W) {
     // ------------------------------------------------------------ copy warp
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
@@ -380,7 +397,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                    picked);
         __syncwarp();
       }
-      const int s = t % kPStages, use = t / kPStages;
+      const int s = t % kStg, use = t / kStg;
       if (use > 0 && !mbar_wait(bar_empty + 8 * s, (use - 1) & 1)) {
         if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
         break;
@@ -392,20 +409,21 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 
   // ---------------------------------------------------------------- MMA warps
-  Consumer mma;
+  Consumer<W> mma;
   mma.queries(qv, sm_q, tid);
   mma.reset();
   // This warp's 16 rows lie in one piece, the piece's second half of channels `half` bytes further on.
   const uint32_t half = piece * 128;
-  const uint32_t block_at = (16 * warp / piece) * piece * kHeadDim * 2 + (16 * warp % piece) * 128;
+  const int wb = warp % kPTileWarps, grp = warp / kPTileWarps;
+  const uint32_t block_at = (16 * wb / piece) * piece * kHeadDim * 2 + (16 * wb % piece) * 128;
   const float sc = p.scale * kLog2e;               // scores in units of log 2
-  for (int t = 0; t < n_tiles; ++t) {
-    const int s = t % kPStages;
-    if (!mbar_wait(bar_full + 8 * s, (t / kPStages) & 1)) {
+  for (int t = grp; t < n_tiles; t += L::kGroups) {
+    const int s = t % kStg;
+    if (!mbar_wait(bar_full + 8 * s, (t / kStg) & 1)) {
       if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
       break;
     }
-    const int rows = sm_rows[4 * s + warp];        // of this warp's block
+    const int rows = sm_rows[4 * s + wb];          // of this warp's block
     if (rows > 0) mma.tile(smem_base + s * kPStageBytes + block_at, half, rows, sc, lane);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_empty + 8 * s);
@@ -415,9 +433,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   if (!kCluster) {
     const int64_t bg = (int64_t)b * n_kv + g;
     const int slot = p.first_slot + split;
-    publish(sm, G, tid, p.partials + (bg * p.max_splits + slot) * PartialLayout::kFloats);
+    publish<W>(sm, G, tid, p.partials + (bg * p.max_splits + slot) * PartialLayout::kFloats);
     if (tid < G) {
-      const float2 v = head_ml(sm, tid);
+      const float2 v = head_ml<W>(sm, tid);
       float* ml = p.ml_t + bg * 16 * p.max_splits + slot;
       ml[(int64_t)tid * p.max_splits] = v.x;
       ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = v.y;
@@ -426,46 +444,46 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
   // C = 1, 2, 4 or 8 CTAs; each finishes 128 / C channels of every head
   const int c_sh = __ffs(n_cta) - 1, own = kHeadDim >> c_sh;
-  float* recv = reinterpret_cast<float*>(smem + kPRecvAt);
+  float* recv = reinterpret_cast<float*>(smem + L::kRecvAt);
   float* recv_ml = recv + kMaxGroup * kHeadDim;
-  for (int item = tid; item < G * 32; item += 32 * kPWarps) {   // (head, four channels)
-    const float4 acc = warps_sum(sm, item);
+  for (int item = tid; item < G * 32; item += 32 * W) {   // (head, four channels)
+    const float4 acc = warps_sum<W>(sm, item);
     const int h = item >> 5, ch = (item & 31) * 4, to = ch / own;
     float* at = recv + (split * G + h) * own + (ch & (own - 1));
     if (n_cta == 1) *reinterpret_cast<float4*>(at) = acc;
     else st_async_f32x4(map_rank(smem_u32(at), to), acc, map_rank(bar_recv, to));
   }
-  for (int i = tid; i < (G << c_sh); i += 32 * kPWarps) {
+  for (int i = tid; i < (G << c_sh); i += 32 * W) {
     const int h = i >> c_sh, to = i & (n_cta - 1);
-    const float2 v = head_ml(sm, h);
+    const float2 v = head_ml<W>(sm, h);
     float* at = recv_ml + 2 * (split * G + h);
     if (n_cta == 1) *reinterpret_cast<float2*>(at) = v;
     else st_async_f32x2(map_rank(smem_u32(at), to), v.x, v.y, map_rank(bar_recv, to));
   }
   if (n_cta == 1) {
-    consumer_bar_n<32 * kPWarps>();
+    consumer_bar_n<32 * W>();
   } else if (!mbar_wait(bar_recv, 0)) {
     if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
     return;
   }
   const int per_sh = 5 - c_sh;                     // log2 of the items per head
-  for (int item = tid; item < (G << per_sh); item += 32 * kPWarps) {
+  for (int item = tid; item < (G << per_sh); item += 32 * W) {
     const int h = item >> per_sh, ch = (item & ((1 << per_sh) - 1)) * 4;
     const float ninf = -INFINITY;
-    float M = ninf, L = 0.f;
+    float M = ninf, sum = 0.f;
     for (int r = 0; r < n_cta; ++r) M = fmaxf(M, recv_ml[2 * (r * G + h)]);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int r = 0; r < n_cta; ++r) {
       const float2 e = *reinterpret_cast<const float2*>(recv_ml + 2 * (r * G + h));
       const float4 v = *reinterpret_cast<const float4*>(recv + (r * G + h) * own + ch);
       const float w = (e.x == ninf) ? 0.f : ex2(e.x - M);
-      L = fmaf(e.y, w, L);
+      sum = fmaf(e.y, w, sum);
       acc.x = fmaf(v.x, w, acc.x);
       acc.y = fmaf(v.y, w, acc.y);
       acc.z = fmaf(v.z, w, acc.z);
       acc.w = fmaf(v.w, w, acc.w);
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;    // (every page of the sequence may be missing)
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (every page of the sequence may be missing)
     *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + head0 + h * kHeadDim + split * own + ch) =
         make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
   }
@@ -612,7 +630,7 @@ paged_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
   const uint32_t half = piece * 128;
   const uint32_t block_at = (16 * warp / piece) * piece * kHeadDim * 2 + (16 * warp % piece) * 128;
   const float sc = p.scale * kLog2e;
-  Consumer mma;
+  Consumer<kPWarps> mma;
   Run s = run_at(t0, t1, b, sm_pref, sm_tiles);
   if (s.count == 0) return;
   uint4 qv = load_query(p, s.b, s.g, tid);
@@ -641,9 +659,9 @@ paged_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     const uint32_t units = sm_tiles[s.b] + 1, head_at = sm_pref[s.b] + s.g * units;
     const int first = (int)(((head_at + 2) * C - 1) / total);   // the run of the head's first tile
     const int slot = p.first_slot + cta - first;
-    publish(sm_merge, p.group, tid, p.partials + ((int64_t)bg * p.max_splits + slot) * PartialLayout::kFloats);
+    publish<kPWarps>(sm_merge, p.group, tid, p.partials + ((int64_t)bg * p.max_splits + slot) * PartialLayout::kFloats);
     if (tid < p.group) {
-      const float2 v = head_ml(sm_merge, tid);
+      const float2 v = head_ml<kPWarps>(sm_merge, tid);
       float* ml = p.ml_t + (int64_t)bg * 16 * p.max_splits + slot;
       ml[(int64_t)tid * p.max_splits] = v.x;
       ml[(int64_t)(kMaxGroup + tid) * p.max_splits] = v.y;
@@ -716,23 +734,32 @@ __global__ void __launch_bounds__(32 * kPFoldWarps) paged_fold_kernel(const Page
 
 cudaError_t prepare_paged_attention() {
   cudaError_t e = cudaSuccess;
-  for (auto kernel : {paged_attn_kernel<true, false, false>, paged_attn_kernel<false, false, false>,
-                      paged_attn_kernel<true, true, false>, paged_attn_kernel<false, true, false>,
-                      paged_attn_kernel<true, true, true>})
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPSmem);
+  for (auto kernel : {paged_attn_kernel<true, false, false, false>, paged_attn_kernel<false, false, false, false>,
+                      paged_attn_kernel<true, true, false, false>, paged_attn_kernel<false, true, false, false>,
+                      paged_attn_kernel<true, true, true, false>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<false>::kSmem);
+  for (auto kernel : {paged_attn_kernel<true, false, false, true>, paged_attn_kernel<true, true, false, true>,
+                      paged_attn_kernel<true, true, true, true>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<true>::kSmem);
   for (auto kernel : {paged_balanced_kernel<true>, paged_balanced_kernel<false>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBSmem);
   return e;
 }
 
 cudaError_t launch_paged_attention(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_seq,
-                                   int grid_x, bool cluster, cudaStream_t st) {
-  const bool listed = p.page_idx != nullptr;
-  auto kernel = p.keys != nullptr ? paged_attn_kernel<true, true, true>
-                : cluster           ? (listed ? paged_attn_kernel<true, true, false> : paged_attn_kernel<true, false, false>)
-                                    : (listed ? paged_attn_kernel<false, true, false> : paged_attn_kernel<false, false, false>);
-  return launch_ex(kernel, dim3(grid_x, p.c.n_kv_heads, n_seq), dim3(kPThreads), (size_t)kPSmem, st, cluster ? grid_x : 1,
-                   tm_k, tm_v, p);
+                                   int grid_x, bool cluster, bool wide, cudaStream_t st) {
+  const bool listed = p.page_idx != nullptr, pick = p.keys != nullptr;
+  const dim3 grid(grid_x, p.c.n_kv_heads, n_seq);
+  if (wide) {
+    auto kernel = pick     ? paged_attn_kernel<true, true, true, true>
+                  : listed ? paged_attn_kernel<true, true, false, true>
+                           : paged_attn_kernel<true, false, false, true>;
+    return launch_ex(kernel, grid, dim3(Lay<true>::kThreads), (size_t)Lay<true>::kSmem, st, grid_x, tm_k, tm_v, p);
+  }
+  auto kernel = pick      ? paged_attn_kernel<true, true, true, false>
+                : cluster ? (listed ? paged_attn_kernel<true, true, false, false> : paged_attn_kernel<true, false, false, false>)
+                          : (listed ? paged_attn_kernel<false, true, false, false> : paged_attn_kernel<false, false, false, false>);
+  return launch_ex(kernel, grid, dim3(Lay<false>::kThreads), (size_t)Lay<false>::kSmem, st, cluster ? grid_x : 1, tm_k, tm_v, p);
 }
 
 cudaError_t launch_paged_balanced(const PagedAttnParams& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, int n_cta,
