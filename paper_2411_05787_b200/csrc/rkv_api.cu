@@ -1071,7 +1071,7 @@ rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_pag
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_SELECT);
-    e = rkv::launch_page_scores(sp, ctx->cfg.n_seq, most, st);
+    e = rkv::launch_page_scores(sp, ctx->cfg.n_seq, most, ctx->sm_count, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "page score launch");
   ctx->launches += 1;

@@ -383,103 +383,120 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_few_kernel(const 
 // then exact and their sums all but exact, and the selection does not depend on the order of the sum.  A bf16 becomes a
 // double of 2^-896 its value by moving its bits (subnormals and zeros too), without a conversion; the queries carry 2^512.
 //
-// Bound by the bounds' bytes (512 per page and head) or by the 64-bit pipe (64 products a clock and SM), whichever takes
-// longer: seven heads a group 1.5 times the bytes' time.  Sixteen threads share a page, eight channels each, and have four
-// pages in flight; four heads at a time.  The sixteen sums (page, head) of a thread meet in fifteen exchanges that leave
-// each thread one of them.
-constexpr int kScorePages = 32;              // of a CTA: four warps of two halves with four pages each
-constexpr int kScoreCtaThreads = 128;
+// Bound, in the end, by the instructions around the products (a choice and a product each, conversions, exchanges).  Sixteen
+// threads share a page, eight channels each, and have four pages in flight; four heads at a time.  The sixteen sums (page, head)
+// of a thread meet in fifteen exchanges that leave each thread one of them.  A CTA of four warps takes 32 pages at a time and
+// looks the next ones up while it works.
+constexpr int kScoreCtaThreads = 128, kEachPages = 4, kHeadsAtOnce = 4;
+constexpr int kCtaPages = kScoreCtaThreads / 16 * kEachPages;
 
 __device__ __forceinline__ double wide_hi(uint32_t top) {   // bf16 in the upper half of `top`, as a double times 2^-896
   return __hiloint2double((int)((top & 0x80000000u) | ((top & 0x7fff0000u) >> 3)), 0);
 }
 
+template <int kRounds>   // of four heads
 __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const PageSelectParams p) {
+  constexpr int kPages = kEachPages, kCta = kCtaPages, kHeads = kHeadsAtOnce;
   __shared__ double2 sm_q[kMaxGroup][4][16];   // channels 8 l + 2 i, 8 l + 2 i + 1 of head h at [h][i][l]
   const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 31, l = lane & 15;
+  const int n_kv = p.c.n_kv_heads, G = p.group;
+  const int32_t* row = p.c.table + (int64_t)b * p.c.table_stride;
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
-  const int n_kv = p.c.n_kv_heads, G = p.group;
+  // sizes, queries and the first pages' numbers (any of the table's): one round trip
   const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
   const int n = __ldcg(p.c.len + b);
-  const int i0 = blockIdx.x * kScorePages + (tid >> 4) * 4;   // this thread's four pages
-  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
-  const int lim = room < p.max_len ? (int)room : p.max_len;
-  const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
-  if (act == 0 || (int)(blockIdx.x * kScorePages) >= pages) return;
-  if (tid < G * 16) {
-    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
-                                                          ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim) + tid);
+  int i0 = blockIdx.x * kCta + (tid >> 4) * kPages;          // this thread's pages
+  int pg[kPages];
+  auto look_up = [&](int at) {
+#pragma unroll
+    for (int u = 0; u < kPages; ++u) pg[u] = at + u < p.c.table_stride ? __ldg(row + at + u) : -1;
+  };
+  look_up(i0);
+  if (tid < kMaxGroup * 16) {
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < G * 16)
+      w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
+                                                ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim) + tid);
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       sm_q[tid >> 4][i][tid & 15] = make_double2(wide_hi(x[i] << 16) * 0x1p1000 * 0x1p408, wide_hi(x[i]) * 0x1p1000 * 0x1p408);
-  } else if (tid < kMaxGroup * 16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sm_q[tid >> 4][i][tid & 15] = make_double2(0.0, 0.0);
   }
-  uint4 least[4], most[4];
-  int bad = 0;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    least[u] = most[u] = make_uint4(0u, 0u, 0u, 0u);
-    if (i0 + u < pages) {
-      const int pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + i0 + u);
-      if ((unsigned)pg >= (unsigned)p.c.n_pages) {
-        bad |= 1 << u;
-      } else {
-        const int64_t at = ((int64_t)pg * n_kv + g) * (kHeadDim / 8) + l;
-        least[u] = __ldcg(static_cast<const uint4*>(p.c.k_min) + at);
-        most[u] = __ldcg(static_cast<const uint4*>(p.c.k_max) + at);
-      }
-    }
-  }
+  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  const int lim = room < p.max_len ? (int)room : p.max_len;
+  const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
+  if (act == 0) return;
+  if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
   __syncthreads();
-  double best = -INFINITY;
-  for (int h0 = 0; h0 < G; h0 += 4) {
-    double v[16];   // [page][head]
+  for (int s0 = blockIdx.x * kCta; s0 < pages; s0 += gridDim.x * kCta, i0 += gridDim.x * kCta) {
+    uint4 least[kPages], most[kPages];
+    int bad = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      double2 q[4];
-#pragma unroll
-      for (int h = 0; h < 4; ++h) q[h] = sm_q[h0 + h][i][l];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t a = i == 0 ? least[u].x : i == 1 ? least[u].y : i == 2 ? least[u].z : least[u].w;
-        const uint32_t z = i == 0 ? most[u].x : i == 1 ? most[u].y : i == 2 ? most[u].z : most[u].w;
-        const double a0 = wide_hi(a << 16), a1 = wide_hi(a), z0 = wide_hi(z << 16), z1 = wide_hi(z);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          v[4 * u + h] = fma(q[h].x, __double2hiint(q[h].x) < 0 ? a0 : z0, v[4 * u + h]);
-          v[4 * u + h] = fma(q[h].y, __double2hiint(q[h].y) < 0 ? a1 : z1, v[4 * u + h]);
+    for (int u = 0; u < kPages; ++u) {
+      least[u] = most[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (i0 + u < pages) {
+        if ((unsigned)pg[u] >= (unsigned)p.c.n_pages) {
+          bad |= 1 << u;
+        } else {
+          const int64_t at = ((int64_t)pg[u] * n_kv + g) * (kHeadDim / 8) + l;
+          least[u] = __ldcg(static_cast<const uint4*>(p.c.k_min) + at);
+          most[u] = __ldcg(static_cast<const uint4*>(p.c.k_max) + at);
         }
       }
     }
+    look_up(i0 + gridDim.x * kCta);
+    const int u = l / kHeads;                    // this thread's sum: page u, head h0 + l % kHeads
+    uint64_t key = 0ull;
+#pragma unroll 1
+    for (int h0 = 0; h0 < kRounds * kHeads; h0 += kHeads) {
+      double v[16];   // [page][head]
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
-      const bool up = (lane & o) != 0;
+      for (int i = 0; i < 16; ++i) v[i] = 0.0;
 #pragma unroll
-      for (int j = 0; j < o; ++j) {
-        const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
-        v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      for (int i = 0; i < 4; ++i) {
+        double a0[kPages], a1[kPages], z0[kPages], z1[kPages];
+#pragma unroll
+        for (int w = 0; w < kPages; ++w) {
+          const uint32_t a = i == 0 ? least[w].x : i == 1 ? least[w].y : i == 2 ? least[w].z : least[w].w;
+          const uint32_t z = i == 0 ? most[w].x : i == 1 ? most[w].y : i == 2 ? most[w].z : most[w].w;
+          a0[w] = wide_hi(a << 16);
+          a1[w] = wide_hi(a);
+          z0[w] = wide_hi(z << 16);
+          z1[w] = wide_hi(z);
+        }
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) {
+          const double2 q = sm_q[h0 + h][i][l];
+          const bool n0 = __double2hiint(q.x) < 0, n1 = __double2hiint(q.y) < 0;
+#pragma unroll
+          for (int w = 0; w < kPages; ++w) {
+            v[kHeads * w + h] = fma(q.x, n0 ? a0[w] : z0[w], v[kHeads * w + h]);
+            v[kHeads * w + h] = fma(q.y, n1 ? a1[w] : z1[w], v[kHeads * w + h]);
+          }
+        }
       }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) {
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int j = 0; j < o; ++j) {
+          const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
+          v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      if (h0 + l % kHeads < G) key = max(key, score_key(v[0]));
     }
-    double s = h0 + (l & 3) < G ? v[0] : -INFINITY;   // page l >> 2, head h0 + (l & 3)
-    s = fmax(s, __shfl_xor_sync(0xffffffffu, s, 1));
-    s = fmax(s, __shfl_xor_sync(0xffffffffu, s, 2));
-    best = fmax(best, s);
-  }
-  const int u = l >> 2;
-  if ((l & 3) == 0 && i0 + u < pages) {
-    if ((bad >> u) & 1) {   // a page that is not there comes after all others
-      best = -INFINITY;
-      if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+#pragma unroll
+    for (int o = 1; o < kHeads; o <<= 1) key = max(key, (uint64_t)__shfl_xor_sync(0xffffffffu, (unsigned long long)key, o));
+    if (l % kHeads == 0 && i0 + u < pages) {
+      if ((bad >> u) & 1) {   // a page that is not there comes after all others
+        key = 0ull;
+        if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+      }
+      p.keys[((int64_t)b * n_kv + g) * p.key_stride + i0 + u] = key;
     }
-    p.keys[((int64_t)b * n_kv + g) * p.key_stride + i0 + u] = score_key(best);
   }
-  if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
 }
 
 // -------------------------------------------------------------------------------------------------------- selection
@@ -511,9 +528,12 @@ cudaError_t prepare_page_select() {
   return cudaFuncSetAttribute(page_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostPages * 8);
 }
 
-cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
-  return launch_ex(page_score_kernel, dim3((most_pages + kScorePages - 1) / kScorePages, p.c.n_kv_heads, n_seq),
-                   dim3(kScoreCtaThreads), 0, st, 1, p);
+cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, int sm_count, cudaStream_t st) {
+  // One sequence: as many CTAs as fit at once (four to an SM), which then go on.  A batch: one for every 32 pages, since some
+  // sequences have many and others few.
+  const int all = (most_pages + kCtaPages - 1) / kCtaPages, fit = (4 * sm_count + p.c.n_kv_heads - 1) / p.c.n_kv_heads;
+  return launch_ex(p.group > kHeadsAtOnce ? page_score_kernel<2> : page_score_kernel<1>,
+                   dim3(n_seq == 1 && fit < all ? fit : all, p.c.n_kv_heads, n_seq), dim3(kScoreCtaThreads), 0, st, 1, p);
 }
 
 cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
