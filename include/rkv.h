@@ -448,8 +448,8 @@ rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int6
 /*
  * Attention of one query token per sequence over a paged cache: out as in rkv_full_step.  A sequence of length 0 has zeros.
  *   shared    int32 [n_shared] or NULL: the pages that hold the first n_shared * page positions of every sequence (its table
- *             names them too).  They are read once for the whole batch, all of its queries together.  A sequence
- *             that is shorter than that is attended through its own table.
+ *             names them too).  Where they are many (RKV_OPT_SHARED_MIN) they are read once for the whole batch, all of its
+ *             queries together.  A sequence that is shorter than that is attended through its own table.
  *   max_len_hint  host value: upper bound of len[b] (0 = cfg.max_len)
  */
 rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cache* cache /*host struct*/,
@@ -576,6 +576,9 @@ int64_t rkv_launch_count(const rkv_ctx* ctx);
  *                             fewer CTAs that each pay the log-sum-exp and the histogram flush once: slower for a
  *                             single selection, cheaper when many run side by side.  Keys, scores and the selected
  *                             set do not depend on it.
+ *   RKV_OPT_SHARED_MIN        rkv_paged_attention: n_seq * Hkv * shared positions from which on the shared positions are
+ *                             attended by one pass for all sequences, default 524288; below it every sequence attends them
+ *                             through its own table
  */
 #define RKV_OPT_SMALL_MIN_CHUNK 1
 #define RKV_OPT_DEPENDENT_LAUNCH 2
@@ -584,6 +587,7 @@ int64_t rkv_launch_count(const rkv_ctx* ctx);
 #define RKV_OPT_INTERLEAVE_TILES 5
 #define RKV_OPT_SELECT_KEYS_PER_CTA 6
 #define RKV_OPT_SCORE_SLICE 7
+#define RKV_OPT_SHARED_MIN 8
 rkv_status rkv_set_option(rkv_ctx* ctx, int32_t option, int32_t value);
 /* The option's current value (host memory); RKV_ERR_INVALID_ARG for an unknown option or a NULL pointer. */
 rkv_status rkv_get_option(const rkv_ctx* ctx, int32_t option, int32_t* value);

@@ -185,6 +185,16 @@ int choose_chunk(const rkv_ctx* ctx, int n_max, bool full, int* grid_x) {
 // Longest small cache that the clustered partial step takes (8 CTAs x 1024 positions).
 constexpr int kClusterMaxLen = 8192;
 
+// From how many (sequences x KV heads x shared positions) on these are attended by one pass for all.  Every sequence by itself
+// / together, us, with 200 positions of their own behind the prefix (* what is taken):
+//   prefix                      1024           4096          16384
+//    8 x 8 heads of 4     *7.2 / 15.2    *17.2 / 17.1    46.2 / *26.4
+//   32 x 8 heads of 4    *20.4 / 24.2    48.0 / *27.4   155.4 / *35.1
+//   64 x 4 heads of 7    *21.5 / 28.5    48.3 / *31.6   157.8 / *43.0
+//   64 x 1 head  of 8     *7.3 / 23.7   *18.1 / 25.3     45.4 / *29.9
+//    4 x 8 heads of 4     *6.2 / 14.1   *12.3 / 15.7     28.1 / *23.7
+constexpr int kSharedMin = 1 << 19;
+
 struct AppendArgs {
   const void* k_new; const void* v_new; const rkv_cache* full;
   const int32_t* evict_order; int32_t* evict_count; const int32_t* k_small; int max_evict;   // all null / 0: the cache grows
@@ -493,6 +503,7 @@ rkv_status rkv_create(const rkv_config* cfg, rkv_ctx** out) {
   ctx->interleave = 1;
   ctx->select_keys_per_cta = 4096;
   ctx->score_slice = 0;
+  ctx->shared_min = kSharedMin;
   ctx->gp = ctx->group <= 4 ? 4 : 8;
   ctx->workspace = nullptr;
   cudaError_t e = cudaGetDevice(&ctx->device);
@@ -997,8 +1008,10 @@ rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cach
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   rkv::PagedAttnParams p = paged_params(ctx, cache, q, active, out, n_max);
   const int64_t from = (int64_t)n_shared * cache->page;
-  // A batch of one shares with nobody; and there has to be a slot for the shared positions beside the sequences' own.
-  if (from == 0 || from > n_max || ctx->cfg.n_seq == 1 || ctx->max_splits < 2)
+  // A batch of one shares with nobody; there has to be a slot for the shared positions beside the sequences' own; and the pass
+  // over them, a pass over the sequences' own and the fold take about 12 us whatever there is to do.
+  if (from == 0 || from > n_max || ctx->cfg.n_seq == 1 || ctx->max_splits < 2 ||
+      from * ctx->cfg.n_seq * ctx->cfg.n_kv_heads < ctx->shared_min)
     return run_paged_attention(ctx, p, cache, n_max, RKV_KERNEL_ATTN_FULL, st);
   rkv::PrefixAttnParams x;
   memset(&x, 0, sizeof(x));
@@ -1323,6 +1336,10 @@ rkv_status rkv_set_option(rkv_ctx* ctx, int32_t option, int32_t value) {
         return RKV_ERR_INVALID_ARG;
       ctx->score_slice = value;
       return RKV_OK;
+    case RKV_OPT_SHARED_MIN:
+      if (value < 0) return RKV_ERR_INVALID_ARG;
+      ctx->shared_min = value;
+      return RKV_OK;
     default:
       return RKV_ERR_INVALID_ARG;
   }
@@ -1338,6 +1355,7 @@ rkv_status rkv_get_option(const rkv_ctx* ctx, int32_t option, int32_t* value) {
     case RKV_OPT_INTERLEAVE_TILES: *value = ctx->interleave; return RKV_OK;
     case RKV_OPT_SELECT_KEYS_PER_CTA: *value = ctx->select_keys_per_cta; return RKV_OK;
     case RKV_OPT_SCORE_SLICE: *value = ctx->score_slice; return RKV_OK;
+    case RKV_OPT_SHARED_MIN: *value = ctx->shared_min; return RKV_OK;
     default: return RKV_ERR_INVALID_ARG;
   }
 }

@@ -403,6 +403,7 @@ struct rkv_ctx {
   int interleave;      // 1: the full-cache pass deals a head's tiles out to its CTAs in turn
   int select_keys_per_cta;   // keys one CTA of a selection cluster takes (about): fewer = shorter chain, more = fewer CTAs
   int score_slice;           // positions per CTA of the score pass; 0: chosen per launch
+  int shared_min;            // n_seq * Hkv * shared positions from which on these are attended by one pass for all
   // geometry of the last rkv_full_attention, for the rkv_select_topk that completes it
   struct { bool valid; int chunk, gx, n_max; const void* full_k; const int32_t* active; const int32_t* counts; bool quant; } pending_full;
   // ... and of the last rkv_score_keys, for the rkv_select_topk that launches the selection alone

@@ -340,10 +340,12 @@ def test_attention_flags(rkv, sparse):
 
 
 # ------------------------------------------------------------------------------------------------------ shared prefixes
+@pytest.mark.parametrize("together", [True, False])
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 @pytest.mark.parametrize("B,n_q,n_kv,prefix", [(2, 4, 4, 128), (5, 8, 1, 384), (20, 14, 2, 2048), (40, 7, 1, 1024),
-                                               (17, 64, 8, 512), (3, 8, 2, 5120), (70, 8, 2, 768)])
-def test_shared_prefix(rkv, page, B, n_q, n_kv, prefix):
+                                               (17, 64, 8, 512), (3, 8, 2, 5120), (70, 8, 2, 768), (2, 2, 2, 128),
+                                               (130, 8, 1, 256)])
+def test_shared_prefix(rkv, page, B, n_q, n_kv, prefix, together):
     g = np.random.default_rng(B + page)
     lens = [prefix + int(x) for x in g.integers(0, 300, B)]
     lens[0] = prefix                              # nothing of its own
@@ -356,6 +358,8 @@ def test_shared_prefix(rkv, page, B, n_q, n_kv, prefix):
             pg, r = PO.place(pool.table[b].tolist(), page, n)
             pool.k[pg, :, r:], pool.v[pg, :, r:] = math.nan, math.inf
     ctx = rkv.Context(B, n_q, n_kv, 6144, 64)
+    if together:                                  # (by itself the library does so for longer prefixes)
+        ctx.set_option(rkv.OPT_SHARED_MIN, 0)
     q = normal(gen(7), B, n_q, 128).to(torch.bfloat16)
     q[B - 1] *= 12                                # one sequence whose attention is sharp
     active = torch.ones(B, dtype=torch.int32, device="cuda")
@@ -371,12 +375,29 @@ def test_shared_prefix(rkv, page, B, n_q, n_kv, prefix):
             check_out(out[b], *PO.attend(f64(q[b]), *pool.host(b, n)), f"sequence {b} of length {n}")
 
 
+def test_shared_prefix_that_the_library_reads_once(rkv):
+    """Long enough for one pass over it; queries far from the origin, whose maxima grow along the prefix."""
+    page, B, n_q, n_kv, prefix = 64, 10, 28, 4, 16384
+    lens = [prefix + 50 * b for b in range(B)]
+    pool = Pool(rkv, lens, n_kv, page, 8, lens=lens, bounds=False, shared=prefix // page)
+    for i in range(prefix // page):               # keys that get louder
+        pool.k[int(pool.shared[i])] *= 0.2 + 2.0 * i * page / prefix
+    ctx = rkv.Context(B, n_q, n_kv, 17408, 64)
+    q = (normal(gen(7), B, n_q, 128) * 3).to(torch.bfloat16)
+    before, out = ctx.launch_count, torch.empty_like(q)
+    ctx.paged_attention(q, pool.struct(), out, shared=pool.shared)
+    assert ctx.launch_count - before == 3 and ctx.device_status() == 0
+    for b in (0, 1, B - 1):
+        check_out(out[b], *PO.attend(f64(q[b]), *pool.host(b, lens[b])))
+
+
 def test_shared_pages_that_are_not_there(rkv):
     page, B, n_q, n_kv, prefix = 32, 6, 4, 2, 512
     lens = [prefix + 10 * b for b in range(B)]
     pool = Pool(rkv, lens, n_kv, page, 8, lens=lens, bounds=False, shared=prefix // page)
     host = [pool.host(b, n) for b, n in enumerate(lens)]
     ctx = rkv.Context(B, n_q, n_kv, 1024, 64)
+    ctx.set_option(rkv.OPT_SHARED_MIN, 0)
     q = normal(gen(7), B, n_q, 128).to(torch.bfloat16)
     out = torch.empty_like(q)
     shared = pool.shared.clone()
@@ -482,6 +503,7 @@ def test_prompt_tokens_and_both_attentions(rkv):
     pool = Pool(rkv, [600] * B, n_kv, page, 21, lens=[0] * B, shared=prefix // page)
     table, g = rkv.RopeTable(128, 10000.0), gen(5)
     one, ctx = rkv.Context(1, n_q, n_kv, 640, 64), rkv.Context(B, n_q, n_kv, 640, 64)
+    ctx.set_option(rkv.OPT_SHARED_MIN, 0)
     width = (n_q + 2 * n_kv) * 128
     xs = [normal(g, 1, prefix, width).to(torch.bfloat16)]
     head = rkv.paged_cache_struct(pool.k, pool.v, pool.table[:1, : prefix // page].contiguous(), i32([0]), pool.k_min, pool.k_max)
@@ -531,6 +553,8 @@ def test_captured_and_replayed_on_one_workspace(rkv):
     B, n_q, n_kv, page, prefix, top = 3, 8, 2, 16, 128, 6
     side, table = torch.cuda.Stream(), rkv.RopeTable()
     shared, own = (rkv.Context(B, n_q, n_kv, 1024, 64) for _ in range(2))
+    for ctx in (shared, own):
+        ctx.set_option(rkv.OPT_SHARED_MIN, 0)
     width, steps = (n_q + 2 * n_kv) * 128, []
     for seed in (1, 2):
         pools = [Pool(rkv, [700, 300, 900], n_kv, page, seed, lens=[140, 128, 500], shared=prefix // page) for _ in range(2)]
@@ -578,6 +602,7 @@ def test_results_do_not_depend_on_the_run(rkv):
     lens = [prefix + 97 * b for b in range(B)]
     pool = Pool(rkv, lens, n_kv, page, 3, lens=lens, shared=prefix // page)
     ctx = rkv.Context(B, n_q, n_kv, 2048, 64)
+    ctx.set_option(rkv.OPT_SHARED_MIN, 0)
     q = normal(gen(7), B, n_q, 128).to(torch.bfloat16)
     first = None
     for _ in range(5):
@@ -648,6 +673,9 @@ def test_refusals_of_the_library(rkv):
         ctx.paged_sparse_attention(q, pool.struct(), 0, idx[..., :0].contiguous(), out)
     with pytest.raises(rkv.RkvError):
         ctx.paged_attention(q, pool.struct(), out, max_len_hint=300)
+    with pytest.raises(rkv.RkvError):
+        ctx.set_option(rkv.OPT_SHARED_MIN, -1)
+    assert ctx.get_option(rkv.OPT_SHARED_MIN) == 1 << 19
     with pytest.raises(ValueError):              # more shared pages than the table has room for
         ctx.paged_attention(q, pool.struct(), out, shared=torch.zeros(8, dtype=torch.int32, device="cuda"))
     with pytest.raises(ValueError):
