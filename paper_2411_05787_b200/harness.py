@@ -106,15 +106,22 @@ class LlamaShape:
 class LlamaDecoder:
     """Weights, caches and the per-token call sequence.  Batch 1.
 
+    page: None, or the page (16, 32, 64 or 128 positions) of paged caches: tokens then attend the top_pages pages that their
+    keys' bounds select, in every layer, and everything in tokens of kind 'full'; there are no small caches.
     cache_bits: 16 (bf16 full caches) or 8 (rkv_quant_cache: e4m3 with a scale per 64 positions and KV head).
     rope_scaling: None (the loop's own unscaled rotation) or the arguments of rkv.RopeTable beside the shape's theta,
     e.g. dict(scaling="bands", factor=8.0) - prompt and tokens are then rotated by rkv_rope."""
 
     def __init__(self, shape: LlamaShape, prompt_len: int, max_new: int, k_small: int, qc_stride: int,
-                 threshold: float, seed: int = 5, device="cuda", cache_bits: int = 16, rope_scaling: dict | None = None):
+                 threshold: float, seed: int = 5, device="cuda", cache_bits: int = 16, rope_scaling: dict | None = None,
+                 page: int | None = None, top_pages: int = 32):
         if cache_bits not in (8, 16):
             raise ValueError("cache_bits is 8 or 16")
-        self.cache_bits = cache_bits
+        if page is not None and cache_bits != 16:
+            raise ValueError("paged caches hold bfloat16")
+        if page is not None and rope_scaling is None:
+            rope_scaling = dict(scaling="none")         # (the append turns queries and keys)
+        self.cache_bits, self.page = cache_bits, page
         self.table = None if rope_scaling is None else rkv.RopeTable(128, shape.theta, device=device, **rope_scaling)
         self.s, self.dev = shape, torch.device(device)
         self.prompt_len, self.max_new, self.k_small = prompt_len, max_new, k_small
@@ -144,6 +151,10 @@ class LlamaDecoder:
         self.ctx = rkv.Context(1, s.n_q, s.n_kv, cap, self.small_hint)
         self.states = []
         for _ in range(s.n_layers):
+            if page is not None:
+                self.states.append(runner.PagedLayerState(self.ctx, synth.alloc_paged_cache([cap], s.n_kv, page, dev), s.n_q,
+                                                          s.n_kv, top_pages))
+                continue
             if cache_bits == 8:
                 cache, state = synth.alloc_quant_cache([cap], s.n_kv, dev), runner.QuantLayerState
             else:
@@ -183,14 +194,22 @@ class LlamaDecoder:
             h = F.rms_norm(x.float(), (s.hidden,), wl["norm1"].float(), eps=s.eps).to(torch.bfloat16)
             qkv = h @ wl["wqkv"].t()
             v = qkv[:, (s.n_q + s.n_kv) * 128:].view(L, s.n_kv, 128)
-            if self.table is not None:
+            if self.page is not None:
+                q = torch.empty((L, s.n_q, 128), dtype=torch.bfloat16, device=self.dev)
+                cache = self.states[l].full
+                cache.len.zero_()
+                self.states[l].append(qkv[None], self.table, q[None])
+                k = cache.k[cache.table[0].long()].transpose(1, 2).reshape(-1, s.n_kv, 128)[:L]
+            elif self.table is not None:
                 q, k = torch.empty((L, s.n_q, 128), dtype=torch.bfloat16, device=self.dev), torch.empty_like(v)
                 self.ctx.rope(qkv, torch.arange(L, dtype=torch.int32, device=self.dev), self.table, q, k)
             else:
                 q = rot(qkv[:, : s.n_q * 128].float().view(L, s.n_q, 128)).to(torch.bfloat16)
                 k = rot(qkv[:, s.n_q * 128: (s.n_q + s.n_kv) * 128].float().view(L, s.n_kv, 128)).to(torch.bfloat16)
             cache = self.states[l].full
-            if self.cache_bits == 8:
+            if self.page is not None:
+                pass                                     # (the append has filled it)
+            elif self.cache_bits == 8:
                 cache.len.zero_()
                 self.states[l].store_prompt(k[None], v[None])
             else:
@@ -211,12 +230,20 @@ class LlamaDecoder:
         self.token.fill_(int(torch.argmax(hl @ self.lm_head.float().t()).item()))
         # small caches: top-K of the last prompt token's scores (a full step on its query; the output is not used)
         for l, st in enumerate(self.states):
-            st.refresh(q_last[l], max_len_hint=self.full_hint)
+            if self.page is None:
+                st.refresh(q_last[l], max_len_hint=self.full_hint)
         torch.cuda.synchronize()
 
     # ------------------------------------------------------------------ one decode token (measured path)
     def attention(self, l: int, kind: str):
         st, q, k, v = self.states[l], self.q[l], self.k[l], self.v[l]
+        if self.page is not None:
+            (st.attend if kind == "full" else st.attend_selected)(q, max_len_hint=self.full_hint)
+            if self.capture is not None and l in self.capture[0]:
+                torch.cuda.synchronize()
+                self.capture[1].append(dict(layer=l, kind=kind, q=q.clone(), out=st.out.clone(), len=int(st.full.len[0]),
+                                            pages=st.page_idx.clone(), qkv=self.qkv.clone()))
+            return st.out
         if kind == "check":
             st.check_trigger(q, self.threshold)
             st.append_partial(q, k, v, active=st.not_flag, max_len_hint=self.small_hint)
@@ -236,7 +263,8 @@ class LlamaDecoder:
         return st.out
 
     def token_step(self, kind: str, with_harness: bool = True, with_attention: bool = True):
-        """kind: 'small' (partial steps everywhere), 'check' (trigger decides per layer) or 'full'."""
+        """kind: 'small' (partial steps everywhere), 'check' (trigger decides per layer) or 'full'; with paged caches 'small'
+        and 'check' are the same, a step over the selected pages."""
         s = self.s
         if with_harness:
             embed(self.embed_w, self.token, self.x)
@@ -244,7 +272,9 @@ class LlamaDecoder:
             if with_harness:
                 gemv(wl["wqkv"], self.x, self.qkv, norm_w=wl["norm1"], eps=s.eps)        # RMSNorm fused into the read of x
                 pos = self.states[l].full.len
-                if self.table is not None:
+                if self.page is not None:
+                    self.states[l].append(self.qkv.view(1, 1, -1), self.table, self.q[l][None])
+                elif self.table is not None:
                     self.ctx.rope(self.qkv[None], pos, self.table, self.q[l], self.k[l], self.v[l])
                 else:
                     rope_split(self.qkv, pos, s.theta, self.q[l], self.k[l], self.v[l], s.n_q, s.n_kv)

@@ -9,7 +9,7 @@ from __future__ import annotations
 import torch
 
 from . import rkv
-from .synth import HEAD_DIM, LayerCache, alloc_cache
+from .synth import HEAD_DIM, LayerCache, PagedCache, alloc_cache
 
 
 class LayerState:
@@ -182,6 +182,34 @@ class QuantLayerState(LayerState):
     def append(self, k_new, v_new):
         self._store(k_new, v_new)
         self.ctx.append(k_new, v_new, None, self.small_c)
+
+
+class PagedLayerState:
+    """A layer whose cache is paged (synth.PagedCache): there is one cache and no refresh.  A step appends the rows of the fused
+    projection and attends either everything or the pages whose bounds promise the largest scores."""
+
+    def __init__(self, ctx: rkv.Context, cache: PagedCache, n_q_heads: int, n_kv_heads: int, top_pages: int):
+        dev = cache.k.device
+        self.ctx, self.full, self.top_pages = ctx, cache, top_pages
+        self.n_seq, self.n_q, self.n_kv = cache.table.shape[0], n_q_heads, n_kv_heads
+        self.full_c = rkv.paged_cache_struct(cache.k, cache.v, cache.table, cache.len, cache.k_min, cache.k_max)
+        self.out = torch.zeros((self.n_seq, n_q_heads, HEAD_DIM), dtype=torch.bfloat16, device=dev)
+        self.page_idx = torch.full((self.n_seq, n_kv_heads, top_pages), -1, dtype=torch.int32, device=dev)
+
+    def append(self, qkv, table: rkv.RopeTable | None, q, start=None, count=None):
+        """Rows [B, T, (Hq + 2 Hkv) * 128] of the projection: queries to q [B, T, Hq, 128], keys and values to their pages."""
+        self.ctx.paged_append(qkv, self.full_c, table, q, start=start, count=count)
+
+    def attend(self, q, active=None, max_len_hint=0):
+        """Attention over everything; the pages that all sequences begin with are read once."""
+        self.ctx.paged_attention(q, self.full_c, self.out, active=active, shared=self.full.shared, max_len_hint=max_len_hint)
+        return self.out
+
+    def attend_selected(self, q, active=None, first_pages=1, last_pages=1, max_len_hint=0):
+        """Attention over the selected pages (page_idx holds them afterwards)."""
+        self.ctx.paged_sparse_attention(q, self.full_c, self.top_pages, self.page_idx, self.out, active=active,
+                                        first_pages=first_pages, last_pages=last_pages, max_len_hint=max_len_hint)
+        return self.out
 
 
 class OverlappedRefresh:

@@ -196,6 +196,41 @@ def alloc_quant_cache(caps: list, n_kv_heads: int, device) -> QuantLayerCache:
                            torch.zeros((len(caps),), dtype=torch.int32, device=device))
 
 
+@dataclass
+class PagedCache:
+    """One layer's pool of pages, the bounds of their keys, and the sequences' tables and lengths."""
+    k: torch.Tensor           # [n_pages, Hkv, page, 128] bf16
+    v: torch.Tensor
+    k_min: torch.Tensor       # [n_pages, Hkv, 128] bf16
+    k_max: torch.Tensor
+    table: torch.Tensor       # [B, pages of a sequence] int32, -1 where a sequence has none
+    len: torch.Tensor         # [B] int32
+    shared: torch.Tensor | None   # [pages] int32: those that every sequence begins with
+
+    @property
+    def page(self) -> int:
+        return self.k.shape[2]
+
+
+def alloc_paged_cache(rooms: list, n_kv_heads: int, page: int, device, shared: int = 0) -> PagedCache:
+    """Allocate one layer's pool, empty, with pages for rooms[b] positions of every sequence; the first `shared` positions (a
+    multiple of the page) are the same pages in all of them."""
+    if shared % page or any(r < shared for r in rooms):
+        raise ValueError("the shared positions are whole pages and part of every sequence")
+    common = shared // page
+    own = [-(-r // page) - common for r in rooms]
+    table = torch.full((len(rooms), max(common + max(own), 1)), -1, dtype=torch.int32)
+    table[:, :common] = torch.arange(common)
+    at = common
+    for b, n in enumerate(own):
+        table[b, common: common + n] = torch.arange(at, at + n)
+        at += n
+    k, v = (torch.zeros((max(at, 1), n_kv_heads, page, HEAD_DIM), dtype=torch.bfloat16, device=device) for _ in range(2))
+    k_min, k_max = (torch.zeros((max(at, 1), n_kv_heads, HEAD_DIM), dtype=torch.bfloat16, device=device) for _ in range(2))
+    return PagedCache(k, v, k_min, k_max, table.to(device), torch.zeros((len(rooms),), dtype=torch.int32, device=device),
+                      torch.arange(common, dtype=torch.int32, device=device) if common else None)
+
+
 def unit_group_mean(q: torch.Tensor, n_kv_heads: int) -> torch.Tensor:
     """Unit vector of the mean of the G query heads of every KV group: [Hkv, 128] fp32."""
     qf = q.float().reshape(n_kv_heads, -1, HEAD_DIM).mean(dim=1)

@@ -153,3 +153,13 @@ def test_attention_refuses():
         ctx.paged_attention(q, _cache(rkv, n_seq=1), q)
     with pytest.raises(TypeError):
         ctx.paged_sparse_attention(q, rkv.RkvCache(), 3, idx, q)
+
+
+def test_alloc_of_paged_caches():
+    from paper_2411_05787_b200 import synth
+    for rooms, shared in (([100], 8), ([100, 20], 32)):
+        with pytest.raises(ValueError):
+            synth.alloc_paged_cache(rooms, 1, 16, "cpu", shared=shared)
+    c = synth.alloc_paged_cache([100, 40], 2, 16, "cpu", shared=32)
+    assert c.table.tolist() == [[0, 1, 2, 3, 4, 5, 6], [0, 1, 7, -1, -1, -1, -1]] and c.k.shape == (8, 2, 16, 128)
+    assert c.shared.tolist() == [0, 1] and c.page == 16
