@@ -1,5 +1,6 @@
 // The paged cache: rows appended with the rotation on the way, and the scores that select pages.
 #include <cuda_bf16.h>
+#include <limits.h>
 
 #include "rkv_internal.h"
 #include "rkv_pick.cuh"
@@ -55,7 +56,7 @@ __device__ __forceinline__ NewRows append_sizes(const PagedAppendParams& p, Appe
   NewRows n;
   n.start = sm.sizes[1];
   n.count = min(max(sm.sizes[2], 0), p.n_tok);
-  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  const int64_t room = min((int64_t)p.c.table_stride << p.c.page_shift, (int64_t)INT_MAX);   // (lengths are 32 bits)
   const bool sound = n.start >= 0 && n.start <= sm.sizes[0] && n.start <= room;
   int flags = 0;
   if (!sound) {

@@ -301,6 +301,51 @@ def test_attention_of_one_sequence(rkv, n, hint):
     check_out(out[0], *PO.attend(f64(q[0]), *pool.host(0, n)))
 
 
+def test_attention_of_many_sequences(rkv):
+    """More than the balanced form takes."""
+    g = np.random.default_rng(3)
+    lens = [int(x) for x in g.integers(0, 700, 300)]
+    pool = Pool(rkv, [n + 1 for n in lens], 1, 32, 5, lens=lens, bounds=False)
+    ctx = rkv.Context(300, 2, 1, 704, 64)
+    q = normal(gen(7), 300, 2, 128).to(torch.bfloat16)
+    out = torch.empty_like(q)
+    ctx.paged_attention(q, pool.struct(), out)
+    assert ctx.device_status() == 0
+    for b, n in enumerate(lens):
+        check_out(out[b], *PO.attend(f64(q[b]), *pool.host(b, n)), f"length {n}")
+
+
+def test_pool_beyond_32_bits(rkv):
+    """Pages whose bytes lie beyond 2^32: rows are written there, attended and selected from there."""
+    page, n_q, n_kv, n_pages, n = 128, 4, 2, 80000, 700       # 5.2 GB a buffer
+    k, v = (torch.empty((n_pages, n_kv, page, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    lo, hi = (torch.empty((n_pages, n_kv, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = i32([[n_pages - 1, n_pages - 3, 5, n_pages - 2, 0, n_pages - 9]])
+    length = i32([0])
+    c = rkv.paged_cache_struct(k, v, table, length, lo, hi)
+    ctx = rkv.Context(1, n_q, n_kv, 1024, 64)
+    x = normal(gen(1), 1, n, (n_q + 2 * n_kv) * 128).to(torch.bfloat16)
+    q = torch.empty((1, n, n_q, 128), dtype=torch.bfloat16, device="cuda")
+    ctx.paged_append(x, c, None, q)
+    rows = f64(x[0]).reshape(n, n_q + 2 * n_kv, 128)
+    kh, vh = (rows[:, a: a + n_kv].transpose(1, 0, 2) for a in (n_q, n_q + n_kv))
+    last = q[:, -1].contiguous()
+    out, near, idx = torch.empty_like(last), torch.empty_like(last), torch.zeros((1, n_kv, 3), dtype=torch.int32, device="cuda")
+    ctx.paged_attention(last, c, out)
+    ctx.paged_sparse_attention(last, c, 3, idx, near)
+    assert ctx.device_status() == 0
+    qh = f64(last[0])
+    check_out(out[0], *PO.attend(qh, kh, vh))
+    at = []
+    for g in range(n_kv):
+        held = [kh[g, i: i + page] for i in range(0, n, page)]
+        s = PO.scores(qh[2 * g: 2 * g + 2], np.array([p.min(0) for p in held]), np.array([p.max(0) for p in held]))
+        want = PO.select(s, 3, 1, 1)
+        assert idx[0, g].tolist() == want
+        at.append([p for i in want for p in range(i * page, min((i + 1) * page, n))])
+    check_out(near[0], *PO.attend(qh, kh, vh, at=at))
+
+
 @pytest.mark.parametrize("sparse", [False, True])
 def test_attention_flags(rkv, sparse):
     """Pages that are not there are not attended, lengths above the table or the bound are cut; both set their flags."""
