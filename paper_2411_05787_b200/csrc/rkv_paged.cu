@@ -414,20 +414,20 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
     for (int u = 0; u < kPages; ++u) pg[u] = at + u < p.c.table_stride ? __ldg(row + at + u) : -1;
   };
   look_up(i0);
+  uint4 qw = make_uint4(0u, 0u, 0u, 0u);
+  if (tid < G * 16)
+    qw = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
+                                               ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim) + tid);
+  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  const int lim = room < p.max_len ? (int)room : p.max_len;
+  const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
+  if (act == 0 || (int)blockIdx.x * kCta >= pages) return;
   if (tid < kMaxGroup * 16) {
-    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-    if (tid < G * 16)
-      w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
-                                                ((int64_t)b * p.n_q_heads + (int64_t)g * G) * kHeadDim) + tid);
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    const uint32_t x[4] = {qw.x, qw.y, qw.z, qw.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       sm_q[tid >> 4][i][tid & 15] = make_double2(wide_hi(x[i] << 16) * 0x1p1000 * 0x1p408, wide_hi(x[i]) * 0x1p1000 * 0x1p408);
   }
-  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
-  const int lim = room < p.max_len ? (int)room : p.max_len;
-  const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
-  if (act == 0) return;
   if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
   __syncthreads();
   for (int s0 = blockIdx.x * kCta; s0 < pages; s0 += gridDim.x * kCta, i0 += gridDim.x * kCta) {
@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
         }
       }
     }
-    look_up(i0 + gridDim.x * kCta);
+    if (s0 + (int)gridDim.x * kCta < pages) look_up(i0 + gridDim.x * kCta);
     const int u = l / kHeads;                    // this thread's sum: page u, head h0 + l % kHeads
     uint64_t key = 0ull;
 #pragma unroll 1
