@@ -189,30 +189,37 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_base + kXTmemAt) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  tmem_before();
+  __syncthreads();
+  tmem_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kXTmemAt);   // S [2 groups][2] of 64 columns, O [2] of 128
   pdl_wait();
   pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
   const int positions = p.n_shared << shift;
   const int n_all = (positions + kXTile - 1) / kXTile;
   const int n_tiles = (n_all - split + n_cta - 1) / n_cta;   // (at least one: no more CTAs than tiles)
 
-  if (warp < 8) {   // the query rows, swizzled; zeros behind the last one
-    for (int i = tid; i < (kXRows << pair) * 16; i += 256) {
-      const int r = i >> 4, c = i & 15, row = row0 + r;
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (row < rows) {
-        const int b = row / G, h = row - b * G;
-        x = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
-                                                  ((int64_t)b * p.n_q_heads + g * G + h) * kHeadDim) + c);
+  if (warp < 8) {   // the query rows, swizzled; zeros behind the last one.  (The copy warp is at the first tiles meanwhile.)
+    const int c = tid & 15;
+    for (int r0 = tid >> 4; r0 < (kXRows << pair); r0 += kXRows) {
+      uint4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = row0 + r0 + 16 * i, b = min(row, rows - 1) / G, h = min(row, rows - 1) - b * G;
+        x[i] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
+                                                     ((int64_t)b * p.n_q_heads + g * G + h) * kHeadDim) + c);
+        if (row >= rows) x[i] = make_uint4(0u, 0u, 0u, 0u);
       }
-      *reinterpret_cast<uint4*>(smem + kXQAt + (2 * (r >> 7) + (c >> 3)) * kXQPart + (r & 127) * 128 +
-                                (((c & 7) ^ (r & 7)) << 4)) = x;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        *reinterpret_cast<uint4*>(smem + kXQAt + (2 * (r >> 7) + (c >> 3)) * kXQPart + (r & 127) * 128 +
+                                  (((c & 7) ^ (r & 7)) << 4)) = x[i];
+      }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // what tcgen05.mma will read
   }
-  tmem_before();
-  __syncthreads();
-  tmem_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kXTmemAt);   // S [2 groups][2] of 64 columns, O [2] of 128
+  if (warp != 8) asm volatile("bar.sync 2, 320;" ::: "memory");    // the softmax warps and those that issue products
 
   if (warp == 8) {
     // ------------------------------------------------------------ copy warp: lane = (piece, part)
