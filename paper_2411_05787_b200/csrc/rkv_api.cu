@@ -922,12 +922,24 @@ rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int6
 
 // The pass over pages, in one of three forms:
 //   splits    a head's tiles are dealt out in turn to as many CTAs per KV head as fit one wave (two to an SM), a fold finishes
-//   cluster   1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves: while no CTA can get
-//             more than 8 tiles
+//   cluster   1, 2, 4 or 8 CTAs per (sequence, KV head) are a cluster and finish the output themselves
 //   balanced  longer batches, and what sequences hold behind a shared prefix (whose partials have to be folded in any case):
 //             equal runs of tiles across heads and sequences, then the fold
-struct PagedForm { bool cluster; int gx; };
-static PagedForm paged_form(const rkv_ctx* ctx, int first_slot, int most) {
+// A cluster has at most eight CTAs and a wave of them is not always full, so it is for so many tiles a CTA:
+//   one sequence 16; batches whose CTAs fill their waves to four fifths 32, and 64 of listed pages, where sequences differ less in
+//   what they attend; other batches 8.
+// Cluster / otherwise, us (heads x group, positions; ragged: lengths from 0 to that; * what is taken):
+//   1 x 8 x 4   1024  *4.3 / 6.5   4096 *6.4 / 8.6   8192 *8.8 / 9.7   12000 11.3 / *10.6   16384 14.2 / *11.9
+//   4 x 8 x 4   8192 *23.1 / 24.3, ragged *16.5 / 18.6     32768 79.8 / *81.2, ragged 28.2 / *30.4
+//   8 x 8 x 4   4096 *22.8 / 24.5, ragged *15.8 / 17.3     16384 80.2 / *83.4, ragged 44.0 / *37.7
+//  16 x 4 x 7   8192 *42.6 / 46.3, ragged *27.1 / 28.9     32768 156.3 / *160.1, ragged 85.3 / *71.7
+//  64 x 8 x 4   2048 *78.9 / 84.8, ragged *46.6 / 47.2      8192 293.9 / *311.2, ragged 169.4 / *156.3
+//   listed, with its selection: 8 x 8 x 4, 4096 of 32768 *35.7 / 38.9, ragged *27.3 / 34.2
+//                              64 x 8 x 4, 4096 of 8192 *170.6 / 184.4, ragged *136.1 / 137.2
+// Wide CTAs (one to an SM) pay where all clusters are resident at once: eight-CTA clusters find room for 14 on 148 SMs.  Wide /
+// narrow: 14 heads, 4096 positions *6.5 / 7.6; 16 heads 12.2 / *8.3; 2 x 8 heads, 2048 of 32768 listed 19.3 / *14.3.
+struct PagedForm { bool cluster, wide; int gx; };
+static PagedForm paged_form(const rkv_ctx* ctx, int first_slot, int most, bool listed) {
   const int64_t bg = (int64_t)ctx->cfg.n_seq * ctx->cfg.n_kv_heads, slots = 2 * ctx->sm_count;
   const int tiles = (most + rkv::kTile - 1) / rkv::kTile, room = ctx->max_splits - first_slot;
   int gx = (int)(slots / bg);
@@ -935,8 +947,10 @@ static PagedForm paged_form(const rkv_ctx* ctx, int first_slot, int most) {
   if (gx > tiles) gx = tiles;
   if (gx < 1) gx = 1;
   const int cluster_gx = gx >= 8 ? 8 : gx >= 4 ? 4 : gx >= 2 ? 2 : 1;
-  const bool cluster = first_slot == 0 && tiles <= 8 * cluster_gx;
-  return {cluster, cluster ? cluster_gx : gx};
+  const int64_t ctas = cluster_gx * bg, waves = (ctas + slots - 1) / slots;
+  const int limit = 5 * ctas >= 4 * waves * slots ? (listed ? 64 : 32) : ctx->cfg.n_seq == 1 ? 16 : 8;
+  const bool cluster = first_slot == 0 && tiles <= limit * cluster_gx;
+  return {cluster, cluster && 5 * ctas <= 4 * ctx->sm_count, cluster ? cluster_gx : gx};
 }
 
 static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, const rkv_paged_cache* cache, int most,
@@ -949,7 +963,7 @@ static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, con
   s = tensor_map(ctx, cache->v, rows, &tm_v, false, box);
   if (s != RKV_OK) return s;
   const int64_t bg = (int64_t)ctx->cfg.n_seq * ctx->cfg.n_kv_heads, slots = 2 * ctx->sm_count;
-  const PagedForm form = paged_form(ctx, p.first_slot, most);
+  const PagedForm form = paged_form(ctx, p.first_slot, most, p.page_idx != nullptr);
   const bool cluster = form.cluster;
   const int gx = form.gx;
   // tiles that there can be: behind a shared prefix a sequence may be shorter than that, but not as long in all
@@ -961,7 +975,7 @@ static rkv_status run_paged_attention(rkv_ctx* ctx, rkv::PagedAttnParams& p, con
   {
     LaunchScope scope(ctx, st, kind);
     e = balanced ? rkv::launch_paged_balanced(p, tm_k, tm_v, (int)(units < slots ? units : slots), st)
-                 : rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, cluster && gx * bg <= ctx->sm_count, st);
+                 : rkv::launch_paged_attention(p, tm_k, tm_v, ctx->cfg.n_seq, gx, cluster, form.wide, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "paged attention launch");
   ctx->launches += 1;
@@ -1084,7 +1098,7 @@ rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_pag
   cudaError_t e;
   {
     LaunchScope scope(ctx, st, RKV_KERNEL_SELECT);
-    e = rkv::launch_page_scores(sp, ctx->cfg.n_seq, most, ctx->sm_count, st);
+    e = rkv::launch_page_scores(sp, ctx->cfg.n_seq, most, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "page score launch");
   ctx->launches += 1;
@@ -1093,7 +1107,7 @@ rkv_status rkv_paged_sparse_attention(rkv_ctx* ctx, const void* q, const rkv_pag
   p.page_idx = page_idx;
   p.top = top_pages;
   const int taken = top_pages < most ? top_pages : most;
-  if (paged_form(ctx, 0, taken * cache->page).cluster && most <= rkv::kMaxPickFrom && taken <= rkv::kMaxPicked) {
+  if (paged_form(ctx, 0, taken * cache->page, true).cluster && most <= rkv::kMaxPickFrom && taken <= rkv::kMaxPicked) {
     p.keys = sp.keys;
     p.key_stride = sp.key_stride;
     p.first = first_pages;

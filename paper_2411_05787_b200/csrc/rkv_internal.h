@@ -206,7 +206,7 @@ struct PageSelectParams {
   int64_t key_stride;
   int32_t n_q_heads, group, top, first, last, max_len;
 };
-cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, int sm_count, cudaStream_t st);
+cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
 cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st);
 cudaError_t prepare_page_select();
 

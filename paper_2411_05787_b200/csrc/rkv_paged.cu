@@ -407,13 +407,10 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
   // sizes, queries and the first pages' numbers (any of the table's): one round trip
   const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
   const int n = __ldcg(p.c.len + b);
-  int i0 = blockIdx.x * kCta + (tid >> 4) * kPages;          // this thread's pages
+  const int i0 = blockIdx.x * kCta + (tid >> 4) * kPages;    // this thread's pages
   int pg[kPages];
-  auto look_up = [&](int at) {
 #pragma unroll
-    for (int u = 0; u < kPages; ++u) pg[u] = at + u < p.c.table_stride ? __ldg(row + at + u) : -1;
-  };
-  look_up(i0);
+  for (int u = 0; u < kPages; ++u) pg[u] = i0 + u < p.c.table_stride ? __ldg(row + i0 + u) : -1;
   uint4 qw = make_uint4(0u, 0u, 0u, 0u);
   if (tid < G * 16)
     qw = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
@@ -430,73 +427,70 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
   }
   if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
   __syncthreads();
-  for (int s0 = blockIdx.x * kCta; s0 < pages; s0 += gridDim.x * kCta, i0 += gridDim.x * kCta) {
-    uint4 least[kPages], most[kPages];
-    int bad = 0;
+  uint4 least[kPages], most[kPages];
+  int bad = 0;
 #pragma unroll
-    for (int u = 0; u < kPages; ++u) {
-      least[u] = most[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (i0 + u < pages) {
-        if ((unsigned)pg[u] >= (unsigned)p.c.n_pages) {
-          bad |= 1 << u;
-        } else {
-          const int64_t at = ((int64_t)pg[u] * n_kv + g) * (kHeadDim / 8) + l;
-          least[u] = __ldcg(static_cast<const uint4*>(p.c.k_min) + at);
-          most[u] = __ldcg(static_cast<const uint4*>(p.c.k_max) + at);
-        }
+  for (int u = 0; u < kPages; ++u) {
+    least[u] = most[u] = make_uint4(0u, 0u, 0u, 0u);
+    if (i0 + u < pages) {
+      if ((unsigned)pg[u] >= (unsigned)p.c.n_pages) {
+        bad |= 1 << u;
+      } else {
+        const int64_t at = ((int64_t)pg[u] * n_kv + g) * (kHeadDim / 8) + l;
+        least[u] = __ldcg(static_cast<const uint4*>(p.c.k_min) + at);
+        most[u] = __ldcg(static_cast<const uint4*>(p.c.k_max) + at);
       }
     }
-    if (s0 + (int)gridDim.x * kCta < pages) look_up(i0 + gridDim.x * kCta);
-    const int u = l / kHeads;                    // this thread's sum: page u, head h0 + l % kHeads
-    uint64_t key = 0ull;
+  }
+  const int u = l / kHeads;                    // this thread's sum: page u, head h0 + l % kHeads
+  uint64_t key = 0ull;
 #pragma unroll 1
-    for (int h0 = 0; h0 < kRounds * kHeads; h0 += kHeads) {
-      double v[16];   // [page][head]
+  for (int h0 = 0; h0 < kRounds * kHeads; h0 += kHeads) {
+    double v[16];   // [page][head]
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = 0.0;
+    for (int i = 0; i < 16; ++i) v[i] = 0.0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        double a0[kPages], a1[kPages], z0[kPages], z1[kPages];
+    for (int i = 0; i < 4; ++i) {
+      double a0[kPages], a1[kPages], z0[kPages], z1[kPages];
+#pragma unroll
+      for (int w = 0; w < kPages; ++w) {
+        const uint32_t a = i == 0 ? least[w].x : i == 1 ? least[w].y : i == 2 ? least[w].z : least[w].w;
+        const uint32_t z = i == 0 ? most[w].x : i == 1 ? most[w].y : i == 2 ? most[w].z : most[w].w;
+        a0[w] = wide_hi(a << 16);
+        a1[w] = wide_hi(a);
+        z0[w] = wide_hi(z << 16);
+        z1[w] = wide_hi(z);
+      }
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        const double2 q = sm_q[h0 + h][i][l];
+        const bool n0 = __double2hiint(q.x) < 0, n1 = __double2hiint(q.y) < 0;
 #pragma unroll
         for (int w = 0; w < kPages; ++w) {
-          const uint32_t a = i == 0 ? least[w].x : i == 1 ? least[w].y : i == 2 ? least[w].z : least[w].w;
-          const uint32_t z = i == 0 ? most[w].x : i == 1 ? most[w].y : i == 2 ? most[w].z : most[w].w;
-          a0[w] = wide_hi(a << 16);
-          a1[w] = wide_hi(a);
-          z0[w] = wide_hi(z << 16);
-          z1[w] = wide_hi(z);
-        }
-#pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-          const double2 q = sm_q[h0 + h][i][l];
-          const bool n0 = __double2hiint(q.x) < 0, n1 = __double2hiint(q.y) < 0;
-#pragma unroll
-          for (int w = 0; w < kPages; ++w) {
-            v[kHeads * w + h] = fma(q.x, n0 ? a0[w] : z0[w], v[kHeads * w + h]);
-            v[kHeads * w + h] = fma(q.y, n1 ? a1[w] : z1[w], v[kHeads * w + h]);
-          }
+          v[kHeads * w + h] = fma(q.x, n0 ? a0[w] : z0[w], v[kHeads * w + h]);
+          v[kHeads * w + h] = fma(q.y, n1 ? a1[w] : z1[w], v[kHeads * w + h]);
         }
       }
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) {
-        const bool up = (lane & o) != 0;
-#pragma unroll
-        for (int j = 0; j < o; ++j) {
-          const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
-          v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-        }
-      }
-      if (h0 + l % kHeads < G) key = max(key, score_key(v[0]));
     }
 #pragma unroll
-    for (int o = 1; o < kHeads; o <<= 1) key = max(key, (uint64_t)__shfl_xor_sync(0xffffffffu, (unsigned long long)key, o));
-    if (l % kHeads == 0 && i0 + u < pages) {
-      if ((bad >> u) & 1) {   // a page that is not there comes after all others
-        key = 0ull;
-        if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+    for (int o = 8; o > 0; o >>= 1) {
+      const bool up = (lane & o) != 0;
+#pragma unroll
+      for (int j = 0; j < o; ++j) {
+        const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
+        v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
       }
-      p.keys[((int64_t)b * n_kv + g) * p.key_stride + i0 + u] = key;
     }
+    if (h0 + l % kHeads < G) key = max(key, score_key(v[0]));
+  }
+#pragma unroll
+  for (int o = 1; o < kHeads; o <<= 1) key = max(key, (uint64_t)__shfl_xor_sync(0xffffffffu, (unsigned long long)key, o));
+  if (l % kHeads == 0 && i0 + u < pages) {
+    if ((bad >> u) & 1) {   // a page that is not there comes after all others
+      key = 0ull;
+      if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+    }
+    p.keys[((int64_t)b * n_kv + g) * p.key_stride + i0 + u] = key;
   }
 }
 
@@ -529,12 +523,9 @@ cudaError_t prepare_page_select() {
   return cudaFuncSetAttribute(page_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostPages * 8);
 }
 
-cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, int sm_count, cudaStream_t st) {
-  // One sequence: as many CTAs as fit at once (four to an SM), which then go on.  A batch: one for every 32 pages, since some
-  // sequences have many and others few.
-  const int all = (most_pages + kCtaPages - 1) / kCtaPages, fit = (4 * sm_count + p.c.n_kv_heads - 1) / p.c.n_kv_heads;
+cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
   return launch_ex(p.group > kHeadsAtOnce ? page_score_kernel<2> : page_score_kernel<1>,
-                   dim3(n_seq == 1 && fit < all ? fit : all, p.c.n_kv_heads, n_seq), dim3(kScoreCtaThreads), 0, st, 1, p);
+                   dim3((most_pages + kCtaPages - 1) / kCtaPages, p.c.n_kv_heads, n_seq), dim3(kScoreCtaThreads), 0, st, 1, p);
 }
 
 cudaError_t launch_page_select(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
