@@ -188,11 +188,11 @@ constexpr int kClusterMaxLen = 8192;
 // From how many (sequences x KV heads x shared positions) on these are attended by one pass for all.  Every sequence by itself
 // / together, us, with 200 positions of their own behind the prefix (* what is taken):
 //   prefix                      1024           4096          16384
-//    8 x 8 heads of 4     *7.2 / 15.2    *17.2 / 17.1    46.2 / *26.4
-//   32 x 8 heads of 4    *20.4 / 24.2    48.0 / *27.4   155.4 / *35.1
-//   64 x 4 heads of 7    *21.5 / 28.5    48.3 / *31.6   157.8 / *43.0
-//   64 x 1 head  of 8     *7.3 / 23.7   *18.1 / 25.3     45.4 / *29.9
-//    4 x 8 heads of 4     *6.2 / 14.1   *12.3 / 15.7     28.1 / *23.7
+//    8 x 8 heads of 4     *7.2 / 14.8    *14.2 / 16.7   46.2 / *25.5
+//   32 x 8 heads of 4    *17.0 / 22.0    48.1 / *25.5  156.3 / *32.9
+//   64 x 4 heads of 7    *17.5 / 24.6    48.0 / *28.0  157.1 / *39.2
+//   64 x 1 head  of 8     *7.3 / 20.0   *14.3 / 21.7    45.4 / *26.0
+//    4 x 8 heads of 4     *6.5 / 13.8    *10.2 / 15.7    28.4 / *23.1
 constexpr int kSharedMin = 1 << 19;
 
 struct AppendArgs {
@@ -928,7 +928,8 @@ rkv_status rkv_paged_append(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int6
 // A cluster has at most eight CTAs and a wave of them is not always full, so it is for so many tiles a CTA:
 //   one sequence 16; batches whose CTAs fill their waves to four fifths 32, and 64 of listed pages, where sequences differ less in
 //   what they attend; other batches 8.
-// Cluster / otherwise, us (heads x group, positions; ragged: lengths from 0 to that; * what is taken):
+// Cluster / otherwise, us (sequences x heads x group, positions; ragged: lengths from 0 to that; one cache again and again; * what
+// is taken):
 //   1 x 8 x 4   1024  *4.3 / 6.5   4096 *6.4 / 8.6   8192 *8.8 / 9.7   12000 11.3 / *10.6   16384 14.2 / *11.9
 //   4 x 8 x 4   8192 *23.1 / 24.3, ragged *16.5 / 18.6     32768 79.8 / *81.2, ragged 28.2 / *30.4
 //   8 x 8 x 4   4096 *22.8 / 24.5, ragged *15.8 / 17.3     16384 80.2 / *83.4, ragged 44.0 / *37.7
@@ -1023,7 +1024,7 @@ rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cach
   rkv::PagedAttnParams p = paged_params(ctx, cache, q, active, out, n_max);
   const int64_t from = (int64_t)n_shared * cache->page;
   // A batch of one shares with nobody; there has to be a slot for the shared positions beside the sequences' own; and the pass
-  // over them, a pass over the sequences' own and the fold take about 12 us whatever there is to do.
+  // over them, a pass over the sequences' own and the fold take about 11 us whatever there is to do.
   if (from == 0 || from > n_max || ctx->cfg.n_seq == 1 || ctx->max_splits < 2 ||
       from * ctx->cfg.n_seq * ctx->cfg.n_kv_heads < ctx->shared_min)
     return run_paged_attention(ctx, p, cache, n_max, RKV_KERNEL_ATTN_FULL, st);

@@ -21,6 +21,10 @@ namespace {
 // of 16 rows, four of a thread's, all of them requested before the first is used.  Sines and cosines of the unit's (row, pair)s
 // are worked out once per CTA, in shared memory, while the first batch is on its way.
 // With up to kFewRows rows a sequence (tokens of a decode step) eight threads take a head, and a CTA 32 of them.
+// Measured (32 + 16 heads): a prompt of 32768 bf16 rows 139 us, 5.8 TB/s (rows requested one by one as others are done with 215, two
+// batches in turn 153, three or four CTAs to an SM, which spill, 158 to 231, 512 threads 144); one row 3.4 us.
+// Few rows here / in units: 1 row 3.1 / 4.3 us, 64 sequences of 1 row 3.4 / 8.8, of 4 rows 5.4 / 9.9, of 8 rows 8.2 / 10.4, but
+// 1 sequence of 8 rows 6.7 / 4.6, of 16 rows 11.0 / 5.0, 64 of 16 rows 14.1 / 11.2.
 constexpr int kAppendThreads = 256, kAppendWarps = kAppendThreads / 32;
 constexpr int kUnit = 64;                    // positions of a CTA
 constexpr int kBatchRows = 16, kAhead = kBatchRows / 4;      // rows of a warp in flight, and of a thread
@@ -384,21 +388,21 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_few_kernel(const 
 // then exact and their sums all but exact, and the selection does not depend on the order of the sum.  A bf16 becomes a
 // double of 2^-896 its value by moving its bits (subnormals and zeros too), without a conversion; the queries carry 2^512.
 //
-// Bound, in the end, by the instructions around the products (a choice and a product each, conversions, exchanges).  Sixteen
-// threads share a page, eight channels each, and have four pages in flight; four heads at a time.  The sixteen sums (page, head)
-// of a thread meet in fifteen exchanges that leave each thread one of them.  A CTA of four warps takes 32 pages at a time and
-// looks the next ones up while it works.
-constexpr int kScoreCtaThreads = 128, kEachPages = 4, kHeadsAtOnce = 4;
+// Bound by the bounds' bytes and, in the end, by the instructions around the products (a choice and a product each, conversions,
+// exchanges).  Up to four heads: sixteen threads share a page, eight channels each, and have four pages in flight.  The sixteen sums
+// (page, head) of a thread meet in fifteen exchanges that leave each thread one of them.  More heads: the MMAs below, which need no
+// exchanges but twice the products, all eight columns of them.  A CTA of four warps takes 32 pages.  Measured: 2048 pages of
+// 8 x 4 heads 6.5 us (MMAs 8.1), sixteen ragged sequences of up to 2048 pages of 4 x 7 heads 22.4 (as two rounds of four heads 28.5).
+constexpr int kScoreCtaThreads = 128, kEachPages = 4, kScalarHeads = 4;
 constexpr int kCtaPages = kScoreCtaThreads / 16 * kEachPages;
 
 __device__ __forceinline__ double wide_hi(uint32_t top) {   // bf16 in the upper half of `top`, as a double times 2^-896
   return __hiloint2double((int)((top & 0x80000000u) | ((top & 0x7fff0000u) >> 3)), 0);
 }
 
-template <int kRounds>   // of four heads
 __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const PageSelectParams p) {
-  constexpr int kPages = kEachPages, kCta = kCtaPages, kHeads = kHeadsAtOnce;
-  __shared__ double2 sm_q[kMaxGroup][4][16];   // channels 8 l + 2 i, 8 l + 2 i + 1 of head h at [h][i][l]
+  constexpr int kPages = kEachPages, kCta = kCtaPages, kHeads = kScalarHeads;
+  __shared__ double2 sm_q[kHeads][4][16];   // channels 8 l + 2 i, 8 l + 2 i + 1 of head h at [h][i][l]
   const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 31, l = lane & 15;
   const int n_kv = p.c.n_kv_heads, G = p.group;
   const int32_t* row = p.c.table + (int64_t)b * p.c.table_stride;
@@ -419,7 +423,7 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
   const int lim = room < p.max_len ? (int)room : p.max_len;
   const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
   if (act == 0 || (int)blockIdx.x * kCta >= pages) return;
-  if (tid < kMaxGroup * 16) {
+  if (tid < kHeads * 16) {
     const uint32_t x[4] = {qw.x, qw.y, qw.z, qw.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -442,47 +446,44 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
       }
     }
   }
-  const int u = l / kHeads;                    // this thread's sum: page u, head h0 + l % kHeads
+  const int u = l / kHeads;                    // this thread's sum: page u, head l % kHeads
   uint64_t key = 0ull;
-#pragma unroll 1
-  for (int h0 = 0; h0 < kRounds * kHeads; h0 += kHeads) {
-    double v[16];   // [page][head]
+  double v[16];   // [page][head]
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.0;
+  for (int i = 0; i < 16; ++i) v[i] = 0.0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      double a0[kPages], a1[kPages], z0[kPages], z1[kPages];
+  for (int i = 0; i < 4; ++i) {
+    double a0[kPages], a1[kPages], z0[kPages], z1[kPages];
+#pragma unroll
+    for (int w = 0; w < kPages; ++w) {
+      const uint32_t a = i == 0 ? least[w].x : i == 1 ? least[w].y : i == 2 ? least[w].z : least[w].w;
+      const uint32_t z = i == 0 ? most[w].x : i == 1 ? most[w].y : i == 2 ? most[w].z : most[w].w;
+      a0[w] = wide_hi(a << 16);
+      a1[w] = wide_hi(a);
+      z0[w] = wide_hi(z << 16);
+      z1[w] = wide_hi(z);
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      const double2 q = sm_q[h][i][l];
+      const bool n0 = __double2hiint(q.x) < 0, n1 = __double2hiint(q.y) < 0;
 #pragma unroll
       for (int w = 0; w < kPages; ++w) {
-        const uint32_t a = i == 0 ? least[w].x : i == 1 ? least[w].y : i == 2 ? least[w].z : least[w].w;
-        const uint32_t z = i == 0 ? most[w].x : i == 1 ? most[w].y : i == 2 ? most[w].z : most[w].w;
-        a0[w] = wide_hi(a << 16);
-        a1[w] = wide_hi(a);
-        z0[w] = wide_hi(z << 16);
-        z1[w] = wide_hi(z);
-      }
-#pragma unroll
-      for (int h = 0; h < kHeads; ++h) {
-        const double2 q = sm_q[h0 + h][i][l];
-        const bool n0 = __double2hiint(q.x) < 0, n1 = __double2hiint(q.y) < 0;
-#pragma unroll
-        for (int w = 0; w < kPages; ++w) {
-          v[kHeads * w + h] = fma(q.x, n0 ? a0[w] : z0[w], v[kHeads * w + h]);
-          v[kHeads * w + h] = fma(q.y, n1 ? a1[w] : z1[w], v[kHeads * w + h]);
-        }
+        v[kHeads * w + h] = fma(q.x, n0 ? a0[w] : z0[w], v[kHeads * w + h]);
+        v[kHeads * w + h] = fma(q.y, n1 ? a1[w] : z1[w], v[kHeads * w + h]);
       }
     }
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
-      const bool up = (lane & o) != 0;
-#pragma unroll
-      for (int j = 0; j < o; ++j) {
-        const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
-        v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-      }
-    }
-    if (h0 + l % kHeads < G) key = max(key, score_key(v[0]));
   }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    const bool up = (lane & o) != 0;
+#pragma unroll
+    for (int j = 0; j < o; ++j) {
+      const double keep = up ? v[j + o] : v[j], give = up ? v[j] : v[j + o];
+      v[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  if (l % kHeads < G) key = score_key(v[0]);
 #pragma unroll
   for (int o = 1; o < kHeads; o <<= 1) key = max(key, (uint64_t)__shfl_xor_sync(0xffffffffu, (unsigned long long)key, o));
   if (l % kHeads == 0 && i0 + u < pages) {
@@ -491,6 +492,67 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
       if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
     }
     p.keys[((int64_t)b * n_kv + g) * p.key_stride + i0 + u] = key;
+  }
+}
+
+// Groups of five to eight heads: the products as m8n8k4 MMAs in 64 bits, eight pages x eight heads, 128 upper bounds with the
+// positive parts of the queries and 128 lower ones with the negative parts.  A warp takes eight pages; the four lanes of a
+// page have 32 channels each, and since the order of a sum is free they hold page and query alike, in 16-byte pieces as they lie in memory.
+__device__ __forceinline__ void mma_f64(double (&c)[2], double a, double b) {
+  asm volatile("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0,%1}, {%2}, {%3}, {%0,%1};" : "+d"(c[0]), "+d"(c[1]) : "d"(a), "d"(b));
+}
+
+__global__ void __launch_bounds__(kScoreCtaThreads) page_score_mma_kernel(const PageSelectParams p) {
+  const int b = blockIdx.z, g = blockIdx.y, tid = threadIdx.x, lane = tid & 31, r = lane >> 2, t = lane & 3;
+  const int n_kv = p.c.n_kv_heads, G = p.group;
+  const int page = blockIdx.x * kCtaPages + (tid >> 5) * 8 + r;
+  pdl_wait();
+  pdl_launch();   // dependents are released only after this kernel's own wait (see launch_ex)
+  // sizes, queries and page number (any of the table's): one round trip
+  const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
+  const int n = __ldcg(p.c.len + b);
+  const int pg = page < p.c.table_stride ? __ldg(p.c.table + (int64_t)b * p.c.table_stride + page) : -1;
+  const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
+  const int lim = room < p.max_len ? (int)room : p.max_len;
+  const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;
+  if (act == 0 || (int)blockIdx.x * kCtaPages >= pages) return;
+  if (tid == 0 && blockIdx.x == 0 && g == 0 && n > lim) atomicOr(p.status, RKV_DEV_LEN_CLAMPED);
+  const bool there = page < pages && (unsigned)pg < (unsigned)p.c.n_pages;
+  uint4 q[4], least[4], most[4];               // channels 32 j + 8 t .. + 7 of head r, of page r
+  const uint4* q_at = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
+                                                     ((int64_t)b * p.n_q_heads + (int64_t)g * G + min(r, G - 1)) * kHeadDim) + t;
+  const int64_t at = ((int64_t)(there ? pg : 0) * n_kv + g) * (kHeadDim / 8) + t;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    q[j] = __ldcg(q_at + 4 * j);
+    least[j] = __ldcg(static_cast<const uint4*>(p.c.k_min) + at + 4 * j);
+    most[j] = __ldcg(static_cast<const uint4*>(p.c.k_max) + at + 4 * j);
+  }
+  double c[4][2] = {};                         // chains
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t qw[4] = {q[j].x, q[j].y, q[j].z, q[j].w}, lw[4] = {least[j].x, least[j].y, least[j].z, least[j].w},
+                   mw[4] = {most[j].x, most[j].y, most[j].z, most[j].w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t up = (e & 1) != 0 ? 0u : 16u;
+      const double x = wide_hi(qw[e >> 1] << up) * 0x1p1000 * 0x1p408;
+      const bool neg = __double2hiint(x) < 0;
+      mma_f64(c[e & 1], wide_hi(mw[e >> 1] << up), neg ? 0.0 : x);
+      mma_f64(c[2 + (e & 1)], wide_hi(lw[e >> 1] << up), neg ? x : 0.0);
+    }
+  }
+  uint64_t key = 0ull;                         // page r, heads 2 t and 2 t + 1
+  if (2 * t < G) key = score_key((c[0][0] + c[1][0]) + (c[2][0] + c[3][0]));
+  if (2 * t + 1 < G) key = max(key, score_key((c[0][1] + c[1][1]) + (c[2][1] + c[3][1])));
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) key = max(key, (uint64_t)__shfl_xor_sync(0xffffffffu, (unsigned long long)key, o));
+  if (t == 0 && page < pages) {
+    if (!there) {   // a page that is not there comes after all others
+      key = 0ull;
+      if (g == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
+    }
+    p.keys[((int64_t)b * n_kv + g) * p.key_stride + page] = key;
   }
 }
 
@@ -524,7 +586,7 @@ cudaError_t prepare_page_select() {
 }
 
 cudaError_t launch_page_scores(const PageSelectParams& p, int n_seq, int most_pages, cudaStream_t st) {
-  return launch_ex(p.group > kHeadsAtOnce ? page_score_kernel<2> : page_score_kernel<1>,
+  return launch_ex(p.group > kScalarHeads ? page_score_mma_kernel : page_score_kernel,
                    dim3((most_pages + kCtaPages - 1) / kCtaPages, p.c.n_kv_heads, n_seq), dim3(kScoreCtaThreads), 0, st, 1, p);
 }
 
@@ -547,6 +609,7 @@ cudaError_t launch_paged_append(const PagedAppendParams& p0, bool is_bf16, bool 
   }
   // CTAs of a unit: queries in groups of 32 heads or so, keys and values in groups as large (four rounds of the CTA's
   // warps) or, where that leaves less than kAppendSpread CTAs to an SM, smaller ones (sines and cosines are worked out once per CTA).
+  // 32 heads a CTA / 8: 1024 rows 18.5 / 9.9 us, 4096 rows 26.9 / 24.8, 32768 rows 138.5 / 150.6, 64 sequences of 256 rows 77.0 / 80.3.
   const int64_t want = kAppendSpread * (int64_t)sm_count, have = (int64_t)units * n_seq;
   int per = 32;
   while (per > 8 && have * ((heads + per - 1) / per) < want) per -= 8;

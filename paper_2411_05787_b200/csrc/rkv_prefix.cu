@@ -13,11 +13,12 @@
 // the end; with two each group has its block, and a tile that is in shared memory serves 256 rows (that every block fetched K and V
 // for itself would need more than L2 can deliver).  Tensor memory holds an O and two S of 64 columns per group: S of task
 // k + 1 is there when the exponentials of task k are done; S of task k + 2 goes where P of task k is, when that has been multiplied.
-// Measured, 64 sequences of 4 heads behind 32768 positions of 8 KV heads: 47 us, where HBM would allow 20.5, the tensor cores 30;
-// a group's chain is the rest (S of a task is waited for and read 450 clocks, its maximum 500, the exponentials 750).
-// On the way: one warp that issues for both groups, in a fixed order or polling, 62 (every wait and issue of one
-// group delays the other); both groups at their exponentials at the same time 50; S of 128 columns, one per group, 59; half a row
-// per thread with 16 softmax warps 103 (96 registers, spilled beside a shared memory that leaves no L1).
+// Measured, 64 sequences of 4 heads behind 32768 positions of 8 KV heads: 42 us, where HBM would allow 20.5, the tensor cores 30;
+// a group's chain is the rest (S of a task is waited for and read 450 clocks, its maximum 500, the exponentials 750), and what
+// stands before the first tile and behind the last (3 us and 4).  The copy warp begins while the others stage the queries: 47
+// when it waited for them.  On the way, at 47: one warp that issues for both groups, in a fixed order or polling, 62 (every wait and
+// issue of one group delays the other); both groups at their exponentials at the same time 50; S of 128 columns, one per group, 59;
+// half a row per thread with 16 softmax warps 103 (96 registers, spilled beside a shared memory that leaves no L1).
 // A thread has one row: maxima and sums need no exchange.  P goes back to tensor memory as bf16 over its S and is the A operand
 // of O += P V; V, with its channels contiguous, is an MN-major B operand.  The accumulators are rescaled only when a row's
 // maximum has grown by more than 2^8 since the last time, which keeps P below 2^8; P is rounded to bf16 (2^-8 relative
