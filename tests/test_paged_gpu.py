@@ -315,6 +315,21 @@ def test_attention_of_many_sequences(rkv):
         check_out(out[b], *PO.attend(f64(q[b]), *pool.host(b, n)), f"length {n}")
 
 
+@pytest.mark.parametrize("n_kv,longest", [(2, 9001), (4, 4100), (8, 3000)])
+def test_attention_of_a_batch_that_fills_the_chip(rkv, n_kv, longest):
+    """Clusters whose CTAs have many tiles each, few for some sequences, none for others."""
+    g = np.random.default_rng(n_kv)
+    lens = [longest, 0, 1, 511, longest - 1] + [int(x) for x in g.integers(0, longest, 11)]
+    pool = Pool(rkv, [n + 1 for n in lens], n_kv, 16, 5, lens=lens, bounds=False)
+    ctx = rkv.Context(16, 3 * n_kv, n_kv, longest, 64)
+    q = normal(gen(7), 16, 3 * n_kv, 128).to(torch.bfloat16)
+    out = torch.empty_like(q)
+    ctx.paged_attention(q, pool.struct(), out)
+    assert ctx.device_status() == 0
+    for b, n in enumerate(lens):
+        check_out(out[b], *PO.attend(f64(q[b]), *pool.host(b, n)), f"length {n}")
+
+
 def test_pool_beyond_32_bits(rkv):
     """Pages whose bytes lie beyond 2^32: rows are written there, attended and selected from there."""
     page, n_q, n_kv, n_pages, n = 128, 4, 2, 80000, 700       # 5.2 GB a buffer
@@ -502,6 +517,17 @@ def test_sparse_of_a_long_sequence(rkv, n, page, top):
     q = normal(gen(3), 1, 4, 128).to(torch.bfloat16)
     check_sparse(rkv, ctx, pool, q, [n], top, 1, 1)
     check_sparse(rkv, ctx, pool, q, [n], top, 1, 1, hint=n)
+
+
+@pytest.mark.parametrize("n_q", [4, 16])
+@pytest.mark.parametrize("top", [500, 600])
+def test_sparse_of_many_pages_in_a_batch(rkv, top, n_q):
+    """About as many pages as the attention's CTAs pick themselves; a batch that fills the chip."""
+    lens = [9600, 9601, 9700, 0, 3, 8000, 8001, 9599] * 2
+    pool = Pool(rkv, [n + 1 for n in lens], 2, 16, top, lens=lens)
+    ctx = rkv.Context(16, n_q, 2, 9728, 64)
+    q = normal(gen(8), 16, n_q, 128).to(torch.bfloat16)
+    check_sparse(rkv, ctx, pool, q, lens, top, 1, 1)
 
 
 @pytest.mark.parametrize("how", ["all alike", "pairs", "two kinds", "zero query", "extremes", "infinite"])
