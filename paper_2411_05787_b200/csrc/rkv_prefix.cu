@@ -22,7 +22,8 @@
 // A thread has one row: maxima and sums need no exchange.  P goes back to tensor memory as bf16 over its S and is the A operand
 // of O += P V; V, with its channels contiguous, is an MN-major B operand.  The accumulators are rescaled only when a row's
 // maximum has grown by more than 2^8 since the last time, which keeps P below 2^8; P is rounded to bf16 (2^-8 relative
-// at most) where it meets V, and l adds the values up unrounded, in fp32.
+// at most) where it meets V, and l adds up the rounded values, in fp32, so that what all values have in common comes through
+// unrounded, as in the other passes (a sharp row's largest probability is not 1 beside an older maximum, and is rounded too).
 //
 // A tile is gathered page by page, each of the four (K | V) x (channels 0-63 | 64-127) parts of a piece by one copy, so that
 // the tile lies in shared memory as [part][64 rows][64 channels] with the 128-byte swizzle, whatever the page.  Pieces that
@@ -396,7 +397,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         a = ex2(a);
         b = ex2(b);
         y[e] = pack_bf16(a, b);
-        sum[e & 1] = add_pair(sum[e & 1], pair_of(a, b));
+        sum[e & 1] = add_pair(sum[e & 1], pair_of(__uint_as_float(y[e] << 16), __uint_as_float(y[e] & 0xffff0000u)));
       }
       tmem_st32(s_at, y);
       mbar_arrive(bar_turn + 8 * (1 - w));    // (behind the store, which needs all of them)
