@@ -426,7 +426,7 @@ typedef struct {
 /*
  * Append a prompt's, a chunk's or a token's rows to a paged cache straight from the fused projection, in one launch: queries,
  * keys and values are split, queries and keys turned by their positions as rkv_rope turns them (freqs, rot_dim,
- * layout, amplitude as there; sines and cosines may be up to 2^-20 apart from its; freqs == NULL: nothing is turned), and
+ * layout, amplitude as there, and the same to the last bit; freqs == NULL: nothing is turned), and
  * rounded to bf16.  For row t < count[b] of sequence b,
  * p = start[b] + t:  q[b][t] = its queries, k and v at position p = its keys and values;  len[b] = start[b] + count[b].
  * Bounds: the page that p lies in has, when the call is over,

@@ -19,9 +19,10 @@ namespace {
 // bounds stay in the warp's registers until the page ends, and no two CTAs meet at a page and head.  Eight threads share
 // a row, each with two pieces of eight channels (eight pairs, or channels that are only copied).  A warp works through batches
 // of 16 rows, four of a thread's, all of them requested before the first is used.  Sines and cosines of the unit's (row, pair)s
-// are worked out once per CTA, in shared memory, while the first batch is on its way.
+// are worked out once per CTA, in shared memory, each from its own angle, so that rows are those of rkv_rope to the last bit (from the
+// angles of every eighth position and of 0 .. 7 positions, by the sum's formula: no faster, the prompt 140 us, and 2^-22 off instead of 2^-23).
 // With up to kFewRows rows a sequence (tokens of a decode step) eight threads take a head, and a CTA 32 of them.
-// Measured (32 + 16 heads): a prompt of 32768 bf16 rows 139 us, 5.8 TB/s (rows requested one by one as others are done with 215, two
+// Measured (32 + 16 heads): a prompt of 32768 bf16 rows 138 us, 5.8 TB/s (rows requested one by one as others are done with 215, two
 // batches in turn 153, three or four CTAs to an SM, which spill, 158 to 231, 512 threads 144); one row 3.4 us.
 // Few rows here / in units: 1 row 3.1 / 4.3 us, 64 sequences of 1 row 3.4 / 8.8, of 4 rows 5.4 / 9.9, of 8 rows 8.2 / 10.4, but
 // 1 sequence of 8 rows 6.7 / 4.6, of 16 rows 11.0 / 5.0, 64 of 16 rows 14.1 / 11.2.
@@ -37,10 +38,6 @@ struct AppendShared {
   float2 cs[kUnit][kCsRow];                  // pair 8 i + j of a row at 8 j + i: the eight threads of a row read side by side
   int sizes[3];
   int page[kUnit / 16];
-};
-
-struct BulkShared : AppendShared {
-  float2 ef[16][kHeadDim / 2];               // of rows 0, 8, .., 56 of the unit, and of 0 .. 7 positions
 };
 
 struct NewRows { int start, count; };
@@ -80,20 +77,17 @@ __device__ __forceinline__ NewRows append_sizes(const PagedAppendParams& p, Appe
   return n;
 }
 
-// (cos, sin) of a position's angle, and of the sum of two angles.
+// (cos, sin) of a position's angle, as rkv_rope forms them.
 __device__ __forceinline__ float2 angle(int64_t pos, unsigned long long freq) {
   float s, c;
   sincospif((float)(int)(((unsigned long long)pos * freq) >> 32) * 4.656612873e-10f, &s, &c);   // 2^-31: half turns
   return make_float2(c, s);
 }
-__device__ __forceinline__ float2 turn_by(float2 a, float2 b) {
-  return make_float2(__fmaf_rn(a.x, b.x, -__fmul_rn(a.y, b.y)), __fmaf_rn(a.x, b.y, __fmul_rn(a.y, b.x)));
-}
 
 // Pages and angles of the rows of positions lo .. hi - 1, which lie in the unit (or the half of a page of 128) that begins at
 // s0; row r of it at sm.cs[r].
-template <bool kFew, typename Shared>
-__device__ __forceinline__ void append_part(const PagedAppendParams& p, Shared& sm, int b, int64_t s0, int64_t lo, int64_t hi,
+template <bool kFew>
+__device__ __forceinline__ void append_part(const PagedAppendParams& p, AppendShared& sm, int b, int64_t s0, int64_t lo, int64_t hi,
                                             int tid) {
   const int most = min(1 << p.c.page_shift, kUnit);       // positions of a page in this part
   if (tid < kUnit / most) {
@@ -108,24 +102,17 @@ __device__ __forceinline__ void append_part(const PagedAppendParams& p, Shared& 
     }
     sm.page[tid] = pg;
   }
-  // a row's angle is that of the multiple of 8 below it and that of the rest: 16 sines and cosines a pair instead of 64
   const int half = p.rot >> 1, r0 = (int)(lo - s0), n = (int)(hi - lo);
-  auto put = [&](int r, int j, float2 e) { sm.cs[r][8 * (j & 7) + (j >> 3)] = make_float2(e.x * p.amp, e.y * p.amp); };
+  auto put = [&](int r, int j, unsigned long long freq) {
+    const float2 e = angle(s0 + r, freq);
+    sm.cs[r][8 * (j & 7) + (j >> 3)] = make_float2(e.x * p.amp, e.y * p.amp);
+  };
   if constexpr (kFew) {
-    for (int i = tid; i < n * half; i += kAppendThreads) {
-      const int r = r0 + i / half, j = i % half;
-      const unsigned long long f = __ldg(p.freqs + j);
-      put(r, j, turn_by(angle(s0 + (r & ~7), f), angle(r & 7, f)));
-    }
-  } else {
-    for (int i = tid; i < 16 * half; i += kAppendThreads) {
-      const int k = i / half, j = i - k * half;
-      sm.ef[k][j] = angle(k < 8 ? s0 + 8 * k : k - 8, __ldg(p.freqs + j));
-    }
-    __syncthreads();
-    for (int i = tid; i < n * half; i += kAppendThreads) {
-      const int r = r0 + i / half, j = i % half;
-      put(r, j, turn_by(sm.ef[r >> 3][j], sm.ef[8 + (r & 7)][j]));
+    for (int i = tid; i < n * half; i += kAppendThreads) put(r0 + i / half, i % half, __ldg(p.freqs + i % half));
+  } else {                                                 // a warp per row
+    for (int j = tid & 31; j < half; j += 32) {
+      const unsigned long long freq = __ldg(p.freqs + j);
+      for (int r = r0 + (tid >> 5); r < r0 + n; r += kAppendWarps) put(r, j, freq);
     }
   }
 }
@@ -189,7 +176,7 @@ struct Head {   // of the fused projection
 
 template <typename T, bool kInterleaved>
 __global__ void __launch_bounds__(kAppendThreads, 2) paged_append_kernel(const PagedAppendParams p) {
-  __shared__ BulkShared sm;
+  __shared__ AppendShared sm;
   const int b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int part = tid & 7, octet = lane >> 3;
   const int page = 1 << p.c.page_shift, unit = page > kUnit ? page : kUnit, most = page < kUnit ? page : kUnit;

@@ -2,9 +2,32 @@
 import pytest
 import torch
 
-from test_paged_gpu import Pool, rkv  # noqa: F401  (rkv: the fixture)
+from test_paged_gpu import Pool, i32, normal, gen, rkv  # noqa: F401  (rkv: the fixture)
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layout,rot,scaling,factor", [("half", 128, "none", 1.0), ("interleaved", 128, "bands", 8.0),
+                                                       ("half", 48, "ramp", 4.0), ("interleaved", 64, "linear", 2.0)])
+@pytest.mark.parametrize("T", [1, 4, 5, 700])
+def test_appended_rows_are_those_that_rope_turns(rkv, T, layout, rot, scaling, factor, dtype):
+    """Tokens, chunks and prompts, near and far: one angle, one sine and cosine, one product."""
+    n_q, n_kv, page, starts = 14, 2, 128 if T > 4 else 32, [0, 7, 70001]
+    pool = Pool(rkv, [s + T for s in starts], n_kv, page, T, lens=starts)
+    ctx = rkv.Context(len(starts), n_q, n_kv, 1024, 64)
+    x = normal(gen(rot + T), len(starts), T, (n_q + 2 * n_kv) * 128).to(dtype)
+    q = torch.empty((len(starts), T, n_q, 128), dtype=torch.bfloat16, device="cuda")
+    table = rkv.RopeTable(rot, 500000.0, layout, scaling, factor)
+    ctx.paged_append(x, pool.struct(), table, q)
+    for b, s in enumerate(starts):
+        want = [torch.empty((T, h, 128), dtype=torch.bfloat16, device="cuda") for h in (n_q, n_kv, n_kv)]
+        ctx.rope(x[b], i32(list(range(s, s + T))), table, *want)
+        at = torch.arange(s, s + T, device="cuda")
+        pages, rows = pool.table[b].long()[at // page], at % page
+        assert torch.equal(q[b], want[0])
+        assert torch.equal(pool.k[pages, :, rows], want[1]) and torch.equal(pool.v[pages, :, rows], want[2])
+    assert ctx.device_status() == 0
 
 
 @pytest.mark.parametrize("B", [16, 40])
