@@ -94,7 +94,7 @@ __device__ __forceinline__ void append_part(const PagedAppendParams& p, AppendSh
     const int64_t at = s0 + tid * most;
     int pg = -1;
     if (at < hi && at + most > lo) {
-      pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + (at >> p.c.page_shift));
+      pg = __ldcg(p.c.table + (int64_t)b * p.c.table_stride + (at >> p.c.page_shift));
       if ((unsigned)pg >= (unsigned)p.c.n_pages) {
         pg = -1;
         if (blockIdx.y == 0) atomicOr(p.status, RKV_DEV_BAD_INDEX);
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_kernel(const Page
   const int i0 = blockIdx.x * kCta + (tid >> 4) * kPages;    // this thread's pages
   int pg[kPages];
 #pragma unroll
-  for (int u = 0; u < kPages; ++u) pg[u] = i0 + u < p.c.table_stride ? __ldg(row + i0 + u) : -1;
+  for (int u = 0; u < kPages; ++u) pg[u] = i0 + u < p.c.table_stride ? __ldcg(row + i0 + u) : -1;
   uint4 qw = make_uint4(0u, 0u, 0u, 0u);
   if (tid < G * 16)
     qw = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) +
@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(kScoreCtaThreads) page_score_mma_kernel(const 
   // sizes, queries and page number (any of the table's): one round trip
   const int act = p.active != nullptr ? __ldcg(p.active + b) : 1;
   const int n = __ldcg(p.c.len + b);
-  const int pg = page < p.c.table_stride ? __ldg(p.c.table + (int64_t)b * p.c.table_stride + page) : -1;
+  const int pg = page < p.c.table_stride ? __ldcg(p.c.table + (int64_t)b * p.c.table_stride + page) : -1;
   const int64_t room = (int64_t)p.c.table_stride << p.c.page_shift;
   const int lim = room < p.max_len ? (int)room : p.max_len;
   const int pages = (min(max(n, 0), lim) + (1 << p.c.page_shift) - 1) >> p.c.page_shift;

@@ -277,7 +277,7 @@ struct Pieces {
     if (i < 0) return;
     const int left = s.n - ((i << shift) + off);
     if (left <= 0) return;
-    const int pg = __ldg(p.c.table + (int64_t)b * p.c.table_stride + i);
+    const int pg = __ldcg(p.c.table + (int64_t)b * p.c.table_stride + i);
     if ((unsigned)pg >= (unsigned)p.c.n_pages) {
       atomicOr(p.status, RKV_DEV_BAD_INDEX);
       return;

@@ -232,7 +232,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int mine = lane >> 2, part = lane & 3;
     auto page_of = [&](int t) {              // of this lane's piece; -1: none
       const int pos = (split + t * n_cta) * kXTile + mine * piece;
-      return t < n_tiles && mine < pieces && pos < positions ? __ldg(p.shared + (pos >> shift)) : -1;
+      return t < n_tiles && mine < pieces && pos < positions ? __ldcg(p.shared + (pos >> shift)) : -1;
     };
     bool ok = true;
     int pg = page_of(0), issued = 0;
