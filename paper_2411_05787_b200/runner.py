@@ -186,7 +186,8 @@ class QuantLayerState(LayerState):
 
 class PagedLayerState:
     """A layer whose cache is paged (synth.PagedCache): there is one cache and no refresh.  A step appends the rows of the fused
-    projection and attends either everything or the pages whose bounds promise the largest scores."""
+    projection and attends either everything or the pages whose bounds promise the largest scores.  An alternative to the
+    method of LayerState, not one of its forms: the schedules below, which refresh small caches, do not take it."""
 
     def __init__(self, ctx: rkv.Context, cache: PagedCache, n_q_heads: int, n_kv_heads: int, top_pages: int):
         dev = cache.k.device
@@ -210,6 +211,14 @@ class PagedLayerState:
         self.ctx.paged_sparse_attention(q, self.full_c, self.top_pages, self.page_idx, self.out, active=active,
                                         first_pages=first_pages, last_pages=last_pages, max_len_hint=max_len_hint)
         return self.out
+
+    def _refused(self, *args, **kwargs):
+        raise NotImplementedError("a paged cache has no small cache to refresh: append, attend, attend_selected")
+
+    refresh = refresh_attention = append_refresh_attention = refresh_select = refresh_score_keys = _refused
+    refresh_select_only = refresh_scores_only = partial = append_partial = check_trigger = _refused
+    enable_eviction = refresh_evict = append_partial_evict = _refused
+    small = flag = not_flag = topk_idx = property(_refused)
 
 
 class OverlappedRefresh:
