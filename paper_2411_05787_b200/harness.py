@@ -237,7 +237,8 @@ class LlamaDecoder:
     # ------------------------------------------------------------------ one decode token (measured path)
     def attention(self, l: int, kind: str):
         st, q, k, v = self.states[l], self.q[l], self.k[l], self.v[l]
-        if self.page is not None:
+        if self.page is not None:                        # (the append turns and splits the projection's row on its way)
+            st.append(self.qkv.view(1, 1, -1), self.table, q[None])
             (st.attend if kind == "full" else st.attend_selected)(q, max_len_hint=self.full_hint)
             if self.capture is not None and l in self.capture[0]:
                 torch.cuda.synchronize()
@@ -264,7 +265,8 @@ class LlamaDecoder:
 
     def token_step(self, kind: str, with_harness: bool = True, with_attention: bool = True):
         """kind: 'small' (partial steps everywhere), 'check' (trigger decides per layer) or 'full'; with paged caches 'small'
-        and 'check' are the same, a step over the selected pages."""
+        and 'check' are the same, a step over the selected pages.  Without its decoder a token appends and attends what the last
+        one's buffers hold (over pages: the last projection's row in every layer)."""
         s = self.s
         if with_harness:
             embed(self.embed_w, self.token, self.x)
@@ -273,7 +275,7 @@ class LlamaDecoder:
                 gemv(wl["wqkv"], self.x, self.qkv, norm_w=wl["norm1"], eps=s.eps)        # RMSNorm fused into the read of x
                 pos = self.states[l].full.len
                 if self.page is not None:
-                    self.states[l].append(self.qkv.view(1, 1, -1), self.table, self.q[l][None])
+                    pass                                                                 # (attention() appends, which turns)
                 elif self.table is not None:
                     self.ctx.rope(self.qkv[None], pos, self.table, self.q[l], self.k[l], self.v[l])
                 else:
