@@ -15,17 +15,19 @@ namespace {
 // their positions (the angle as in rkv_rope.cu: turns as 64-bit fixed point), and the keys' bounds follow.
 //
 // HBM-bound for prompts: every channel is read once and written once.  A CTA takes the new rows of kUnit positions (or of
-// one page, where that is more) for 8 or more heads, a warp one head at a time over all of those rows, so that a page's
-// bounds stay in the warp's registers until the page ends, and no two CTAs meet at a page and head.  Eight threads share
-// a row, each with two pieces of eight channels (eight pairs, or channels that are only copied).  A warp works through batches
-// of 16 rows, four of a thread's, all of them requested before the first is used.  Sines and cosines of the unit's (row, pair)s
+// one page, where that is more) for 8 or more heads, of queries or of keys and values.  Eight threads share a row, each with two
+// pieces of eight channels (eight pairs, or channels that are only copied).  Keys and values: a warp takes one head at a time
+// over all of those rows, so that a page's bounds stay in the warp's registers until the page ends, and no two CTAs meet at a page
+// and head; it works through batches of 16 rows, four of a thread's, all of them requested before the first is used.  Queries: four
+// rows to a warp, of which eight threads go through the heads, four at a time.  Sines and cosines of the unit's (row, pair)s
 // are worked out once per CTA, in shared memory, each from its own angle, so that rows are those of rkv_rope to the last bit (from the
-// angles of every eighth position and of 0 .. 7 positions, by the sum's formula: no faster, the prompt 140 us, and 2^-22 off instead of 2^-23).
+// angles of every eighth position and of 0 .. 7 positions, by the sum's formula: the prompt 139 us, 16 rows 4.9 instead of 4.2, and 2^-22 off instead of 2^-23).
 // With up to kFewRows rows a sequence (tokens of a decode step) eight threads take a head, and a CTA 32 of them.
-// Measured (32 + 16 heads): a prompt of 32768 bf16 rows 138 us, 5.8 TB/s (rows requested one by one as others are done with 215, two
-// batches in turn 153, three or four CTAs to an SM, which spill, 158 to 231, 512 threads 144); one row 3.4 us.
-// Few rows here / in units: 1 row 3.1 / 4.3 us, 64 sequences of 1 row 3.4 / 8.8, of 4 rows 5.4 / 9.9, of 8 rows 8.2 / 10.4, but
-// 1 sequence of 8 rows 6.7 / 4.6, of 16 rows 11.0 / 5.0, 64 of 16 rows 14.1 / 11.2.
+// Measured (32 + 16 heads): a prompt of 32768 bf16 rows 135 us, 6.0 TB/s (rows requested one by one as others are done with 215, two
+// batches in turn 153, three or four CTAs to an SM, which spill, 158 to 231, 512 threads 144); one row 3.1 us.
+// Few rows here / in units: 1 row 3.1 / 4.1 us, 64 sequences of 1 row 3.1 / 7.8, of 4 rows 5.3 / 9.2, of 8 rows 8.1 / 9.4, but
+// 1 sequence of 8 rows 6.6 / 4.0, of 16 rows 10.9 / 4.2, 64 of 16 rows 16.4 / 10.6.
+// fp32 rows hold twice the registers in flight: 128 of them and 28 to 36 bytes spilled; a prompt of 16384 rows 104 us, 5.8 TB/s (interleaved pairs 130).
 constexpr int kAppendThreads = 256, kAppendWarps = kAppendThreads / 32;
 constexpr int kUnit = 64;                    // positions of a CTA
 constexpr int kBatchRows = 16, kAhead = kBatchRows / 4;      // rows of a warp in flight, and of a thread
@@ -168,6 +170,9 @@ struct Head {   // of the fused projection
   // where the row of position pos (token t) goes; null: its page is not there
   __device__ __forceinline__ __nv_bfloat16* row(const PagedAppendParams& p, int b, int t, int64_t pos, int pg) const {
     if (is_q) return static_cast<__nv_bfloat16*>(p.q) + (((int64_t)b * p.n_tok + t) * p.n_q_heads + g) * kHeadDim;
+    return in_page(p, pos, pg);
+  }
+  __device__ __forceinline__ __nv_bfloat16* in_page(const PagedAppendParams& p, int64_t pos, int pg) const {
     if (pg < 0) return nullptr;
     return static_cast<__nv_bfloat16*>(is_k ? p.c.k : p.c.v) +
            ((((int64_t)pg * p.c.n_kv_heads + g) << p.c.page_shift) + (pos & ((1 << p.c.page_shift) - 1))) * kHeadDim;
@@ -241,7 +246,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) paged_append_kernel(const P
     for (int round = 0; round < n_heads; ++round) {
       const int h = h0 + round * kAppendWarps;
       const Head head(p, h);
-      const bool turn = turns && (head.is_q || head.is_k), bounds = head.is_k && p.c.k_min != nullptr;
+      const bool turn = turns && head.is_k, bounds = head.is_k && p.c.k_min != nullptr;
       const T* x = part_rows + h * kHeadDim;
       Bounds8 ba, bb;
       ba.reset();
@@ -256,8 +261,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) paged_append_kernel(const P
           xa[i].load(x + r * p.tok_stride + ca);
           xb[i].load(x + r * p.tok_stride + cb);
         }
-        __nv_bfloat16* to = head.row(p, b, (int)(s0 + at + octet - nr.start), s0 + at + octet, pg);
-        const int64_t to_step = head.is_q ? (int64_t)p.n_q_heads * kHeadDim : kHeadDim;
+        __nv_bfloat16* to = head.in_page(p, s0 + at + octet, pg);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
           const int r = at + 4 * i + octet;
@@ -278,8 +282,8 @@ __global__ void __launch_bounds__(kAppendThreads, 2) paged_append_kernel(const P
               bb.take(pb);
             }
             if (to != nullptr) {
-              *reinterpret_cast<uint4*>(to + 4 * i * to_step + ca) = pa;
-              *reinterpret_cast<uint4*>(to + 4 * i * to_step + cb) = pb;
+              *reinterpret_cast<uint4*>(to + 4 * i * kHeadDim + ca) = pa;
+              *reinterpret_cast<uint4*>(to + 4 * i * kHeadDim + cb) = pb;
             }
           }
         }
@@ -344,11 +348,11 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_few_kernel(const 
       xa.get(a);
       xb.get(w);
       if (turn) {
-            float2 cs[8];
+        float2 cs[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) cs[j] = sm.cs[r][part + 8 * j];
-            turn_pieces<kInterleaved>(a, w, cs);
-          }
+        for (int j = 0; j < 8; ++j) cs[j] = sm.cs[r][part + 8 * j];
+        turn_pieces<kInterleaved>(a, w, cs);
+      }
       const uint4 pa = pack8(a), pb = pack8(w);
       __nv_bfloat16* to = head.row(p, b, t, pos, pg);
       if (to != nullptr) {
@@ -596,7 +600,7 @@ cudaError_t launch_paged_append(const PagedAppendParams& p0, bool is_bf16, bool 
   }
   // CTAs of a unit: queries in groups of 32 heads or so, keys and values in groups as large (four rounds of the CTA's
   // warps) or, where that leaves less than kAppendSpread CTAs to an SM, smaller ones (sines and cosines are worked out once per CTA).
-  // 32 heads a CTA / 8: 1024 rows 18.5 / 9.9 us, 4096 rows 26.9 / 24.8, 32768 rows 138.5 / 150.6, 64 sequences of 256 rows 77.0 / 80.3.
+  // 32 heads a CTA / 8: 1024 rows 21.0 / 10.4 us, 4096 rows 29.0 / 26.7, 32768 rows 134.5 / 143.6, 64 sequences of 256 rows 75.7 / 76.4.
   const int64_t want = kAppendSpread * (int64_t)sm_count, have = (int64_t)units * n_seq;
   int per = 32;
   while (per > 8 && have * ((heads + per - 1) / per) < want) per -= 8;
