@@ -406,9 +406,11 @@ rkv_status rkv_rope(rkv_ctx* ctx, const void* qkv, int32_t is_bf16, int64_t tok_
  *   k_min, k_max  [n_pages][Hkv][128]
  * which rkv_paged_append keeps and rkv_paged_sparse_attention scores pages by; both NULL: no bounds are kept.
  * A page may be in several tables (a common prefix) as long as no call writes it.  Entries of table below a sequence's
- * length (or, in an append, its new length) are read; one outside 0 .. n_pages - 1 sets RKV_DEV_BAD_INDEX, and its
- * positions are neither written nor attended.  Lengths above table_stride * page (or the call's bound) are clamped to it
- * and set RKV_DEV_LEN_CLAMPED.
+ * length (or, in an append, its new length) count; one outside 0 .. n_pages - 1 sets RKV_DEV_BAD_INDEX, and its
+ * positions are neither written nor attended.  (The others may be read and hold anything.)  Lengths above
+ * table_stride * page (or the call's bound) are clamped to it and set RKV_DEV_LEN_CLAMPED.
+ * Inactive sequences of the attention calls (active[b] == 0): out and page_idx are left as they are and no flag is set; their
+ * queries, lengths and tables may be read and hold anything.
  * The attention calls end what rkv_full_attention or rkv_quant_full_attention left in the context for a rkv_select_topk.
  */
 typedef struct {
@@ -463,11 +465,10 @@ rkv_status rkv_paged_attention(rkv_ctx* ctx, const void* q, const rkv_paged_cach
  * With n = len[b] and P = ceil(n / page) pages, for page i
  *   score[i] = max_{h in group g} sum_c max(q[h][c] k_min[i][c], q[h][c] k_max[i][c]),
  * which no <q[h], k> of the page exceeds; evaluated in 64 bits, so that only equal sums tie.  The first `first_pages` and the
- * last `last_pages` of the P pages come before all others; then the larger score, then the lower page.  The m = min(top_pages, P)
+ * last `last_pages` of the P pages come before all others, the lower ones first; then the larger score, then the lower page.  The m = min(top_pages, P)
  * foremost pages are attended as in rkv_full_step (positions >= n are not), and
  *   page_idx[b][g][0..m) = those pages in ascending order, m..top_pages-1 = -1.
  * In the scores an infinity, of a bound or a query, counts as 2^128 with its sign, and NaN as some number of that size.
- * Inactive sequences: nothing is read or written.
  *   page_idx   int32 [B][Hkv][top_pages]
  *   top_pages, first_pages, last_pages   host values, >= 1, >= 0, >= 0
  */

@@ -210,3 +210,33 @@ def test_ragged_batch_of_large_groups(rkv, G):
     q = normal(gen(8), 8, 3 * G, 128).to(torch.bfloat16)
     active = i32([1, 1, 1, 1, 0, 1, 1, 1])
     check_sparse(rkv, ctx, pool, q, lens, 11, 1, 1, active=active)
+
+
+# ------------------------------------------------------------------------------------------------------ inactive sequences
+@pytest.mark.parametrize("G", [4, 7])
+@pytest.mark.parametrize("form", ["clusters", "balanced", "shared"])
+def test_inactive_sequences_may_hold_anything(rkv, form, G):
+    """Queries of NaN, lengths and tables of garbage where the mask is zero: no flag, outputs left alone, the others as ever."""
+    n_kv, page, prefix = 2, 64, 1024
+    lens = [prefix + x for x in ((100, 0, 700, 31, 5) if form != "balanced" else (9000, 0, 3, 8000, 1))]
+    B = len(lens)
+    pool = Pool(rkv, lens, n_kv, page, G, lens=lens, shared=prefix // page)
+    pool.pages = pool.table.clone()
+    ctx = rkv.Context(B, G * n_kv, n_kv, 32768 if form == "balanced" else 2048, 64)
+    ctx.set_option(rkv.OPT_SHARED_MIN, 0)
+    q = normal(gen(2), B, G * n_kv, 128).to(torch.bfloat16)
+    active = i32([1, 0, 1, 0, 0])
+    q[1], q[3], q[4] = math.nan, math.inf, -math.inf
+    pool.len[1], pool.len[3], pool.len[4] = 2 ** 31 - 1, -7, prefix
+    pool.table[1], pool.table[3], pool.table[4] = 10 ** 9, -(10 ** 9), -1
+    out, near, idx = torch.full_like(q, 7.0), torch.full_like(q, 7.0), i32([[[-7] * 9] * n_kv] * B)
+    ctx.paged_attention(q, pool.struct(), out, active=active, shared=pool.shared if form == "shared" else None)
+    ctx.paged_sparse_attention(q, pool.struct(), 9, idx, near, active=active)
+    assert ctx.device_status() == 0
+    for b, n in enumerate(lens):
+        if not int(active[b]):
+            assert (out[b] == 7).all() and (near[b] == 7).all() and (idx[b] == -7).all()
+            continue
+        check_out(out[b], *attend64(q[b], pool, b, n), f"length {n}")
+        at = [[p for i in idx[b, g].tolist() if i >= 0 for p in range(i * page, min((i + 1) * page, n))] for g in range(n_kv)]
+        check_out(near[b], *PO.attend(f64(q[b]), *pool.host(b, n), at=at), f"length {n}, selected")
