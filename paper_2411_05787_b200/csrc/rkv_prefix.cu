@@ -13,7 +13,7 @@
 // the end; with two each group has its block, and a tile that is in shared memory serves 256 rows (that every block fetched K and V
 // for itself would need more than L2 can deliver).  Tensor memory holds an O and two S of 64 columns per group: S of task
 // k + 1 is there when the exponentials of task k are done; S of task k + 2 goes where P of task k is, when that has been multiplied.
-// Measured, 64 sequences of 4 heads behind 32768 positions of 8 KV heads: 42 us, where HBM would allow 20.5, the tensor cores 30;
+// Measured, 64 sequences of 4 heads behind 32768 positions of 8 KV heads: 43 us, where HBM would allow 20.5, the tensor cores 30;
 // a group's chain is the rest (S of a task is waited for and read 450 clocks, its maximum 500, the exponentials 750), and what
 // stands before the first tile and behind the last (3 us and 4).  The copy warp begins while the others stage the queries: 47
 // when it waited for them.  On the way, at 47: one warp that issues for both groups, in a fixed order or polling, 62 (every wait and
