@@ -305,6 +305,17 @@ __device__ __forceinline__ void request_tile(const Pieces& pc, int from, int pie
   }
 }
 
+// After a wait that ran out: waits, again with a limit, until what was requested of the first `issued` tiles has landed.  Shared memory
+// is another CTA's as soon as this one has gone.  (Where all waits end, the MMA warps have seen every tile land.)
+template <int kStages>
+__device__ __forceinline__ void await_tiles(uint32_t bar_full, int issued) {
+#pragma unroll 1
+  for (int s = 0; s < kStages; ++s) {
+    const int uses = (issued - s + kStages - 1) / kStages;
+    if (uses > 0) mbar_wait(bar_full + 8 * s, (uses - 1) & 1);
+  }
+}
+
 __device__ __forceinline__ uint4 load_query(const PagedAttnParams& p, int b, int g, int tid) {
   uint4 qv = make_uint4(0u, 0u, 0u, 0u);
   const int64_t head0 = ((int64_t)b * p.n_q_heads + (int64_t)g * p.group) * kHeadDim;
@@ -403,6 +414,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       const int s = t % kStg, use = t / kStg;
       if (use > 0 && !mbar_wait(bar_empty + 8 * s, (use - 1) & 1)) {
         if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+        await_tiles<kStg>(bar_full, t);
         break;
       }
       request_tile(pc, (t % per) * pieces, piece, smem_base + s * kPStageBytes, sm_rows + 4 * s, bar_full + 8 * s, &tm_k, &tm_v,
@@ -424,6 +436,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     const int s = t % kStg;
     if (!mbar_wait(bar_full + 8 * s, (t / kStg) & 1)) {
       if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+      await_tiles<kStg>(bar_full, min(t + kStg, n_tiles));
       break;
     }
     const int rows = sm_rows[4 * s + wb];          // of this warp's block
@@ -620,6 +633,7 @@ paged_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         const int st = it % kBStages, use = it / kBStages;
         if (use > 0 && !mbar_wait(bar_empty + 8 * st, (use - 1) & 1)) {
           if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+          await_tiles<kBStages>(bar_full, it);
           return;
         }
         request_tile(pc, (i % per) * pieces, piece, smem_base + st * kPStageBytes, sm_rows + 4 * st, bar_full + 8 * st, &tm_k,
@@ -648,6 +662,7 @@ paged_balanced_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       const int st = it % kBStages;
       if (!mbar_wait(bar_full + 8 * st, (it / kBStages) & 1)) {
         if (lane == 0) atomicOr(p.status, RKV_DEV_TIMEOUT);
+        await_tiles<kBStages>(bar_full, it + kBStages);
         lost = true;   // a copy that never came: no further waits, but the warps still meet at the merges
         break;
       }
